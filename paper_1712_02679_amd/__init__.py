@@ -8,3 +8,6 @@ from .binding import (AdacompError, adacomp_compress, adacomp_compress_static, a
                       adacomp_timing_read, adacomp_unpack_accumulate, adacomp_unpack_update, OPT_SGD_MOMENTUM, OPT_ADAM, adacomp_workspace_bytes, adacomp_workspace_bytes_batch,
                       adacomp_workspace_gmax, adacomp_workspace_init, adacomp_workspace_release,
                       read_packet_summary, RULE_ADACOMP, RULE_PRINTED_COMPARE, RULE_LOCAL_SELECTION)
+from .layers import (LAYER_EXPORTS, Dropout, RelativeBias, adacomp_bias_softmax_backward, adacomp_bias_softmax_forward,  # noqa: F401
+                     adacomp_bias_softmax_workspace_bytes, adacomp_dropout, adacomp_norm_backward, adacomp_norm_forward,
+                     adacomp_norm_workspace_bytes, adacomp_relative_buckets)

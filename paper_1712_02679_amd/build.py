@@ -8,7 +8,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libadacomp.so")
-SOURCES = ["adacomp_api.hip", "adacomp_kernels.hip"]
+SOURCES = ["adacomp_api.hip", "adacomp_kernels.hip", "layers_api.hip", "layers_norm.hip", "layers_softmax.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

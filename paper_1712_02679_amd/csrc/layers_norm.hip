@@ -1,0 +1,297 @@
+// layers_norm.hip -- kernels of dropout and layer norm (adacomp_layers.h).
+#include "layers_device.h"
+
+namespace adacomp {
+
+// ---- dropout ------------------------------------------------------------------------------------------------------
+// y = [residual +] D(x).  One group of 8 columns to a thread and round; rows are cut into groups of their own, so that a
+// group is one counter wherever it lies.
+
+constexpr uint32_t kDropRounds = 4;
+
+template <typename T> __global__ __launch_bounds__(256) void k_dropout(DropoutLaunch a)
+{
+    const Drop d = drop_of(a.drop);
+    const uint32_t total = a.rows * a.groups;
+#pragma unroll
+    for (uint32_t u = 0; u < kDropRounds; ++u) {
+        const uint32_t g = (blockIdx.x * kDropRounds + u) * 256u + threadIdx.x;
+        if (g >= total) break;
+        const uint32_t r = g / a.groups, c = g - r * a.groups;
+        const uint64_t row = a.first_row + r;
+        const int n = int(a.cols - c * 8u);
+        f32x8 v = widen<T>(load8(static_cast<const T *>(a.x) + row * a.x_stride + c * 8ull, n));
+        v = drop8(v, d, c, uint32_t(row));
+        if (a.residual) v += widen<T>(load8(static_cast<const T *>(a.residual) + row * a.residual_stride + c * 8ull, n));
+        store8(static_cast<T *>(a.y) + row * a.y_stride + c * 8ull, n, v);
+    }
+}
+
+// ---- layer norm, forward ------------------------------------------------------------------------------------------
+// A row stays in the registers of its threads: mean first, then the squared distances from it.
+
+template <typename OP, int TPR> __device__ __forceinline__ float over_row(float x, float *room)
+{
+    if constexpr (TPR <= 64) return over_lanes<OP, TPR>(x);
+    else return over_waves<OP, TPR / 64>(over_lanes<OP, 64>(x), room);
+}
+
+template <typename T, int TPR, int V> __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_norm_forward(NormForward a)
+{
+    constexpr uint32_t TEAMS = TPR > 256 ? 1 : 256 / TPR;
+    __shared__ float room[2][16];
+    const uint32_t t = threadIdx.x % TPR;
+    uint32_t team = threadIdx.x / TPR;
+    if constexpr (TPR >= 64) team = __builtin_amdgcn_readfirstlane(team);
+    const Drop d = drop_of(a.drop);
+    for (uint32_t row = blockIdx.x * TEAMS + team; row < a.rows; row += gridDim.x * TEAMS) {
+        const T *x = static_cast<const T *>(a.x) + row * a.x_stride;
+        const T *res = a.residual ? static_cast<const T *>(a.residual) + row * a.residual_stride : nullptr;
+        f32x8 z[V];
+        float sum = 0.f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const uint32_t g = t + v * TPR;
+            const int n = int(a.cols) - int(g * 8u);
+            z[v] = widen<T>(load8(x + g * 8u, n));
+            if (a.drop.on) z[v] = drop8(z[v], d, g, row);
+            if (res) z[v] += widen<T>(load8(res + g * 8u, n));
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sum += z[v][k];
+        }
+        const float mean = over_row<Add, TPR>(sum, room[0]) / float(a.cols);
+        float squares = 0.f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int n = int(a.cols) - int((t + v * TPR) * 8u);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float c = k < n ? z[v][k] - mean : 0.f;
+                squares = fmaf(c, c, squares);
+            }
+        }
+        const float rstd = 1.f / sqrtf(over_row<Add, TPR>(squares, room[1]) / float(a.cols) + a.eps);
+        if (t == 0u) {
+            if (a.mean) a.mean[row] = mean;
+            if (a.rstd) a.rstd[row] = rstd;
+        }
+        T *y = static_cast<T *>(a.y) + row * a.y_stride;
+        T *zo = a.z ? static_cast<T *>(a.z) + row * a.z_stride : nullptr;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const uint32_t g = t + v * TPR;
+            const int n = int(a.cols) - int(g * 8u);
+            if (zo) store8(zo + g * 8u, n, z[v]);
+            f32x8 o = (z[v] - mean) * rstd;
+            if (a.gamma) o *= load8(a.gamma + g * 8u, n);
+            if (a.beta) o += load8(a.beta + g * 8u, n);
+            store8(y + g * 8u, n, o);
+        }    }
+}
+
+// ---- layer norm, backward -----------------------------------------------------------------------------------------
+// A workgroup walks over rows, each held in registers as in the forward pass, and keeps its columns' sums of dy h and of dy in
+// registers until its last row; k_norm_reduce adds the workgroups' sums up.
+
+template <typename T, int TPR, int V> __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_norm_backward(NormBackward a)
+{
+    constexpr uint32_t TEAMS = TPR > 256 ? 1 : 256 / TPR;
+    __shared__ float room[2][2][16];
+    __shared__ float sums[TEAMS > 1 ? TEAMS * TPR * V * 8 : 1];
+    const uint32_t t = threadIdx.x % TPR;
+    uint32_t team = threadIdx.x / TPR;
+    if constexpr (TPR >= 64) team = __builtin_amdgcn_readfirstlane(team);
+    const Drop d = drop_of(a.drop);
+    const float per_col = 1.f / float(a.cols);
+    f32x8 dgamma[V] = {}, dbeta[V] = {};
+    uint32_t turn = 0;
+    for (uint32_t row = blockIdx.x * TEAMS + team; row < a.rows; row += gridDim.x * TEAMS) {
+        const T *dy = static_cast<const T *>(a.dy) + row * a.dy_stride, *z = static_cast<const T *>(a.z) + row * a.z_stride;
+        const T *add = a.dz_add ? static_cast<const T *>(a.dz_add) + row * a.dz_add_stride : nullptr;
+        const float mean = a.mean[row], rstd = a.rstd[row];
+        f32x8 g[V], h[V];
+        float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const uint32_t c = (t + v * TPR) * 8u;
+            const int n = int(a.cols) - int(c);
+            g[v] = widen<T>(load8(dy + c, n));
+            h[v] = (widen<T>(load8(z + c, n)) - mean) * rstd;
+            dbeta[v] += g[v];
+            if (a.gamma) {
+                const f32x8 gamma = load8(a.gamma + c, n);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) dgamma[v][k] = fmaf(g[v][k], h[v][k], dgamma[v][k]);
+                g[v] *= gamma;
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) dgamma[v][k] = fmaf(g[v][k], h[v][k], dgamma[v][k]);
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                s1 += g[v][k];   // behind the row's end g is 0
+                s2 = fmaf(g[v][k], h[v][k], s2);
+            }
+        }
+        if constexpr (TPR <= 64) {
+            s1 = over_lanes<Add, TPR>(s1);
+            s2 = over_lanes<Add, TPR>(s2);
+        } else {
+            s1 = over_lanes<Add, 64>(s1);
+            s2 = over_lanes<Add, 64>(s2);
+            if (threadIdx.x % 64u == 0u) { room[turn][0][threadIdx.x / 64u] = s1; room[turn][1][threadIdx.x / 64u] = s2; }
+            __syncthreads();
+            s1 = s2 = 0.f;
+#pragma unroll
+            for (int w = 0; w < TPR / 64; ++w) { s1 += room[turn][0][w]; s2 += room[turn][1][w]; }
+            turn ^= 1u;
+        }
+        s1 *= per_col;
+        s2 *= per_col;
+        T *dz = static_cast<T *>(a.dz) + row * a.dz_stride;
+        T *dx = a.dx ? static_cast<T *>(a.dx) + row * a.dx_stride : nullptr;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const uint32_t c = (t + v * TPR) * 8u;
+            const int n = int(a.cols) - int(c);
+            f32x8 o = {};
+            if (add) o = widen<T>(load8(add + c, n));
+#pragma unroll
+            for (int k = 0; k < 8; ++k) o[k] = fmaf(rstd, g[v][k] - fmaf(h[v][k], s2, s1), o[k]);
+            store8(dz + c, n, o);
+            if (dx) store8(dx + c, n, drop8(o, d, c / 8u, row));
+        }
+    }
+    float *out = a.partial;
+    if (!out) return;
+    out += uint64_t(blockIdx.x) * 2u * a.pitch;
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        if constexpr (TEAMS > 1) {
+            __syncthreads();
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                *reinterpret_cast<f32x8 *>(&sums[(team * TPR * V + t + v * TPR) * 8u]) = which ? dbeta[v] : dgamma[v];
+            __syncthreads();
+            for (uint32_t c = threadIdx.x; c < a.pitch; c += 256u) {
+                float s = 0.f;
+                for (uint32_t m = 0; m < TEAMS; ++m) s += sums[m * TPR * V * 8u + c];
+                out[which * a.pitch + c] = s;
+            }
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const uint32_t c = (t + v * TPR) * 8u;
+                if (c < a.pitch) *reinterpret_cast<f32x8 *>(out + which * a.pitch + c) = which ? dbeta[v] : dgamma[v];
+            }
+        }
+    }
+}
+
+// 32 columns to a workgroup, 32 slices of the parts; always in the same order.
+__global__ __launch_bounds__(1024) void k_norm_reduce(NormReduce a)
+{
+    __shared__ float sums[32][33];
+    const uint32_t lane = threadIdx.x % 32u, slice = threadIdx.x / 32u;
+    const uint32_t c = blockIdx.x * 32u + lane, which = blockIdx.y;
+    float s = 0.f;
+    if (c < a.cols)
+#pragma unroll 8
+        for (uint32_t p = slice; p < a.parts; p += 32u) s += a.partial[(uint64_t(p) * 2u + which) * a.pitch + c];
+    sums[slice][lane] = s;
+    __syncthreads();
+    if (slice != 0u || c >= a.cols) return;
+    float *out = which ? a.dbeta : a.dgamma;
+    if (!out) return;
+    float all = 0.f;
+    for (uint32_t k = 0; k < 32u; ++k) all += sums[k][lane];
+    out[c] = a.accumulate ? out[c] + all : all;
+}
+
+// ---- launches -----------------------------------------------------------------------------------------------------
+
+static int check_launch() { return hipGetLastError() == hipSuccess ? ADACOMP_OK : ADACOMP_EHIP; }
+
+int launch_dropout(const DropoutLaunch &a, void *stream)
+{
+    const uint32_t total = a.rows * a.groups, per = 256u * kDropRounds;
+    const dim3 grid((total + per - 1u) / per), wg(256);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (a.dtype == ADACOMP_DTYPE_F32) hipLaunchKernelGGL(k_dropout<float>, grid, wg, 0, s, a);
+    else if (a.dtype == ADACOMP_DTYPE_BF16) hipLaunchKernelGGL(k_dropout<bf16>, grid, wg, 0, s, a);
+    else hipLaunchKernelGGL(k_dropout<f16>, grid, wg, 0, s, a);
+    return check_launch();
+}
+
+// The fewest threads that hold a row in up to 32 values each.
+RowForm norm_form(uint32_t cols)
+{
+    if (cols <= 64u) return {8, 1};
+    if (cols <= 128u) return {16, 1};
+    if (cols <= 256u) return {32, 1};
+    if (cols <= 512u) return {64, 1};
+    if (cols <= 1024u) return {64, 2};
+    if (cols <= 2048u) return {64, 4};
+    if (cols <= 4096u) return {256, 2};
+    if (cols <= 8192u) return {256, 4};
+    if (cols <= 16384u) return {1024, 2};
+    return {1024, 4};
+}
+
+constexpr uint32_t kMostWorkgroups = 1u << 20;   // a launch has fewer than 2^32 threads; more rows are walked over
+
+uint32_t norm_parts(uint64_t rows, uint32_t cols)
+{
+    const RowForm f = norm_form(cols);
+    const uint64_t all = (rows + f.teams() - 1u) / f.teams();
+    return uint32_t(std::min<uint64_t>(all, f.threads > 256u ? kComputeUnits : 4u * kComputeUnits));
+}
+
+template <template <typename, int, int> class K, typename A>
+static int launch_rows(const RowForm &f, uint32_t dtype, uint32_t workgroups, const A &a, void *stream)
+{
+    const dim3 grid(workgroups), wg(f.workgroup());
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    auto go = [&](auto form) {
+        constexpr int TPR = decltype(form)::threads, V = decltype(form)::groups;
+        if (dtype == ADACOMP_DTYPE_F32) hipLaunchKernelGGL((K<float, TPR, V>::kernel), grid, wg, 0, s, a);
+        else if (dtype == ADACOMP_DTYPE_BF16) hipLaunchKernelGGL((K<bf16, TPR, V>::kernel), grid, wg, 0, s, a);
+        else hipLaunchKernelGGL((K<f16, TPR, V>::kernel), grid, wg, 0, s, a);
+    };
+    switch (f.threads * 8u + f.groups) {
+    case 8 * 8 + 1: go(FormOf<8, 1>()); break;
+    case 16 * 8 + 1: go(FormOf<16, 1>()); break;
+    case 32 * 8 + 1: go(FormOf<32, 1>()); break;
+    case 64 * 8 + 1: go(FormOf<64, 1>()); break;
+    case 64 * 8 + 2: go(FormOf<64, 2>()); break;
+    case 64 * 8 + 4: go(FormOf<64, 4>()); break;
+    case 256 * 8 + 2: go(FormOf<256, 2>()); break;
+    case 256 * 8 + 4: go(FormOf<256, 4>()); break;
+    case 1024 * 8 + 2: go(FormOf<1024, 2>()); break;
+    case 1024 * 8 + 4: go(FormOf<1024, 4>()); break;
+    default: return ADACOMP_EINVAL;
+    }
+    return check_launch();
+}
+
+template <typename T, int TPR, int V> struct KForward { static constexpr auto kernel = k_norm_forward<T, TPR, V>; };
+template <typename T, int TPR, int V> struct KBackward { static constexpr auto kernel = k_norm_backward<T, TPR, V>; };
+
+int launch_norm_forward(const NormForward &a, uint32_t dtype, void *stream)
+{
+    const RowForm f = norm_form(a.cols);
+    return launch_rows<KForward>(f, dtype, std::min((a.rows + f.teams() - 1u) / f.teams(), kMostWorkgroups), a, stream);
+}
+
+int launch_norm_backward(const NormBackward &a, uint32_t dtype, uint32_t parts, void *stream)
+{
+    return launch_rows<KBackward>(norm_form(a.cols), dtype, parts, a, stream);
+}
+
+int launch_norm_reduce(const NormReduce &a, void *stream)
+{
+    hipLaunchKernelGGL(k_norm_reduce, dim3((a.cols + 31u) / 32u, 2), dim3(1024), 0, static_cast<hipStream_t>(stream), a);
+    return check_launch();
+}
+
+}  // namespace adacomp

@@ -1,0 +1,455 @@
+// layers_softmax.hip -- kernels of the masked softmax with a learned relative position bias (adacomp_layers.h).
+//
+// The bias of a place depends on its head and on clamp(key - query, -D, D) alone, so a workgroup, whose rows all belong to one
+// head, lays out the head's 2 D + 1 values in LDS once, in units of log2, and a place costs one LDS read; groups of 8 keys that lie
+// beyond D on one side cost none.  The gradient goes the same way back: sums by distance, added up in LDS (inside a row all
+// distances differ, so no two threads of a row meet, and rows follow each other), those beyond D in registers; k_bias_reduce
+// adds the workgroups' sums and only then turns distances into buckets.
+#include "layers_device.h"
+
+namespace adacomp {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kInf = __builtin_huge_valf();
+
+// Where distance x stands in LDS: neighbouring lanes read places 8 apart, and 9 apart they use different banks.
+__host__ __device__ constexpr uint32_t spread(uint32_t x) { return x + (x >> 3); }
+__host__ __device__ constexpr uint32_t spread_size(uint32_t distance) { return (spread(2u * distance) + 4u) & ~3u; }
+
+// A workgroup's copy of its head's bias, by distance, times log2(e).
+__device__ __forceinline__ void stage_bias(float *bias, const SoftmaxArgs &a, uint32_t head)
+{
+    for (uint32_t x = threadIdx.x; x <= 2u * a.distance; x += blockDim.x) {
+        const int32_t b = min(max(a.map[x], 0), int32_t(a.n_buckets) - 1);
+        bias[spread(x)] = a.table[uint64_t(b) * a.heads + head] * kLog2e;
+    }
+}
+
+// What a row looks at.
+struct Row {
+    const uint8_t *mask;   // NULL: none
+    int limit;             // keys below it are admitted, as far as the mask goes
+    int shift;             // distance index of key j: j + shift
+};
+
+__device__ __forceinline__ Row row_of(const SoftmaxArgs &a, uint32_t b, uint32_t h, uint32_t i)
+{
+    Row r;
+    const int64_t at = int64_t(a.query_starts ? a.query_starts[b] : a.query_start) + i;
+    int64_t limit = a.keys;
+    if (a.key_lengths) limit = min(limit, int64_t(a.key_lengths[b]));
+    if (a.causal) limit = min(limit, at + 1);
+    r.limit = int(max(limit, int64_t(0)));
+    // keys are below 2^30: a shift beyond these bounds is beyond D for every key either way
+    r.shift = int(min(max(int64_t(a.distance) - at, -(int64_t(1) << 30) - 8192), int64_t(1) << 30));
+    r.mask = a.mask.data ? static_cast<const uint8_t *>(a.mask.data) + int64_t(b) * a.mask.batch + int64_t(h) * a.mask.head + int64_t(i) * a.mask.row : nullptr;
+    return r;
+}
+
+// The admitted ones of 8 keys from j on, a bit each.  in_row: keys from j on that the row has.
+__device__ __forceinline__ uint32_t admitted8(const Row &r, int j, int in_row)
+{
+    const int n = r.limit - j;
+    uint32_t bits = n >= 8 ? 0xFFu : n > 0 ? (1u << n) - 1u : 0u;
+    if (r.mask && n > 0) {
+        typedef uint64_t at __attribute__((aligned(1)));
+        uint64_t m = 0;
+        if (in_row >= 8) m = *reinterpret_cast<const at *>(r.mask + j);
+        else
+            for (int k = 0; k < 7; ++k)
+                if (k < in_row) m |= uint64_t(r.mask[j + k]) << (8 * k);
+        uint32_t keep = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) keep |= ((m >> (8 * k)) & 0xFFu) ? 1u << k : 0u;
+        bits &= keep;
+    }
+    return bits;
+}
+
+// scale2 * s + bias of 8 keys from j on, -infinity where not admitted.
+__device__ __forceinline__ f32x8 biased8(f32x8 s, const SoftmaxArgs &a, const Row &r, const float *bias, int j, uint32_t bits)
+{
+    const int last = 2 * int(a.distance), x = j + r.shift;
+    f32x8 t;
+    if (x >= last || x <= -8) {
+        const float b = bias[x >= last ? spread(last) : 0u];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) t[k] = fmaf(s[k], a.scale2, b);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) t[k] = fmaf(s[k], a.scale2, bias[spread(uint32_t(min(max(x + k, 0), last)))]);
+    }
+    if (bits != 0xFFu) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) t[k] = bits >> k & 1u ? t[k] : -kInf;
+    }
+    return t;
+}
+
+template <int TPR> __device__ __forceinline__ uint32_t team_of()
+{
+    const uint32_t team = threadIdx.x / TPR;
+    if constexpr (TPR >= 64) return __builtin_amdgcn_readfirstlane(team);
+    return team;
+}
+
+// WHOLE: a row at a time.  STATS, WRITE: a part of a row, first its maximum and sum, then, from those of all parts, the results.
+enum Phase { WHOLE, STATS, WRITE };
+
+// ---- forward ------------------------------------------------------------------------------------------------------
+
+template <typename T, int TPR, int V, int PHASE> __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_softmax_forward(SoftmaxArgs a)
+{
+    constexpr uint32_t TEAMS = TPR > 256 ? 1 : 256 / TPR;
+    extern __shared__ float bias[];
+    __shared__ float room[2][2][16];
+    const uint32_t t = threadIdx.x % TPR, team = team_of<TPR>();
+    const Drop d = drop_of(a.drop);
+    uint32_t turn = 0;
+    const uint64_t blocks = uint64_t(a.batch) * a.heads * a.wgs_per_head * a.row_parts;
+    for (uint64_t block = blockIdx.x; block < blocks; block += gridDim.x) {
+    uint32_t unit = uint32_t(block), part = 0;
+    if constexpr (PHASE != WHOLE) { unit = uint32_t(block / a.row_parts); part = uint32_t(block - uint64_t(unit) * a.row_parts); }
+    const uint32_t bh = unit / a.wgs_per_head, first = (unit - bh * a.wgs_per_head) * a.rows_per_wg;
+    const uint32_t b = bh / a.heads, h = bh - b * a.heads;
+    if (block != blockIdx.x) __syncthreads();   // the rows before are done with the bias
+    stage_bias(bias, a, h);
+    __syncthreads();
+    const T *scores = static_cast<const T *>(a.scores.data) + int64_t(b) * a.scores.batch + int64_t(h) * a.scores.head;
+    T *out = static_cast<T *>(const_cast<void *>(a.out.data)) + int64_t(b) * a.out.batch + int64_t(h) * a.out.head;
+    const int base = int(part * (TPR * V * 8u));
+    for (uint32_t i = first + team; i < min(first + a.rows_per_wg, a.queries); i += TEAMS) {
+        const Row r = row_of(a, b, h, i);
+        const T *s = scores + int64_t(i) * a.scores.row;
+        f32x8 p[V];
+        uint32_t bits = 0;   // admitted places, 8 to a group
+        float m = -kInf;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int j = base + int(t + v * TPR) * 8, in_row = int(a.keys) - j;
+            p[v] = -kInf;
+            if (j < r.limit) {
+                const uint32_t here = admitted8(r, j, in_row);
+                bits |= here << (8 * v);
+                p[v] = biased8(widen<T>(load8(s + j, in_row)), a, r, bias, j, here);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) m = fmaxf(m, p[v][k]);
+            }
+        }
+        // exponentials from the maximum of a team's lanes of one wave; the waves' sums are joined behind them
+        m = over_lanes<Max, (TPR > 64 ? 64 : TPR)>(m);
+        const float from = m == -kInf ? 0.f : m;
+        float l = 0.f;
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                p[v][k] = __builtin_amdgcn_exp2f(p[v][k] - from);
+                l += p[v][k];
+            }
+        l = over_lanes<Add, (TPR > 64 ? 64 : TPR)>(l);
+        float top = m, total = l;
+        if constexpr (TPR > 64) {
+            if (threadIdx.x % 64u == 0u) { room[turn][0][threadIdx.x / 64u] = m; room[turn][1][threadIdx.x / 64u] = l; }
+            __syncthreads();
+            top = -kInf;
+#pragma unroll
+            for (int w = 0; w < TPR / 64; ++w) top = fmaxf(top, room[turn][0][w]);
+            const float from_top = top == -kInf ? 0.f : top;
+            total = 0.f;
+#pragma unroll
+            for (int w = 0; w < TPR / 64; ++w) total = fmaf(room[turn][1][w], __builtin_amdgcn_exp2f(room[turn][0][w] - from_top), total);
+            turn ^= 1u;
+        }
+        const uint64_t row = uint64_t(bh) * a.queries + i;
+        if constexpr (PHASE == STATS) {
+            if (threadIdx.x == 0u) {
+                float *to = a.part_stats + (row * a.row_parts + part) * 2u;
+                to[0] = top;
+                to[1] = total;
+            }
+            continue;
+        }
+        if constexpr (PHASE == WRITE) {
+            const float *of = a.part_stats + row * a.row_parts * 2u;
+            top = -kInf;
+            for (uint32_t q = 0; q < a.row_parts; ++q) top = fmaxf(top, of[2u * q]);
+            const float from_top = top == -kInf ? 0.f : top;
+            total = 0.f;
+            for (uint32_t q = 0; q < a.row_parts; ++q) total = fmaf(of[2u * q + 1u], __builtin_amdgcn_exp2f(of[2u * q] - from_top), total);
+        }
+        const float factor = total == 0.f ? 0.f : __builtin_amdgcn_exp2f(from - (top == -kInf ? 0.f : top)) / total;
+        if (a.lse && t == 0u && part == 0u) a.lse[row] = total == 0.f ? -kInf : (top + log2f(total)) * kLn2;
+        T *o = out + int64_t(i) * a.out.row;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int j = base + int(t + v * TPR) * 8, in_row = int(a.keys) - j;
+            if (in_row <= 0) break;
+            f32x8 y;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) y[k] = bits >> (8 * v + k) & 1u ? p[v][k] * factor : 0.f;
+            if (a.drop.on) y = drop8(y, d, uint32_t(j) / 8u, uint32_t(row));
+            store8(o + j, in_row, y);
+        }
+    }
+    }
+}
+
+// ---- backward -----------------------------------------------------------------------------------------------------
+
+template <typename T, int TPR, int V, int PHASE> __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_softmax_backward(SoftmaxArgs a)
+{
+    constexpr uint32_t TEAMS = TPR > 256 ? 1 : 256 / TPR, WG = TPR > 256 ? TPR : 256;
+    extern __shared__ float lds[];
+    __shared__ float room[2][16];
+    const uint32_t t = threadIdx.x % TPR, team = team_of<TPR>();
+    const uint32_t size = spread_size(a.distance);
+    const int last = 2 * int(a.distance);
+    float *bias = lds, *acc = lds + size * (1u + team);   // every team has sums of its own
+    const bool sums = PHASE != STATS && a.bias_sums;
+    const uint32_t h = blockIdx.x / a.wgs_per_head, group = blockIdx.x - h * a.wgs_per_head;
+    const Drop d = drop_of(a.drop);
+    stage_bias(bias, a, h);
+    if (sums)
+        for (uint32_t x = threadIdx.x; x < size * TEAMS; x += WG) lds[size + x] = 0.f;
+    __syncthreads();
+    float low = 0.f, high = 0.f;   // sums of e at the ends of the map
+    const uint64_t units = uint64_t(a.batch) * a.queries * a.row_parts;
+    uint32_t turn = 0;
+    for (uint64_t unit = uint64_t(group) * TEAMS + team; unit < units; unit += uint64_t(a.wgs_per_head) * TEAMS) {
+        uint32_t row_of_head = uint32_t(unit), part = 0;
+        if constexpr (PHASE != WHOLE) { row_of_head = uint32_t(unit / a.row_parts); part = uint32_t(unit - uint64_t(row_of_head) * a.row_parts); }
+        const uint32_t b = row_of_head / a.queries, i = row_of_head - b * a.queries;
+        const int base = int(part * (TPR * V * 8u));
+        const Row r = row_of(a, b, h, i);
+        const uint64_t row = (uint64_t(b) * a.heads + h) * a.queries + i;
+        const T *s = static_cast<const T *>(a.scores.data) + int64_t(b) * a.scores.batch + int64_t(h) * a.scores.head + int64_t(i) * a.scores.row;
+        const T *up = static_cast<const T *>(a.in.data) + int64_t(b) * a.in.batch + int64_t(h) * a.in.head + int64_t(i) * a.in.row;
+        T *o = static_cast<T *>(const_cast<void *>(a.out.data)) + int64_t(b) * a.out.batch + int64_t(h) * a.out.head + int64_t(i) * a.out.row;
+        const float lse = a.lse[row], lse2 = lse == -kInf ? kInf : lse * kLog2e;
+        f32x8 p[V], dp[V];
+        float inner = 0.f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int j = base + int(t + v * TPR) * 8, in_row = int(a.keys) - j;
+            p[v] = 0.f;
+            dp[v] = 0.f;
+            if (j < r.limit) {
+                const uint32_t bits = admitted8(r, j, in_row);
+                p[v] = biased8(widen<T>(load8(s + j, in_row)), a, r, bias, j, bits);
+                dp[v] = widen<T>(load8(up + j, in_row));
+                if (a.drop.on) dp[v] = drop8(dp[v], d, uint32_t(j) / 8u, uint32_t(row));
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const bool on = bits >> k & 1u;
+                    p[v][k] = on ? __builtin_amdgcn_exp2f(p[v][k] - lse2) : 0.f;
+                    dp[v][k] = on ? dp[v][k] : 0.f;
+                    inner = fmaf(p[v][k], dp[v][k], inner);
+                }
+            }
+        }
+        if constexpr (PHASE != WRITE) {
+            inner = over_lanes<Add, (TPR > 64 ? 64 : TPR)>(inner);
+            if constexpr (TPR > 64) {
+                inner = over_waves<Add, TPR / 64>(inner, room[turn]);
+                turn ^= 1u;
+            }
+        }
+        if constexpr (PHASE == STATS) {
+            if (t == 0u) a.part_stats[(row * a.row_parts + part) * 2u] = inner;
+            continue;
+        }
+        if constexpr (PHASE == WRITE) {
+            inner = 0.f;
+            for (uint32_t q = 0; q < a.row_parts; ++q) inner += a.part_stats[(row * a.row_parts + q) * 2u];
+        }
+        if (sums) {   // the rows before this one are done with the sums
+            if constexpr (TPR > 64) __syncthreads();
+            else {
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+            }
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int j = base + int(t + v * TPR) * 8, in_row = int(a.keys) - j;
+            if (in_row <= 0) break;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) p[v][k] *= dp[v][k] - inner;
+            store8(o + j, in_row, p[v] * a.scale);
+            if (sums && j < r.limit) {
+                const int x = j + r.shift;
+                if (x >= last || x <= -8) {
+                    float e = 0.f;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) e += p[v][k];
+                    (x >= last ? high : low) += e;
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        if (x + k <= 0) low += p[v][k];
+                        else if (x + k >= last) high += p[v][k];
+                        else acc[spread(uint32_t(x + k))] += p[v][k];
+                    }
+                }
+            }
+        }
+    }
+    if constexpr (PHASE == STATS) return;
+    if (!sums) return;
+    constexpr int LANES = TPR > 64 ? 64 : TPR;
+    low = over_lanes<Add, LANES>(low);
+    high = over_lanes<Add, LANES>(high);
+    __syncthreads();
+    if constexpr (TPR > 64) {
+        low = over_waves<Add, TPR / 64>(low, room[0]);
+        high = over_waves<Add, TPR / 64>(high, room[1]);
+    }
+    if (t == 0u) {
+        acc[0] = low;
+        acc[spread(uint32_t(last))] = high;
+    }
+    __syncthreads();
+    float *to = a.bias_sums + uint64_t(blockIdx.x) * (uint32_t(last) + 1u);
+    for (uint32_t x = threadIdx.x; x <= uint32_t(last); x += WG) {
+        float e = 0.f;
+        for (uint32_t m = 0; m < TEAMS; ++m) e += lds[size * (1u + m) + spread(x)];
+        to[x] = e;
+    }
+}
+
+// A workgroup to a head: the sums of its workgroups, 16 slices of them at a time, then the distances of each bucket.
+__global__ __launch_bounds__(1024) void k_bias_reduce(BiasReduce a)
+{
+    extern __shared__ float sums[];   // [2 D + 1]
+    __shared__ float slices[16][65];
+    const uint32_t n = 2u * a.distance + 1u, h = blockIdx.x, lane = threadIdx.x % 64u, wave = threadIdx.x / 64u;
+    const float *from = a.bias_sums + uint64_t(h) * a.groups * n;
+    for (uint32_t x0 = 0; x0 < n; x0 += 64u) {
+        float e = 0.f;
+        if (x0 + lane < n)
+#pragma unroll 4
+            for (uint32_t g = wave; g < a.groups; g += 16u) e += from[uint64_t(g) * n + x0 + lane];
+        slices[wave][lane] = e;
+        __syncthreads();
+        if (wave == 0u && x0 + lane < n) {
+            float all = 0.f;
+#pragma unroll
+            for (int w = 0; w < 16; ++w) all += slices[w][lane];
+            sums[x0 + lane] = all;
+        }
+        __syncthreads();
+    }
+    for (uint32_t k = wave; k < a.n_buckets; k += 16u) {
+        float e = 0.f;
+        for (uint32_t x = lane; x < n; x += 64u) {
+            const uint32_t b = uint32_t(min(max(a.map[x], 0), int32_t(a.n_buckets) - 1));
+            e += b == k ? sums[x] : 0.f;
+        }
+        e = over_lanes<Add, 64>(e);
+        if (lane == 0u) {
+            float *to = a.dtable + uint64_t(k) * a.heads + h;
+            *to = a.accumulate ? *to + e : e;
+        }
+    }
+}
+
+// ---- launches -----------------------------------------------------------------------------------------------------
+
+static int check_launch() { return hipGetLastError() == hipSuccess ? ADACOMP_OK : ADACOMP_EHIP; }
+
+constexpr uint32_t kPartThreads = 256, kPartGroups = 4, kPartKeys = kPartThreads * kPartGroups * 8u;
+
+constexpr uint32_t kLdsMost = 64u << 10;   // of a workgroup
+
+// The fewest threads that hold a row in up to 32 values each; in the backward pass so many that the copies of the sums by
+// distance, one for each row that a workgroup has in hand, fit LDS beside the bias.
+SoftmaxForm softmax_form(uint32_t keys, uint32_t distance, bool backward)
+{
+    if (backward) {
+        const uint32_t copies = kLdsMost / (4u * spread_size(distance)) - 1u;
+        keys = std::max(keys, copies >= 32u ? 0u : copies >= 16u ? 65u : copies >= 8u ? 129u : copies >= 4u ? 257u : 2049u);
+    }
+    if (keys <= 64u) return {{8, 1}, 1};
+    if (keys <= 128u) return {{16, 1}, 1};
+    if (keys <= 256u) return {{32, 1}, 1};
+    if (keys <= 512u) return {{64, 1}, 1};
+    if (keys <= 1024u) return {{64, 2}, 1};
+    if (keys <= 2048u) return {{64, 4}, 1};
+    if (keys <= 4096u) return {{256, 2}, 1};
+    if (keys <= 8192u) return {{256, 4}, 1};
+    if (keys <= 16384u) return {{1024, 2}, 1};
+    return {{kPartThreads, kPartGroups}, (keys + kPartKeys - 1u) / kPartKeys};
+}
+
+uint32_t softmax_back_groups(uint64_t rows_of_head, uint32_t heads, const SoftmaxForm &f)
+{
+    const uint64_t all = (rows_of_head * f.parts + f.row.teams() - 1u) / f.row.teams();
+    const uint32_t wanted = ((f.row.threads > 256u ? 1u : 4u) * kComputeUnits + heads - 1u) / heads;
+    return uint32_t(std::min<uint64_t>(all, wanted));
+}
+
+constexpr uint32_t kMostWorkgroups = 1u << 20;   // a launch has fewer than 2^32 threads; what is left is walked over
+
+template <template <typename, int, int, int> class K>
+static int launch_form(const SoftmaxArgs &a, uint32_t dtype, const SoftmaxForm &f, uint32_t workgroups, uint32_t lds, void *stream)
+{
+    const dim3 grid(workgroups), wg(f.row.workgroup());
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    auto go = [&](auto form, auto phase) {
+        constexpr int TPR = decltype(form)::threads, V = decltype(form)::groups, PHASE = decltype(phase)::value;
+        if (dtype == ADACOMP_DTYPE_F32) hipLaunchKernelGGL((K<float, TPR, V, PHASE>::kernel), grid, wg, lds, s, a);
+        else if (dtype == ADACOMP_DTYPE_BF16) hipLaunchKernelGGL((K<bf16, TPR, V, PHASE>::kernel), grid, wg, lds, s, a);
+        else hipLaunchKernelGGL((K<f16, TPR, V, PHASE>::kernel), grid, wg, lds, s, a);
+    };
+    using Whole = std::integral_constant<int, WHOLE>;
+    if (f.parts > 1u) {
+        go(FormOf<kPartThreads, kPartGroups>(), std::integral_constant<int, STATS>());
+        if (int rc = check_launch()) return rc;
+        go(FormOf<kPartThreads, kPartGroups>(), std::integral_constant<int, WRITE>());
+        return check_launch();
+    }
+    switch (f.row.threads * 8u + f.row.groups) {
+    case 8 * 8 + 1: go(FormOf<8, 1>(), Whole()); break;
+    case 16 * 8 + 1: go(FormOf<16, 1>(), Whole()); break;
+    case 32 * 8 + 1: go(FormOf<32, 1>(), Whole()); break;
+    case 64 * 8 + 1: go(FormOf<64, 1>(), Whole()); break;
+    case 64 * 8 + 2: go(FormOf<64, 2>(), Whole()); break;
+    case 64 * 8 + 4: go(FormOf<64, 4>(), Whole()); break;
+    case 256 * 8 + 2: go(FormOf<256, 2>(), Whole()); break;
+    case 256 * 8 + 4: go(FormOf<256, 4>(), Whole()); break;
+    case 1024 * 8 + 2: go(FormOf<1024, 2>(), Whole()); break;
+    default: return ADACOMP_EINVAL;
+    }
+    return check_launch();
+}
+
+template <typename T, int TPR, int V, int PHASE> struct KForward { static constexpr auto kernel = k_softmax_forward<T, TPR, V, PHASE>; };
+template <typename T, int TPR, int V, int PHASE> struct KBackward { static constexpr auto kernel = k_softmax_backward<T, TPR, V, PHASE>; };
+
+int launch_softmax_forward(const SoftmaxArgs &args, uint32_t dtype, const SoftmaxForm &f, void *stream)
+{
+    SoftmaxArgs a = args;
+    a.rows_per_wg = f.parts > 1u ? 1u : 4u * f.row.teams();
+    a.wgs_per_head = (a.queries + a.rows_per_wg - 1u) / a.rows_per_wg;
+    a.row_parts = f.parts;
+    const uint64_t blocks = uint64_t(a.batch) * a.heads * a.wgs_per_head * f.parts;
+    return launch_form<KForward>(a, dtype, f, uint32_t(std::min<uint64_t>(blocks, kMostWorkgroups)), 4u * spread_size(a.distance), stream);
+}
+
+int launch_softmax_backward(const SoftmaxArgs &args, uint32_t dtype, const SoftmaxForm &f, void *stream)
+{
+    SoftmaxArgs a = args;
+    a.wgs_per_head = softmax_back_groups(uint64_t(a.batch) * a.queries, a.heads, f);
+    a.row_parts = f.parts;
+    const uint32_t copies = 1u + (a.bias_sums ? f.row.teams() : 0u);
+    return launch_form<KBackward>(a, dtype, f, a.heads * a.wgs_per_head, 4u * spread_size(a.distance) * copies, stream);
+}
+
+int launch_bias_reduce(const BiasReduce &a, void *stream)
+{
+    hipLaunchKernelGGL(k_bias_reduce, dim3(a.heads), dim3(1024), 4u * (2u * a.distance + 1u), static_cast<hipStream_t>(stream), a);
+    return check_launch();
+}
+
+}  // namespace adacomp
