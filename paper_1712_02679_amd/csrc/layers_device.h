@@ -18,35 +18,112 @@ template <typename T> struct Raw;
 template <> struct Raw<float> { typedef float vec __attribute__((ext_vector_type(8))); typedef vec at __attribute__((aligned(4))); };
 template <> struct Raw<bf16> { typedef bf16 vec __attribute__((ext_vector_type(8))); typedef vec at __attribute__((aligned(2))); };
 template <> struct Raw<f16> { typedef f16 vec __attribute__((ext_vector_type(8))); typedef vec at __attribute__((aligned(2))); };
+template <> struct Raw<uint8_t> { typedef uint8_t vec __attribute__((ext_vector_type(8))); typedef vec at __attribute__((aligned(1))); };
 template <typename T> using raw8 = typename Raw<T>::vec;
 
-// The first n of 8 values (n >= 8: all, n <= 0: none), zeros behind them.
-template <typename T> __device__ __forceinline__ raw8<T> load8(const T *p, int n)
+// Value `at` of a row: a 32-bit offset from an address that the wave shares.
+template <typename T> __device__ __forceinline__ T *at(T *row, uint32_t col)
+{
+    return reinterpret_cast<T *>(reinterpret_cast<uintptr_t>(row) + uint32_t(col * sizeof(T)));
+}
+
+template <typename T> __device__ __forceinline__ raw8<T> load8(const T *p) { return *reinterpret_cast<const typename Raw<T>::at *>(p); }
+template <typename T> __device__ __forceinline__ raw8<T> narrow(f32x8 x) { return __builtin_convertvector(x, raw8<T>); }
+template <typename T> __device__ __forceinline__ void store8(T *p, f32x8 x) { *reinterpret_cast<typename Raw<T>::at *>(p) = narrow<T>(x); }
+
+// The first n of 8 values, 0 < n < 8, zeros behind them.
+template <typename T> __device__ __forceinline__ raw8<T> load_some(const T *p, uint32_t n)
 {
     raw8<T> v = {};
-    if (n >= 8) {
-        v = *reinterpret_cast<const typename Raw<T>::at *>(p);
-    } else if (n > 0) {
 #pragma unroll
-        for (int k = 0; k < 7; ++k)
-            if (k < n) v[k] = p[k];
-    }
+    for (uint32_t k = 0; k < 7u; ++k)
+        if (k < n) v[k] = p[k];
     return v;
 }
 
-template <typename T> __device__ __forceinline__ void store8(T *p, int n, f32x8 x)
+template <typename T> __device__ __forceinline__ void store_some(T *p, uint32_t n, f32x8 x)
 {
-    const raw8<T> v = __builtin_convertvector(x, raw8<T>);
-    if (n >= 8) {
-        *reinterpret_cast<typename Raw<T>::at *>(p) = v;
-    } else if (n > 0) {
+    const raw8<T> v = narrow<T>(x);
 #pragma unroll
-        for (int k = 0; k < 7; ++k)
-            if (k < n) p[k] = v[k];
-    }
+    for (uint32_t k = 0; k < 7u; ++k)
+        if (k < n) p[k] = v[k];
 }
 
+// The groups of a row that a thread has: group t + v TPR in round v, `cols` columns in all.  At most one group of a row is
+// incomplete; it is handled apart, once, so that the rounds have one form.
+template <typename T, int TPR, int V> struct RowGroups {
+    uint32_t t, cols, first;   // first: column of the part of the row that the threads hold
+    __device__ __forceinline__ uint32_t col(int v) const { return first + (t + uint32_t(v) * TPR) * 8u; }
+    __device__ __forceinline__ bool whole(int v) const { return col(v) + 8u <= cols; }
+    // the round in which this thread has the incomplete group; V: it has none
+    __device__ __forceinline__ uint32_t tail() const
+    {
+        const uint32_t g = cols / 8u - first / 8u;
+        return cols % 8u != 0u && cols > first && g % TPR == t ? g / TPR : uint32_t(V);
+    }
+    // the row's values, zeros behind its end
+    __device__ __forceinline__ void load(raw8<T> (&raw)[V], const T *row) const
+    {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            raw[v] = raw8<T>{};
+            if (whole(v)) raw[v] = load8(at(row, col(v)));
+        }
+        load_tail(raw, row, cols);
+    }
+    // values of columns below `upto` and of their groups, anything elsewhere: no branch, what is not wanted is read where the row begins
+    __device__ __forceinline__ void load_below(raw8<T> (&raw)[V], const T *row, uint32_t upto) const
+    {
+        if (cols >= 8u) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) raw[v] = load8(at(row, whole(v) && col(v) < upto ? col(v) : 0u));
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) raw[v] = raw8<T>{};
+        }
+        load_tail(raw, row, upto);
+    }
+    // the rounds one by one: the values of round v, of which `some` are the incomplete group's
+    __device__ __forceinline__ raw8<T> some(const T *row) const
+    {
+        return cols % 8u != 0u && tail() < uint32_t(V) ? load_some(at(row, cols & ~7u), cols % 8u) : raw8<T>{};
+    }
+    __device__ __forceinline__ raw8<T> round(const T *row, int v, const raw8<T> &some) const { return whole(v) ? load8(at(row, col(v))) : some; }
+    __device__ __forceinline__ void load_tail(raw8<T> (&raw)[V], const T *row, uint32_t upto) const
+    {
+        if (cols % 8u == 0u) return;
+        const uint32_t mine = tail();
+        if (mine < uint32_t(V) && (cols & ~7u) < upto) {
+            const raw8<T> some = load_some(at(row, cols & ~7u), cols % 8u);
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                if (uint32_t(v) == mine) raw[v] = some;
+        }
+    }
+    // x[v] of every round, by a function that makes it
+    template <typename F> __device__ __forceinline__ void store(T *row, F &&x) const
+    {
+        const uint32_t mine = cols % 8u == 0u ? uint32_t(V) : tail();
+        f32x8 some = {};
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            if (col(v) < cols) {
+                const f32x8 y = x(v);
+                if (whole(v)) store8(at(row, col(v)), y);
+                else some = y;
+            }
+        }
+        if (mine < uint32_t(V)) store_some(at(row, cols & ~7u), cols % 8u, some);
+    }
+};
+
 template <typename T> __device__ __forceinline__ f32x8 widen(raw8<T> v) { return __builtin_convertvector(v, f32x8); }
+
+// A value that the compiler takes for a new one: what is made from it inside a loop is made there.  Otherwise everything about
+// a row that its threads and length decide moves in front of the loop over rows, and costs it its registers: scalar ones
+// spilled to lanes of a vector register and read back every time.
+__device__ __forceinline__ uint32_t again_uniform(uint32_t x) { asm volatile("" : "+s"(x)); return x; }
+__device__ __forceinline__ uint32_t again(uint32_t x) { asm volatile("" : "+v"(x)); return x; }
 
 // ---- dropout: Philox-4x32 with 7 rounds ---------------------------------------------------------------------------
 // A round takes two 32 x 32 -> 64 bit products, at a quarter of the rate of other instructions; 7 rounds (the least that
@@ -65,7 +142,13 @@ __device__ __forceinline__ Drop drop_of(const DropArgs &a)
     return {a.seed_lo, a.seed_hi, uint32_t(stream), uint32_t(stream >> 32), a.threshold, a.factor};
 }
 
-__device__ __forceinline__ f32x8 drop8(f32x8 v, const Drop &d, uint32_t group, uint32_t row)
+__device__ __forceinline__ Drop again(const Drop &d)
+{
+    return {again_uniform(d.seed_lo), again_uniform(d.seed_hi), d.stream_lo, d.stream_hi, d.threshold, d.factor};
+}
+
+// The 16-bit numbers of a group's 8 columns, two to a word.
+__device__ __forceinline__ void numbers8(uint32_t (&w)[4], const Drop &d, uint32_t group, uint32_t row)
 {
     uint32_t c0 = group, c1 = row, c2 = d.stream_lo, c3 = d.stream_hi, k0 = d.seed_lo, k1 = d.seed_hi;
 #pragma unroll
@@ -78,13 +161,28 @@ __device__ __forceinline__ f32x8 drop8(f32x8 v, const Drop &d, uint32_t group, u
         k0 += 0x9E3779B9u;
         k1 += 0xBB67AE85u;
     }
-    const uint32_t w[4] = {c0, c1, c2, c3};
+    w[0] = c0;
+    w[1] = c1;
+    w[2] = c2;
+    w[3] = c3;
+}
+
+// Zeros in place of what is dropped; the factor is left to the caller.
+__device__ __forceinline__ f32x8 kept8(f32x8 v, const Drop &d, uint32_t group, uint32_t row)
+{
+    uint32_t w[4];
+    numbers8(w, d, group, row);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-        const uint32_t half = k % 2 ? w[k / 2] >> 16 : w[k / 2] & 0xFFFFu;
-        v[k] = half >= d.threshold ? v[k] * d.factor : 0.f;
+        const uint16_t number = uint16_t(k % 2 ? w[k / 2] >> 16 : w[k / 2]);
+        v[k] = number >= uint16_t(d.threshold) ? v[k] : 0.f;
     }
     return v;
+}
+
+__device__ __forceinline__ f32x8 drop8(f32x8 v, const Drop &d, uint32_t group, uint32_t row)
+{
+    return kept8(v, d, group, row) * d.factor;
 }
 
 // A kernel's form as a type, for the functions that pick a kernel.

@@ -19,11 +19,21 @@ template <typename T> __global__ __launch_bounds__(256) void k_dropout(DropoutLa
         if (g >= total) break;
         const uint32_t r = g / a.groups, c = g - r * a.groups;
         const uint64_t row = a.first_row + r;
-        const int n = int(a.cols - c * 8u);
-        f32x8 v = widen<T>(load8(static_cast<const T *>(a.x) + row * a.x_stride + c * 8ull, n));
-        v = drop8(v, d, c, uint32_t(row));
-        if (a.residual) v += widen<T>(load8(static_cast<const T *>(a.residual) + row * a.residual_stride + c * 8ull, n));
-        store8(static_cast<T *>(a.y) + row * a.y_stride + c * 8ull, n, v);
+        const uint32_t n = a.cols - c * 8u;
+        const T *x = static_cast<const T *>(a.x) + row * a.x_stride + c * 8ull, *res = static_cast<const T *>(a.residual) + row * a.residual_stride + c * 8ull;
+        T *y = static_cast<T *>(a.y) + row * a.y_stride + c * 8ull;
+        raw8<T> raw = {}, raw_res = {};
+        if (n >= 8u) {
+            raw = load8(x);
+            if (a.residual) raw_res = load8(res);
+        } else {
+            raw = load_some(x, n);
+            if (a.residual) raw_res = load_some(res, n);
+        }
+        f32x8 v = drop8(widen<T>(raw), d, c, uint32_t(row));
+        if (a.residual) v += widen<T>(raw_res);
+        if (n >= 8u) store8(y, v);
+        else store_some(y, n, v);
     }
 }
 
@@ -47,46 +57,52 @@ template <typename T, int TPR, int V> __global__ __launch_bounds__(TPR > 256 ? T
     for (uint32_t row = blockIdx.x * TEAMS + team; row < a.rows; row += gridDim.x * TEAMS) {
         const T *x = static_cast<const T *>(a.x) + row * a.x_stride;
         const T *res = a.residual ? static_cast<const T *>(a.residual) + row * a.residual_stride : nullptr;
+        const uint32_t cols = again_uniform(a.cols);
+        const RowGroups<T, TPR, V> groups = {again(t), cols, 0};
+        const Drop dr = again(d);
+        raw8<T> raw[V], raw_res[V];
+        groups.load(raw, x);
+        if (res) groups.load(raw_res, res);
         f32x8 z[V];
         float sum = 0.f;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const uint32_t g = t + v * TPR;
-            const int n = int(a.cols) - int(g * 8u);
-            z[v] = widen<T>(load8(x + g * 8u, n));
-            if (a.drop.on) z[v] = drop8(z[v], d, g, row);
-            if (res) z[v] += widen<T>(load8(res + g * 8u, n));
+            z[v] = widen<T>(raw[v]);
+            if (a.drop.on) z[v] = drop8(z[v], dr, groups.col(v) / 8u, row);
+            if (res) z[v] += widen<T>(raw_res[v]);
 #pragma unroll
             for (int k = 0; k < 8; ++k) sum += z[v][k];
         }
         const float mean = over_row<Add, TPR>(sum, room[0]) / float(a.cols);
         float squares = 0.f;
+        f32x8 c[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int n = int(a.cols) - int((t + v * TPR) * 8u);
+            c[v] = z[v] - mean;
+            if (!groups.whole(v)) {   // nothing behind the row's end counts
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const float c = k < n ? z[v][k] - mean : 0.f;
-                squares = fmaf(c, c, squares);
+                for (int k = 0; k < 8; ++k) c[v][k] = groups.col(v) + k < cols ? c[v][k] : 0.f;
             }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) squares = fmaf(c[v][k], c[v][k], squares);
         }
         const float rstd = 1.f / sqrtf(over_row<Add, TPR>(squares, room[1]) / float(a.cols) + a.eps);
         if (t == 0u) {
             if (a.mean) a.mean[row] = mean;
             if (a.rstd) a.rstd[row] = rstd;
         }
-        T *y = static_cast<T *>(a.y) + row * a.y_stride;
-        T *zo = a.z ? static_cast<T *>(a.z) + row * a.z_stride : nullptr;
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const uint32_t g = t + v * TPR;
-            const int n = int(a.cols) - int(g * 8u);
-            if (zo) store8(zo + g * 8u, n, z[v]);
-            f32x8 o = (z[v] - mean) * rstd;
-            if (a.gamma) o *= load8(a.gamma + g * 8u, n);
-            if (a.beta) o += load8(a.beta + g * 8u, n);
-            store8(y + g * 8u, n, o);
-        }    }
+        if (a.z) groups.store(static_cast<T *>(a.z) + row * a.z_stride, [&](int v) { return z[v]; });
+        const RowGroups<float, TPR, V> params = {groups.t, cols, 0};
+        raw8<float> some_gamma, some_beta;
+        if (a.gamma) some_gamma = params.some(a.gamma);
+        if (a.beta) some_beta = params.some(a.beta);
+        groups.store(static_cast<T *>(a.y) + row * a.y_stride, [&](int v) {
+            f32x8 y = c[v] * rstd;
+            if (a.gamma) y *= params.round(a.gamma, v, some_gamma);
+            if (a.beta) y += params.round(a.beta, v, some_beta);
+            return y;
+        });
+    }
 }
 
 // ---- layer norm, backward -----------------------------------------------------------------------------------------
@@ -104,29 +120,27 @@ template <typename T, int TPR, int V> __global__ __launch_bounds__(TPR > 256 ? T
     const Drop d = drop_of(a.drop);
     const float per_col = 1.f / float(a.cols);
     f32x8 dgamma[V] = {}, dbeta[V] = {};
+    raw8<float> gamma[V];
+    if (a.gamma) RowGroups<float, TPR, V>{t, a.cols, 0}.load(gamma, a.gamma);
     uint32_t turn = 0;
     for (uint32_t row = blockIdx.x * TEAMS + team; row < a.rows; row += gridDim.x * TEAMS) {
-        const T *dy = static_cast<const T *>(a.dy) + row * a.dy_stride, *z = static_cast<const T *>(a.z) + row * a.z_stride;
-        const T *add = a.dz_add ? static_cast<const T *>(a.dz_add) + row * a.dz_add_stride : nullptr;
+        const RowGroups<T, TPR, V> groups = {again(t), again_uniform(a.cols), 0};
+        const Drop dr = again(d);
+        raw8<T> raw_dy[V], raw_z[V], raw_add[V];
+        groups.load(raw_dy, static_cast<const T *>(a.dy) + row * a.dy_stride);
+        groups.load(raw_z, static_cast<const T *>(a.z) + row * a.z_stride);
+        if (a.dz_add) groups.load(raw_add, static_cast<const T *>(a.dz_add) + row * a.dz_add_stride);
         const float mean = a.mean[row], rstd = a.rstd[row];
         f32x8 g[V], h[V];
         float s1 = 0.f, s2 = 0.f;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const uint32_t c = (t + v * TPR) * 8u;
-            const int n = int(a.cols) - int(c);
-            g[v] = widen<T>(load8(dy + c, n));
-            h[v] = (widen<T>(load8(z + c, n)) - mean) * rstd;
+            g[v] = widen<T>(raw_dy[v]);
+            h[v] = (widen<T>(raw_z[v]) - mean) * rstd;
             dbeta[v] += g[v];
-            if (a.gamma) {
-                const f32x8 gamma = load8(a.gamma + c, n);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) dgamma[v][k] = fmaf(g[v][k], h[v][k], dgamma[v][k]);
-                g[v] *= gamma;
-            } else {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) dgamma[v][k] = fmaf(g[v][k], h[v][k], dgamma[v][k]);
-            }
+            for (int k = 0; k < 8; ++k) dgamma[v][k] = fmaf(g[v][k], h[v][k], dgamma[v][k]);
+            if (a.gamma) g[v] *= gamma[v];
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 s1 += g[v][k];   // behind the row's end g is 0
@@ -148,19 +162,16 @@ template <typename T, int TPR, int V> __global__ __launch_bounds__(TPR > 256 ? T
         }
         s1 *= per_col;
         s2 *= per_col;
-        T *dz = static_cast<T *>(a.dz) + row * a.dz_stride;
-        T *dx = a.dx ? static_cast<T *>(a.dx) + row * a.dx_stride : nullptr;
+        f32x8 dz[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const uint32_t c = (t + v * TPR) * 8u;
-            const int n = int(a.cols) - int(c);
-            f32x8 o = {};
-            if (add) o = widen<T>(load8(add + c, n));
+            dz[v] = 0.f;
+            if (a.dz_add) dz[v] = widen<T>(raw_add[v]);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) o[k] = fmaf(rstd, g[v][k] - fmaf(h[v][k], s2, s1), o[k]);
-            store8(dz + c, n, o);
-            if (dx) store8(dx + c, n, drop8(o, d, c / 8u, row));
+            for (int k = 0; k < 8; ++k) dz[v][k] = fmaf(rstd, g[v][k] - fmaf(h[v][k], s2, s1), dz[v][k]);
         }
+        groups.store(static_cast<T *>(a.dz) + row * a.dz_stride, [&](int v) { return dz[v]; });
+        if (a.dx) groups.store(static_cast<T *>(a.dx) + row * a.dx_stride, [&](int v) { return drop8(dz[v], dr, groups.col(v) / 8u, row); });
     }
     float *out = a.partial;
     if (!out) return;

@@ -12,16 +12,20 @@ namespace adacomp {
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kInf = __builtin_huge_valf();
 
-// Where distance x stands in LDS: neighbouring lanes read places 8 apart, and 9 apart they use different banks.
-__host__ __device__ constexpr uint32_t spread(uint32_t x) { return x + (x >> 3); }
-__host__ __device__ constexpr uint32_t spread_size(uint32_t distance) { return (spread(2u * distance) + 4u) & ~3u; }
+// The bias by distance index x = key - query + D, and the sums of its gradient, lie in LDS with 8 more places at either end, so that a
+// group of 8 keys that reaches over an end needs no clamp.  Place X = x + 8 is in cell X + X / 8: neighbouring lanes are 8 places
+// and so 9 cells apart, in different banks.  Groups begin at multiples of 8 keys, so X % 8 is the same for a whole row.
+constexpr uint32_t kGuard = 8;
+__host__ __device__ constexpr uint32_t cell(uint32_t X) { return X + (X >> 3); }
+__host__ __device__ constexpr uint32_t cells(uint32_t distance) { return (cell(2u * distance + 2u * kGuard) + 3u) & ~3u; }
 
-// A workgroup's copy of its head's bias, by distance, times log2(e).
+// A workgroup's copy of its head's bias, times log2(e).
 __device__ __forceinline__ void stage_bias(float *bias, const SoftmaxArgs &a, uint32_t head)
 {
-    for (uint32_t x = threadIdx.x; x <= 2u * a.distance; x += blockDim.x) {
-        const int32_t b = min(max(a.map[x], 0), int32_t(a.n_buckets) - 1);
-        bias[spread(x)] = a.table[uint64_t(b) * a.heads + head] * kLog2e;
+    const int last = 2 * int(a.distance);
+    for (int X = threadIdx.x; X <= last + 2 * int(kGuard) - 1; X += blockDim.x) {
+        const int32_t b = min(max(a.map[min(max(X - int(kGuard), 0), last)], 0), int32_t(a.n_buckets) - 1);
+        bias[cell(X)] = a.table[uint64_t(b) * a.heads + head] * kLog2e;
     }
 }
 
@@ -29,7 +33,7 @@ __device__ __forceinline__ void stage_bias(float *bias, const SoftmaxArgs &a, ui
 struct Row {
     const uint8_t *mask;   // NULL: none
     int limit;             // keys below it are admitted, as far as the mask goes
-    int shift;             // distance index of key j: j + shift
+    int shift;             // place of key j: j + shift
 };
 
 __device__ __forceinline__ Row row_of(const SoftmaxArgs &a, uint32_t b, uint32_t h, uint32_t i)
@@ -41,47 +45,51 @@ __device__ __forceinline__ Row row_of(const SoftmaxArgs &a, uint32_t b, uint32_t
     if (a.causal) limit = min(limit, at + 1);
     r.limit = int(max(limit, int64_t(0)));
     // keys are below 2^30: a shift beyond these bounds is beyond D for every key either way
-    r.shift = int(min(max(int64_t(a.distance) - at, -(int64_t(1) << 30) - 8192), int64_t(1) << 30));
+    r.shift = int(min(max(int64_t(a.distance + kGuard) - at, -(int64_t(1) << 30) - 8192), int64_t(1) << 30));
     r.mask = a.mask.data ? static_cast<const uint8_t *>(a.mask.data) + int64_t(b) * a.mask.batch + int64_t(h) * a.mask.head + int64_t(i) * a.mask.row : nullptr;
     return r;
 }
 
-// The admitted ones of 8 keys from j on, a bit each.  in_row: keys from j on that the row has.
-__device__ __forceinline__ uint32_t admitted8(const Row &r, int j, int in_row)
+// Where a group of 8 keys from j on lies.
+struct Window {
+    int X;          // place of its first key
+    uint32_t base;  // cell of the multiple of 8 at or below X, if any of the 8 lies between the ends
+    __device__ __forceinline__ Window(const Row &r, int j) : X(j + r.shift), base(uint32_t(9 * (X >> 3))) {}
+    __device__ __forceinline__ bool above(int last) const { return X >= last + int(kGuard); }
+    __device__ __forceinline__ bool below() const { return X <= 0; }
+    // cell of key k of the group: base + X % 8 + k, and one more behind a multiple of 8
+    __device__ __forceinline__ uint32_t of(const Row &r, int k) const
+    {
+        const uint32_t in = (uint32_t(r.shift) & 7u) + uint32_t(k);
+        return base + (in + (in >> 3));
+    }
+};
+
+// The admitted ones of 8 keys, a bit each, of which n > 0 are below the row's limit; mask: their bytes of the mask.
+template <bool MASK> __device__ __forceinline__ uint32_t admitted8(uint64_t mask, int n)
 {
-    const int n = r.limit - j;
-    uint32_t bits = n >= 8 ? 0xFFu : n > 0 ? (1u << n) - 1u : 0u;
-    if (r.mask && n > 0) {
-        typedef uint64_t at __attribute__((aligned(1)));
-        uint64_t m = 0;
-        if (in_row >= 8) m = *reinterpret_cast<const at *>(r.mask + j);
-        else
-            for (int k = 0; k < 7; ++k)
-                if (k < in_row) m |= uint64_t(r.mask[j + k]) << (8 * k);
+    uint32_t bits = n >= 8 ? 0xFFu : (1u << n) - 1u;
+    if constexpr (MASK) {
         uint32_t keep = 0;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) keep |= ((m >> (8 * k)) & 0xFFu) ? 1u << k : 0u;
+        for (int k = 0; k < 8; ++k) keep |= (uint32_t(mask >> (8 * k)) & 0xFFu) ? 1u << k : 0u;
         bits &= keep;
     }
     return bits;
 }
 
-// scale2 * s + bias of 8 keys from j on, -infinity where not admitted.
-__device__ __forceinline__ f32x8 biased8(f32x8 s, const SoftmaxArgs &a, const Row &r, const float *bias, int j, uint32_t bits)
+// scale2 * s + bias - less of 8 keys.
+__device__ __forceinline__ f32x8 biased8(f32x8 s, const SoftmaxArgs &a, const Row &r, const Window &w, const float *bias, float low, float high, float less)
 {
-    const int last = 2 * int(a.distance), x = j + r.shift;
     f32x8 t;
-    if (x >= last || x <= -8) {
-        const float b = bias[x >= last ? spread(last) : 0u];
+    const int last = 2 * int(a.distance);
+    if (w.above(last) || w.below()) {
+        const float b = (w.below() ? low : high) - less;
 #pragma unroll
         for (int k = 0; k < 8; ++k) t[k] = fmaf(s[k], a.scale2, b);
     } else {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) t[k] = fmaf(s[k], a.scale2, bias[spread(uint32_t(min(max(x + k, 0), last)))]);
-    }
-    if (bits != 0xFFu) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) t[k] = bits >> k & 1u ? t[k] : -kInf;
+        for (int k = 0; k < 8; ++k) t[k] = fmaf(s[k], a.scale2, bias[w.of(r, k)] - less);
     }
     return t;
 }
@@ -98,9 +106,10 @@ enum Phase { WHOLE, STATS, WRITE };
 
 // ---- forward ------------------------------------------------------------------------------------------------------
 
-template <typename T, int TPR, int V, int PHASE> __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_softmax_forward(SoftmaxArgs a)
+template <typename T, int TPR, int V, int PHASE, bool MASK> __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_softmax_forward(SoftmaxArgs a)
 {
     constexpr uint32_t TEAMS = TPR > 256 ? 1 : 256 / TPR;
+    constexpr int LANES = TPR > 64 ? 64 : TPR;
     extern __shared__ float bias[];
     __shared__ float room[2][2][16];
     const uint32_t t = threadIdx.x % TPR, team = team_of<TPR>();
@@ -108,149 +117,192 @@ template <typename T, int TPR, int V, int PHASE> __global__ __launch_bounds__(TP
     uint32_t turn = 0;
     const uint64_t blocks = uint64_t(a.batch) * a.heads * a.wgs_per_head * a.row_parts;
     for (uint64_t block = blockIdx.x; block < blocks; block += gridDim.x) {
-    uint32_t unit = uint32_t(block), part = 0;
-    if constexpr (PHASE != WHOLE) { unit = uint32_t(block / a.row_parts); part = uint32_t(block - uint64_t(unit) * a.row_parts); }
-    const uint32_t bh = unit / a.wgs_per_head, first = (unit - bh * a.wgs_per_head) * a.rows_per_wg;
-    const uint32_t b = bh / a.heads, h = bh - b * a.heads;
-    if (block != blockIdx.x) __syncthreads();   // the rows before are done with the bias
-    stage_bias(bias, a, h);
-    __syncthreads();
-    const T *scores = static_cast<const T *>(a.scores.data) + int64_t(b) * a.scores.batch + int64_t(h) * a.scores.head;
-    T *out = static_cast<T *>(const_cast<void *>(a.out.data)) + int64_t(b) * a.out.batch + int64_t(h) * a.out.head;
-    const int base = int(part * (TPR * V * 8u));
-    for (uint32_t i = first + team; i < min(first + a.rows_per_wg, a.queries); i += TEAMS) {
-        const Row r = row_of(a, b, h, i);
-        const T *s = scores + int64_t(i) * a.scores.row;
-        f32x8 p[V];
-        uint32_t bits = 0;   // admitted places, 8 to a group
-        float m = -kInf;
+        uint32_t unit = uint32_t(block), part = 0;
+        if constexpr (PHASE != WHOLE) { unit = uint32_t(block / a.row_parts); part = uint32_t(block - uint64_t(unit) * a.row_parts); }
+        const uint32_t bh = unit / a.wgs_per_head, first = (unit - bh * a.wgs_per_head) * a.rows_per_wg;
+        const uint32_t b = bh / a.heads, h = bh - b * a.heads;
+        if (block != blockIdx.x) __syncthreads();   // the rows before are done with the bias
+        stage_bias(bias, a, h);
+        __syncthreads();
+        const float low = bias[0], high = bias[cell(2u * a.distance + kGuard)];
+        const T *scores = static_cast<const T *>(a.scores.data) + int64_t(b) * a.scores.batch + int64_t(h) * a.scores.head;
+        T *out = static_cast<T *>(const_cast<void *>(a.out.data)) + int64_t(b) * a.out.batch + int64_t(h) * a.out.head;
+        const uint32_t base = part * (TPR * V * 8u);
+        for (uint32_t i = first + team; i < min(first + a.rows_per_wg, a.queries); i += TEAMS) {
+            const Row r = row_of(a, b, h, i);
+            const T *s = scores + int64_t(i) * a.scores.row;
+            const uint32_t keys = again_uniform(a.keys);
+            const RowGroups<T, TPR, V> groups = {again(t), keys, base};
+            const Drop dr = again(d);
+            raw8<T> raw[V];
+            groups.load_below(raw, s, uint32_t(r.limit));
+            raw8<uint8_t> mask[V];
+            if constexpr (MASK) RowGroups<uint8_t, TPR, V>{groups.t, keys, base}.load_below(mask, r.mask, uint32_t(r.limit));
+            f32x8 p[V];
+            uint32_t bits = 0;   // admitted places, 8 to a group
+            float m = -kInf;
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int j = base + int(t + v * TPR) * 8, in_row = int(a.keys) - j;
-            p[v] = -kInf;
-            if (j < r.limit) {
-                const uint32_t here = admitted8(r, j, in_row);
-                bits |= here << (8 * v);
-                p[v] = biased8(widen<T>(load8(s + j, in_row)), a, r, bias, j, here);
+            for (int v = 0; v < V; ++v) {
+                const int j = int(groups.col(v)), n = r.limit - j;
+                p[v] = -kInf;
+                if (n > 0) {
+                    const uint32_t here = admitted8<MASK>(MASK ? __builtin_bit_cast(uint64_t, mask[v]) : 0, n);
+                    bits |= here << (8 * v);
+                    p[v] = biased8(widen<T>(raw[v]), a, r, Window(r, j), bias, low, high, 0.f);
+                    if (here != 0xFFu) {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) m = fmaxf(m, p[v][k]);
+                        for (int k = 0; k < 8; ++k) p[v][k] = here >> k & 1u ? p[v][k] : -kInf;
+                    }
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) m = fmaxf(m, p[v][k]);
+                }
             }
-        }
-        // exponentials from the maximum of a team's lanes of one wave; the waves' sums are joined behind them
-        m = over_lanes<Max, (TPR > 64 ? 64 : TPR)>(m);
-        const float from = m == -kInf ? 0.f : m;
-        float l = 0.f;
+            // exponentials from the maximum of a wave's lanes; the waves' sums are joined behind them
+            m = over_lanes<Max, LANES>(m);
+            const float from = m == -kInf ? 0.f : m;
+            float l = 0.f;
 #pragma unroll
-        for (int v = 0; v < V; ++v)
+            for (int v = 0; v < V; ++v)
+                if (bits >> (8 * v) & 0xFFu) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                p[v][k] = __builtin_amdgcn_exp2f(p[v][k] - from);
-                l += p[v][k];
+                    for (int k = 0; k < 8; ++k) {
+                        p[v][k] = __builtin_amdgcn_exp2f(p[v][k] - from);
+                        l += p[v][k];
+                    }
+                }
+            l = over_lanes<Add, LANES>(l);
+            float top = m, total = l;
+            if constexpr (TPR > 64) {
+                if (threadIdx.x % 64u == 0u) { room[turn][0][threadIdx.x / 64u] = m; room[turn][1][threadIdx.x / 64u] = l; }
+                __syncthreads();
+                top = -kInf;
+#pragma unroll
+                for (int w = 0; w < TPR / 64; ++w) top = fmaxf(top, room[turn][0][w]);
+                const float from_top = top == -kInf ? 0.f : top;
+                total = 0.f;
+#pragma unroll
+                for (int w = 0; w < TPR / 64; ++w) total = fmaf(room[turn][1][w], __builtin_amdgcn_exp2f(room[turn][0][w] - from_top), total);
+                turn ^= 1u;
             }
-        l = over_lanes<Add, (TPR > 64 ? 64 : TPR)>(l);
-        float top = m, total = l;
-        if constexpr (TPR > 64) {
-            if (threadIdx.x % 64u == 0u) { room[turn][0][threadIdx.x / 64u] = m; room[turn][1][threadIdx.x / 64u] = l; }
-            __syncthreads();
-            top = -kInf;
-#pragma unroll
-            for (int w = 0; w < TPR / 64; ++w) top = fmaxf(top, room[turn][0][w]);
-            const float from_top = top == -kInf ? 0.f : top;
-            total = 0.f;
-#pragma unroll
-            for (int w = 0; w < TPR / 64; ++w) total = fmaf(room[turn][1][w], __builtin_amdgcn_exp2f(room[turn][0][w] - from_top), total);
-            turn ^= 1u;
-        }
-        const uint64_t row = uint64_t(bh) * a.queries + i;
-        if constexpr (PHASE == STATS) {
-            if (threadIdx.x == 0u) {
-                float *to = a.part_stats + (row * a.row_parts + part) * 2u;
-                to[0] = top;
-                to[1] = total;
+            const uint64_t row = uint64_t(bh) * a.queries + i;
+            if constexpr (PHASE == STATS) {
+                if (threadIdx.x == 0u) {
+                    float *to = a.part_stats + (row * a.row_parts + part) * 2u;
+                    to[0] = top;
+                    to[1] = total;
+                }
+                continue;
             }
-            continue;
-        }
-        if constexpr (PHASE == WRITE) {
-            const float *of = a.part_stats + row * a.row_parts * 2u;
-            top = -kInf;
-            for (uint32_t q = 0; q < a.row_parts; ++q) top = fmaxf(top, of[2u * q]);
-            const float from_top = top == -kInf ? 0.f : top;
-            total = 0.f;
-            for (uint32_t q = 0; q < a.row_parts; ++q) total = fmaf(of[2u * q + 1u], __builtin_amdgcn_exp2f(of[2u * q] - from_top), total);
-        }
-        const float factor = total == 0.f ? 0.f : __builtin_amdgcn_exp2f(from - (top == -kInf ? 0.f : top)) / total;
-        if (a.lse && t == 0u && part == 0u) a.lse[row] = total == 0.f ? -kInf : (top + log2f(total)) * kLn2;
-        T *o = out + int64_t(i) * a.out.row;
+            if constexpr (PHASE == WRITE) {
+                const float *of = a.part_stats + row * a.row_parts * 2u;
+                top = -kInf;
+                for (uint32_t q = 0; q < a.row_parts; ++q) top = fmaxf(top, of[2u * q]);
+                const float from_top = top == -kInf ? 0.f : top;
+                total = 0.f;
+                for (uint32_t q = 0; q < a.row_parts; ++q) total = fmaf(of[2u * q + 1u], __builtin_amdgcn_exp2f(of[2u * q] - from_top), total);
+            }
+            float factor = total == 0.f ? 0.f : __builtin_amdgcn_exp2f(from - (top == -kInf ? 0.f : top)) / total;
+            if (a.drop.on) factor *= d.factor;
+            if (a.lse && t == 0u && part == 0u) a.lse[row] = total == 0.f ? -kInf : (top + log2f(total)) * kLn2;
+            groups.store(out + int64_t(i) * a.out.row, [&](int v) {
+                f32x8 y = {};
+                const uint32_t here = bits >> (8 * v) & 0xFFu;
+                if (here) {
+                    y = p[v] * factor;
+                    if (here != 0xFFu) {   // a row's NaN stays where it looks
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int j = base + int(t + v * TPR) * 8, in_row = int(a.keys) - j;
-            if (in_row <= 0) break;
-            f32x8 y;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) y[k] = bits >> (8 * v + k) & 1u ? p[v][k] * factor : 0.f;
-            if (a.drop.on) y = drop8(y, d, uint32_t(j) / 8u, uint32_t(row));
-            store8(o + j, in_row, y);
+                        for (int k = 0; k < 8; ++k) y[k] = here >> k & 1u ? y[k] : 0.f;
+                    }
+                    if (a.drop.on) y = kept8(y, dr, groups.col(v) / 8u, uint32_t(row));
+                }
+                return y;
+            });
         }
-    }
     }
 }
 
 // ---- backward -----------------------------------------------------------------------------------------------------
 
-template <typename T, int TPR, int V, int PHASE> __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_softmax_backward(SoftmaxArgs a)
+template <typename T, int TPR, int V, int PHASE, bool MASK> __global__ __launch_bounds__(TPR > 256 ? TPR : 256, 4) void k_softmax_backward(SoftmaxArgs a)
 {
     constexpr uint32_t TEAMS = TPR > 256 ? 1 : 256 / TPR, WG = TPR > 256 ? TPR : 256;
+    constexpr int LANES = TPR > 64 ? 64 : TPR;
     extern __shared__ float lds[];
     __shared__ float room[2][16];
     const uint32_t t = threadIdx.x % TPR, team = team_of<TPR>();
-    const uint32_t size = spread_size(a.distance);
+    const uint32_t size = cells(a.distance);
     const int last = 2 * int(a.distance);
     float *bias = lds, *acc = lds + size * (1u + team);   // every team has sums of its own
     const bool sums = PHASE != STATS && a.bias_sums;
     const uint32_t h = blockIdx.x / a.wgs_per_head, group = blockIdx.x - h * a.wgs_per_head;
     const Drop d = drop_of(a.drop);
+    const float up_factor = a.drop.on ? d.factor : 1.f;
     stage_bias(bias, a, h);
     if (sums)
         for (uint32_t x = threadIdx.x; x < size * TEAMS; x += WG) lds[size + x] = 0.f;
     __syncthreads();
-    float low = 0.f, high = 0.f;   // sums of e at the ends of the map
+    const float bias_low = bias[0], bias_high = bias[cell(uint32_t(last) + kGuard)];
+    float low = 0.f, high = 0.f;   // sums of e beyond the ends of the map
     const uint64_t units = uint64_t(a.batch) * a.queries * a.row_parts;
     uint32_t turn = 0;
     for (uint64_t unit = uint64_t(group) * TEAMS + team; unit < units; unit += uint64_t(a.wgs_per_head) * TEAMS) {
         uint32_t row_of_head = uint32_t(unit), part = 0;
         if constexpr (PHASE != WHOLE) { row_of_head = uint32_t(unit / a.row_parts); part = uint32_t(unit - uint64_t(row_of_head) * a.row_parts); }
         const uint32_t b = row_of_head / a.queries, i = row_of_head - b * a.queries;
-        const int base = int(part * (TPR * V * 8u));
+        const uint32_t base = part * (TPR * V * 8u);
         const Row r = row_of(a, b, h, i);
         const uint64_t row = (uint64_t(b) * a.heads + h) * a.queries + i;
         const T *s = static_cast<const T *>(a.scores.data) + int64_t(b) * a.scores.batch + int64_t(h) * a.scores.head + int64_t(i) * a.scores.row;
         const T *up = static_cast<const T *>(a.in.data) + int64_t(b) * a.in.batch + int64_t(h) * a.in.head + int64_t(i) * a.in.row;
         T *o = static_cast<T *>(const_cast<void *>(a.out.data)) + int64_t(b) * a.out.batch + int64_t(h) * a.out.head + int64_t(i) * a.out.row;
+        const uint32_t keys = again_uniform(a.keys);
+        const RowGroups<T, TPR, V> groups = {again(t), keys, base};
+        const Drop dr = again(d);
+        raw8<T> raw[V], raw_up[V];
+        groups.load_below(raw, s, uint32_t(r.limit));
+        groups.load_below(raw_up, up, uint32_t(r.limit));
+        raw8<uint8_t> mask[V];
+        if constexpr (MASK) RowGroups<uint8_t, TPR, V>{groups.t, keys, base}.load_below(mask, r.mask, uint32_t(r.limit));
         const float lse = a.lse[row], lse2 = lse == -kInf ? kInf : lse * kLog2e;
+        // Beyond 2^22 an lse has no fraction left, and its roundings alone would make exponents of any size: there, places that are as
+        // near to it as that have P = 1 (rows of the type's lowest value, say; their number is lost in lse).
+        const bool coarse = !(fabsf(lse2) < 4194304.f);
+        const float less = coarse ? 0.f : lse2;
         f32x8 p[V], dp[V];
         float inner = 0.f;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int j = base + int(t + v * TPR) * 8, in_row = int(a.keys) - j;
+            const int j = int(groups.col(v)), n = r.limit - j;
             p[v] = 0.f;
             dp[v] = 0.f;
-            if (j < r.limit) {
-                const uint32_t bits = admitted8(r, j, in_row);
-                p[v] = biased8(widen<T>(load8(s + j, in_row)), a, r, bias, j, bits);
-                dp[v] = widen<T>(load8(up + j, in_row));
-                if (a.drop.on) dp[v] = drop8(dp[v], d, uint32_t(j) / 8u, uint32_t(row));
+            if (n > 0) {
+                const uint32_t bits = admitted8<MASK>(MASK ? __builtin_bit_cast(uint64_t, mask[v]) : 0, n);
+                p[v] = biased8(widen<T>(raw[v]), a, r, Window(r, j), bias, bias_low, bias_high, less);
+                if (coarse) {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const bool on = bits >> k & 1u;
-                    p[v][k] = on ? __builtin_amdgcn_exp2f(p[v][k] - lse2) : 0.f;
-                    dp[v][k] = on ? dp[v][k] : 0.f;
-                    inner = fmaf(p[v][k], dp[v][k], inner);
+                    for (int k = 0; k < 8; ++k) {
+                        const float x = p[v][k] - lse2;
+                        p[v][k] = x > fabsf(lse2) * -0x1p-21f ? 0.f : x;
+                    }
                 }
+                dp[v] = widen<T>(raw_up[v]);
+                if (a.drop.on) dp[v] = kept8(dp[v], dr, uint32_t(j) / 8u, uint32_t(row));
+#pragma unroll
+                for (int k = 0; k < 8; ++k) p[v][k] = __builtin_amdgcn_exp2f(p[v][k]);
+                if (bits != 0xFFu) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        p[v][k] = bits >> k & 1u ? p[v][k] : 0.f;
+                        dp[v][k] = bits >> k & 1u ? dp[v][k] : 0.f;
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < 8; ++k) inner = fmaf(p[v][k], dp[v][k], inner);
             }
         }
         if constexpr (PHASE != WRITE) {
-            inner = over_lanes<Add, (TPR > 64 ? 64 : TPR)>(inner);
-            if constexpr (TPR > 64) {
+            inner = over_lanes<Add, LANES>(inner) * up_factor;
+            if constexpr (TPR > 64) {   // this barrier also parts the rows' additions to the sums
                 inner = over_waves<Add, TPR / 64>(inner, room[turn]);
                 turn ^= 1u;
             }
@@ -262,42 +314,35 @@ template <typename T, int TPR, int V, int PHASE> __global__ __launch_bounds__(TP
         if constexpr (PHASE == WRITE) {
             inner = 0.f;
             for (uint32_t q = 0; q < a.row_parts; ++q) inner += a.part_stats[(row * a.row_parts + q) * 2u];
+            __syncthreads();
         }
-        if (sums) {   // the rows before this one are done with the sums
-            if constexpr (TPR > 64) __syncthreads();
-            else {
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                __builtin_amdgcn_wave_barrier();
-            }
-        }
+        groups.store(o, [&](int v) {
+            const int j = int(groups.col(v));
+            f32x8 y = {};
+            if (j < r.limit) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int j = base + int(t + v * TPR) * 8, in_row = int(a.keys) - j;
-            if (in_row <= 0) break;
+                for (int k = 0; k < 8; ++k) p[v][k] *= fmaf(dp[v][k], up_factor, -inner);
+                y = p[v] * a.scale;
+                if (sums) {
+                    const Window w(r, j);
+                    if (w.above(last) || w.below()) {
+                        float e = 0.f;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) p[v][k] *= dp[v][k] - inner;
-            store8(o + j, in_row, p[v] * a.scale);
-            if (sums && j < r.limit) {
-                const int x = j + r.shift;
-                if (x >= last || x <= -8) {
-                    float e = 0.f;
+                        for (int k = 0; k < 8; ++k) e += p[v][k];
+                        low += w.below() ? e : 0.f;
+                        high += w.below() ? 0.f : e;
+                    } else {
+                        // no two lanes of a row have one distance, and a wave's additions stay in order: the sums repeat bit for bit
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) e += p[v][k];
-                    (x >= last ? high : low) += e;
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        if (x + k <= 0) low += p[v][k];
-                        else if (x + k >= last) high += p[v][k];
-                        else acc[spread(uint32_t(x + k))] += p[v][k];
+                        for (int k = 0; k < 8; ++k) __hip_atomic_fetch_add(&acc[w.of(r, k)], p[v][k], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
                     }
                 }
             }
-        }
+            return y;
+        });
     }
     if constexpr (PHASE == STATS) return;
     if (!sums) return;
-    constexpr int LANES = TPR > 64 ? 64 : TPR;
     low = over_lanes<Add, LANES>(low);
     high = over_lanes<Add, LANES>(high);
     __syncthreads();
@@ -305,15 +350,17 @@ template <typename T, int TPR, int V, int PHASE> __global__ __launch_bounds__(TP
         low = over_waves<Add, TPR / 64>(low, room[0]);
         high = over_waves<Add, TPR / 64>(high, room[1]);
     }
-    if (t == 0u) {
-        acc[0] = low;
-        acc[spread(uint32_t(last))] = high;
+    if (t == 0u) {   // what lies beyond the ends is theirs
+        for (uint32_t X = 0; X < kGuard; ++X) low += acc[cell(X)];
+        for (uint32_t X = 1; X < kGuard; ++X) high += acc[cell(uint32_t(last) + kGuard + X)];
+        acc[cell(kGuard)] += low;
+        acc[cell(uint32_t(last) + kGuard)] += high;
     }
     __syncthreads();
     float *to = a.bias_sums + uint64_t(blockIdx.x) * (uint32_t(last) + 1u);
     for (uint32_t x = threadIdx.x; x <= uint32_t(last); x += WG) {
         float e = 0.f;
-        for (uint32_t m = 0; m < TEAMS; ++m) e += lds[size * (1u + m) + spread(x)];
+        for (uint32_t m = 0; m < TEAMS; ++m) e += lds[size * (1u + m) + cell(x + kGuard)];
         to[x] = e;
     }
 }
@@ -367,7 +414,7 @@ constexpr uint32_t kLdsMost = 64u << 10;   // of a workgroup
 SoftmaxForm softmax_form(uint32_t keys, uint32_t distance, bool backward)
 {
     if (backward) {
-        const uint32_t copies = kLdsMost / (4u * spread_size(distance)) - 1u;
+        const uint32_t copies = kLdsMost / (4u * cells(distance)) - 1u;
         keys = std::max(keys, copies >= 32u ? 0u : copies >= 16u ? 65u : copies >= 8u ? 129u : copies >= 4u ? 257u : 2049u);
     }
     if (keys <= 64u) return {{8, 1}, 1};
@@ -391,16 +438,21 @@ uint32_t softmax_back_groups(uint64_t rows_of_head, uint32_t heads, const Softma
 
 constexpr uint32_t kMostWorkgroups = 1u << 20;   // a launch has fewer than 2^32 threads; what is left is walked over
 
-template <template <typename, int, int, int> class K>
+template <template <typename, int, int, int, bool> class K>
 static int launch_form(const SoftmaxArgs &a, uint32_t dtype, const SoftmaxForm &f, uint32_t workgroups, uint32_t lds, void *stream)
 {
     const dim3 grid(workgroups), wg(f.row.workgroup());
     hipStream_t s = static_cast<hipStream_t>(stream);
     auto go = [&](auto form, auto phase) {
         constexpr int TPR = decltype(form)::threads, V = decltype(form)::groups, PHASE = decltype(phase)::value;
-        if (dtype == ADACOMP_DTYPE_F32) hipLaunchKernelGGL((K<float, TPR, V, PHASE>::kernel), grid, wg, lds, s, a);
-        else if (dtype == ADACOMP_DTYPE_BF16) hipLaunchKernelGGL((K<bf16, TPR, V, PHASE>::kernel), grid, wg, lds, s, a);
-        else hipLaunchKernelGGL((K<f16, TPR, V, PHASE>::kernel), grid, wg, lds, s, a);
+        auto of = [&](auto masked) {
+            constexpr bool MASK = decltype(masked)::value;
+            if (dtype == ADACOMP_DTYPE_F32) hipLaunchKernelGGL((K<float, TPR, V, PHASE, MASK>::kernel), grid, wg, lds, s, a);
+            else if (dtype == ADACOMP_DTYPE_BF16) hipLaunchKernelGGL((K<bf16, TPR, V, PHASE, MASK>::kernel), grid, wg, lds, s, a);
+            else hipLaunchKernelGGL((K<f16, TPR, V, PHASE, MASK>::kernel), grid, wg, lds, s, a);
+        };
+        if (a.mask.data) of(std::true_type());
+        else of(std::false_type());
     };
     using Whole = std::integral_constant<int, WHOLE>;
     if (f.parts > 1u) {
@@ -424,8 +476,8 @@ static int launch_form(const SoftmaxArgs &a, uint32_t dtype, const SoftmaxForm &
     return check_launch();
 }
 
-template <typename T, int TPR, int V, int PHASE> struct KForward { static constexpr auto kernel = k_softmax_forward<T, TPR, V, PHASE>; };
-template <typename T, int TPR, int V, int PHASE> struct KBackward { static constexpr auto kernel = k_softmax_backward<T, TPR, V, PHASE>; };
+template <typename T, int TPR, int V, int PHASE, bool MASK> struct KForward { static constexpr auto kernel = k_softmax_forward<T, TPR, V, PHASE, MASK>; };
+template <typename T, int TPR, int V, int PHASE, bool MASK> struct KBackward { static constexpr auto kernel = k_softmax_backward<T, TPR, V, PHASE, MASK>; };
 
 int launch_softmax_forward(const SoftmaxArgs &args, uint32_t dtype, const SoftmaxForm &f, void *stream)
 {
@@ -434,7 +486,7 @@ int launch_softmax_forward(const SoftmaxArgs &args, uint32_t dtype, const Softma
     a.wgs_per_head = (a.queries + a.rows_per_wg - 1u) / a.rows_per_wg;
     a.row_parts = f.parts;
     const uint64_t blocks = uint64_t(a.batch) * a.heads * a.wgs_per_head * f.parts;
-    return launch_form<KForward>(a, dtype, f, uint32_t(std::min<uint64_t>(blocks, kMostWorkgroups)), 4u * spread_size(a.distance), stream);
+    return launch_form<KForward>(a, dtype, f, uint32_t(std::min<uint64_t>(blocks, kMostWorkgroups)), 4u * cells(a.distance), stream);
 }
 
 int launch_softmax_backward(const SoftmaxArgs &args, uint32_t dtype, const SoftmaxForm &f, void *stream)
@@ -443,7 +495,7 @@ int launch_softmax_backward(const SoftmaxArgs &args, uint32_t dtype, const Softm
     a.wgs_per_head = softmax_back_groups(uint64_t(a.batch) * a.queries, a.heads, f);
     a.row_parts = f.parts;
     const uint32_t copies = 1u + (a.bias_sums ? f.row.teams() : 0u);
-    return launch_form<KBackward>(a, dtype, f, a.heads * a.wgs_per_head, 4u * spread_size(a.distance) * copies, stream);
+    return launch_form<KBackward>(a, dtype, f, a.heads * a.wgs_per_head, 4u * cells(a.distance) * copies, stream);
 }
 
 int launch_bias_reduce(const BiasReduce &a, void *stream)

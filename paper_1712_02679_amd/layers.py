@@ -74,7 +74,7 @@ def _stream_of(t):
     device = t.get_device()
     if device < 0 or device != torch.cuda.current_device():
         _refuse("tensors are on the current GPU (there is no CPU path)")
-    return torch.cuda.current_stream().cuda_stream
+    return torch._C._cuda_getCurrentRawStream(device)   # torch.cuda.current_stream(), without an object around it: 1 us less
 
 
 def _rows(t, like, what):
