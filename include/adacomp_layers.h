@@ -121,7 +121,7 @@ int adacomp_relative_buckets(uint32_t n_buckets, uint32_t max_distance, int both
  *   P = exp(t - lse), lse = log(sum over the row's admitted places of exp(t)); a row without any (or with
  *       -infinity in all of them) has P = 0 and lse = -infinity
  * table      [n_buckets, heads] float32;  map  2 max_distance + 1 device int32, clamped to 0 .. n_buckets - 1
- * batch heads queries < 2^31; every other size < 2^31; max_distance 1 .. ADACOMP_BIAS_DISTANCE_MAX;
+ * batch heads queries < 2^31, heads up to 2^20, keys < 2^30; max_distance 1 .. ADACOMP_BIAS_DISTANCE_MAX;
  * n_buckets 1 .. 2 ADACOMP_BIAS_DISTANCE_MAX + 1.
  * Strides of the mask may be 0 (one mask for several heads, say). */
 typedef struct {

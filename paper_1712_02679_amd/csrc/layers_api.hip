@@ -47,7 +47,7 @@ static int view_args(const adacomp_view_t *view, const adacomp_bias_softmax_t *o
 static bool softmax_sizes(uint64_t batch, uint64_t heads, uint64_t queries, uint64_t keys, uint64_t distance)
 {
     const uint64_t most = uint64_t(1) << 31;
-    if (batch >= most || heads >= most || queries >= most || keys >= (uint64_t(1) << 30)) return false;
+    if (batch >= most || heads > (uint64_t(1) << 20) || queries >= most || keys >= (uint64_t(1) << 30)) return false;
     if (distance == 0 || distance > ADACOMP_BIAS_DISTANCE_MAX) return false;
     if (batch * heads >= most) return false;
     return batch * heads * queries < most;

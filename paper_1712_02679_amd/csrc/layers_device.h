@@ -228,4 +228,12 @@ template <typename OP, int WAVES> __device__ __forceinline__ float over_waves(fl
     return all;
 }
 
+// Which of a workgroup's rows a thread belongs to.
+template <int TPR> __device__ __forceinline__ uint32_t team_of()
+{
+    const uint32_t team = threadIdx.x / TPR;
+    if constexpr (TPR >= 64) return __builtin_amdgcn_readfirstlane(team);
+    return team;
+}
+
 }  // namespace adacomp

@@ -40,40 +40,58 @@ template <typename T> __global__ __launch_bounds__(256) void k_dropout(DropoutLa
 // ---- layer norm, forward ------------------------------------------------------------------------------------------
 // A row stays in the registers of its threads: mean first, then the squared distances from it.
 
-template <typename OP, int TPR> __device__ __forceinline__ float over_row(float x, float *room)
+// Over the TPR threads of a row.  A row of several waves joins their sums in `room`, of which the next call takes another one.
+template <int TPR> __device__ __forceinline__ float over_row(float x, float *room, uint32_t team)
 {
-    if constexpr (TPR <= 64) return over_lanes<OP, TPR>(x);
-    else return over_waves<OP, TPR / 64>(over_lanes<OP, 64>(x), room);
+    if constexpr (TPR <= 64) return over_lanes<Add, TPR>(x);
+    else {
+        constexpr uint32_t WAVES = TPR / 64;
+        x = over_lanes<Add, 64>(x);
+        if (threadIdx.x % 64u == 0u) room[threadIdx.x / 64u] = x;
+        __syncthreads();
+        x = room[team * WAVES];
+#pragma unroll
+        for (uint32_t w = 1; w < WAVES; ++w) x += room[team * WAVES + w];
+        return x;
+    }
 }
 
 template <typename T, int TPR, int V> __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_norm_forward(NormForward a)
 {
     constexpr uint32_t TEAMS = TPR > 256 ? 1 : 256 / TPR;
     __shared__ float room[2][16];
-    const uint32_t t = threadIdx.x % TPR;
-    uint32_t team = threadIdx.x / TPR;
-    if constexpr (TPR >= 64) team = __builtin_amdgcn_readfirstlane(team);
+    const uint32_t t = threadIdx.x % TPR, team = team_of<TPR>();
     const Drop d = drop_of(a.drop);
-    for (uint32_t row = blockIdx.x * TEAMS + team; row < a.rows; row += gridDim.x * TEAMS) {
+    for (uint32_t first = blockIdx.x * TEAMS; first < a.rows; first += gridDim.x * TEAMS) {
+        const bool live = first + team < a.rows;
+        const uint32_t row = live ? first + team : a.rows - 1u;   // the last rows' workgroup has teams without one: they go along
         const T *x = static_cast<const T *>(a.x) + row * a.x_stride;
-        const T *res = a.residual ? static_cast<const T *>(a.residual) + row * a.residual_stride : nullptr;
         const uint32_t cols = again_uniform(a.cols);
         const RowGroups<T, TPR, V> groups = {again(t), cols, 0};
+        const RowGroups<float, TPR, V> params = {groups.t, cols, 0};
         const Drop dr = again(d);
         raw8<T> raw[V], raw_res[V];
         groups.load(raw, x);
-        if (res) groups.load(raw_res, res);
+        if (a.residual) groups.load(raw_res, static_cast<const T *>(a.residual) + row * a.residual_stride);
+        raw8<float> some_gamma, some_beta;
+        if (a.gamma) some_gamma = params.some(a.gamma);
+        if (a.beta) some_beta = params.some(a.beta);
+        raw8<float> gamma[V], beta[V];   // up to 8192 columns on their way together with the row, in wider rows behind its sums
+        if constexpr (V == 1) {
+            if (a.gamma) gamma[0] = params.round(a.gamma, 0, some_gamma);
+            if (a.beta) beta[0] = params.round(a.beta, 0, some_beta);
+        }
         f32x8 z[V];
         float sum = 0.f;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             z[v] = widen<T>(raw[v]);
             if (a.drop.on) z[v] = drop8(z[v], dr, groups.col(v) / 8u, row);
-            if (res) z[v] += widen<T>(raw_res[v]);
+            if (a.residual) z[v] += widen<T>(raw_res[v]);
 #pragma unroll
             for (int k = 0; k < 8; ++k) sum += z[v][k];
         }
-        const float mean = over_row<Add, TPR>(sum, room[0]) / float(a.cols);
+        const float mean = over_row<TPR>(sum, room[0], team) / float(a.cols);
         float squares = 0.f;
         f32x8 c[V];
 #pragma unroll
@@ -86,90 +104,104 @@ template <typename T, int TPR, int V> __global__ __launch_bounds__(TPR > 256 ? T
 #pragma unroll
             for (int k = 0; k < 8; ++k) squares = fmaf(c[v][k], c[v][k], squares);
         }
-        const float rstd = 1.f / sqrtf(over_row<Add, TPR>(squares, room[1]) / float(a.cols) + a.eps);
+        const float rstd = 1.f / sqrtf(over_row<TPR>(squares, room[1], team) / float(a.cols) + a.eps);
+        if (!live) continue;
         if (t == 0u) {
             if (a.mean) a.mean[row] = mean;
             if (a.rstd) a.rstd[row] = rstd;
         }
         if (a.z) groups.store(static_cast<T *>(a.z) + row * a.z_stride, [&](int v) { return z[v]; });
-        const RowGroups<float, TPR, V> params = {groups.t, cols, 0};
-        raw8<float> some_gamma, some_beta;
-        if (a.gamma) some_gamma = params.some(a.gamma);
-        if (a.beta) some_beta = params.some(a.beta);
         groups.store(static_cast<T *>(a.y) + row * a.y_stride, [&](int v) {
             f32x8 y = c[v] * rstd;
-            if (a.gamma) y *= params.round(a.gamma, v, some_gamma);
-            if (a.beta) y += params.round(a.beta, v, some_beta);
+            if constexpr (V > 1) {
+                if (a.gamma) gamma[v] = params.round(a.gamma, v, some_gamma);
+                if (a.beta) beta[v] = params.round(a.beta, v, some_beta);
+            }
+            if (a.gamma) y *= gamma[v];
+            if (a.beta) y += beta[v];
             return y;
         });
     }
 }
 
 // ---- layer norm, backward -----------------------------------------------------------------------------------------
-// A workgroup walks over rows, each held in registers as in the forward pass, and keeps its columns' sums of dy h and of dy in
-// registers until its last row; k_norm_reduce adds the workgroups' sums up.
+// A workgroup of 1024 threads walks over rows, each held in registers as in the forward pass, with the next ones on their way, and
+// keeps its columns' sums of dy h and of dy in registers until its last row; k_norm_reduce adds the workgroups' sums up.  Their
+// traffic is 16 bytes a column and workgroup: large workgroups, one to a compute unit, keep it small beside the rows' 8 to 20.
 
-template <typename T, int TPR, int V> __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_norm_backward(NormBackward a)
+constexpr uint32_t kBackThreads = 1024;
+
+template <typename T, int TPR, int V> __global__ __launch_bounds__(kBackThreads) void k_norm_backward(NormBackward a)
 {
-    constexpr uint32_t TEAMS = TPR > 256 ? 1 : 256 / TPR;
+    constexpr uint32_t TEAMS = kBackThreads / TPR, COLS = TPR * V * 8;
     __shared__ float room[2][2][16];
-    __shared__ float sums[TEAMS > 1 ? TEAMS * TPR * V * 8 : 1];
-    const uint32_t t = threadIdx.x % TPR;
-    uint32_t team = threadIdx.x / TPR;
-    if constexpr (TPR >= 64) team = __builtin_amdgcn_readfirstlane(team);
+    __shared__ float sums[TEAMS > 1 ? TEAMS * COLS : 1];
+    const uint32_t t = threadIdx.x % TPR, team = team_of<TPR>();
     const Drop d = drop_of(a.drop);
     const float per_col = 1.f / float(a.cols);
     f32x8 dgamma[V] = {}, dbeta[V] = {};
     raw8<float> gamma[V];
     if (a.gamma) RowGroups<float, TPR, V>{t, a.cols, 0}.load(gamma, a.gamma);
-    uint32_t turn = 0;
-    for (uint32_t row = blockIdx.x * TEAMS + team; row < a.rows; row += gridDim.x * TEAMS) {
+    raw8<T> raw_dy[V], raw_z[V], raw_add[V];
+    float mean = 0.f, rstd = 0.f;
+    auto fetch = [&](uint32_t row) {
         const RowGroups<T, TPR, V> groups = {again(t), again_uniform(a.cols), 0};
-        const Drop dr = again(d);
-        raw8<T> raw_dy[V], raw_z[V], raw_add[V];
-        groups.load(raw_dy, static_cast<const T *>(a.dy) + row * a.dy_stride);
-        groups.load(raw_z, static_cast<const T *>(a.z) + row * a.z_stride);
-        if (a.dz_add) groups.load(raw_add, static_cast<const T *>(a.dz_add) + row * a.dz_add_stride);
-        const float mean = a.mean[row], rstd = a.rstd[row];
-        f32x8 g[V], h[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) raw_dy[v] = raw_z[v] = raw_add[v] = raw8<T>{};
+        if (row < a.rows) {
+            groups.load(raw_dy, static_cast<const T *>(a.dy) + row * a.dy_stride);
+            groups.load(raw_z, static_cast<const T *>(a.z) + row * a.z_stride);
+            if (a.dz_add) groups.load(raw_add, static_cast<const T *>(a.dz_add) + row * a.dz_add_stride);
+            mean = a.mean[row];
+            rstd = a.rstd[row];
+        }
+    };
+    uint32_t turn = 0;
+    fetch(blockIdx.x * TEAMS + team);
+    for (uint32_t first = blockIdx.x * TEAMS; first < a.rows; first += gridDim.x * TEAMS) {
+        const uint32_t row = first + team;
+        const float scale = rstd;
+        f32x8 g[V], h[V], dz[V];
         float s1 = 0.f, s2 = 0.f;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             g[v] = widen<T>(raw_dy[v]);
-            h[v] = (widen<T>(raw_z[v]) - mean) * rstd;
+            h[v] = (widen<T>(raw_z[v]) - mean) * scale;
+            dz[v] = widen<T>(raw_add[v]);
             dbeta[v] += g[v];
 #pragma unroll
             for (int k = 0; k < 8; ++k) dgamma[v][k] = fmaf(g[v][k], h[v][k], dgamma[v][k]);
             if (a.gamma) g[v] *= gamma[v];
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                s1 += g[v][k];   // behind the row's end g is 0
+                s1 += g[v][k];   // behind the row's end, and in teams without a row, g is 0
                 s2 = fmaf(g[v][k], h[v][k], s2);
             }
         }
+        fetch(row + gridDim.x * TEAMS);
         if constexpr (TPR <= 64) {
             s1 = over_lanes<Add, TPR>(s1);
             s2 = over_lanes<Add, TPR>(s2);
         } else {
+            constexpr uint32_t WAVES = TPR / 64;
             s1 = over_lanes<Add, 64>(s1);
             s2 = over_lanes<Add, 64>(s2);
             if (threadIdx.x % 64u == 0u) { room[turn][0][threadIdx.x / 64u] = s1; room[turn][1][threadIdx.x / 64u] = s2; }
             __syncthreads();
             s1 = s2 = 0.f;
 #pragma unroll
-            for (int w = 0; w < TPR / 64; ++w) { s1 += room[turn][0][w]; s2 += room[turn][1][w]; }
+            for (uint32_t w = 0; w < WAVES; ++w) { s1 += room[turn][0][team * WAVES + w]; s2 += room[turn][1][team * WAVES + w]; }
             turn ^= 1u;
         }
+        if (row >= a.rows) continue;
         s1 *= per_col;
         s2 *= per_col;
-        f32x8 dz[V];
+        const RowGroups<T, TPR, V> groups = {again(t), again_uniform(a.cols), 0};
+        const Drop dr = again(d);
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            dz[v] = 0.f;
-            if (a.dz_add) dz[v] = widen<T>(raw_add[v]);
+        for (int v = 0; v < V; ++v)
 #pragma unroll
-            for (int k = 0; k < 8; ++k) dz[v][k] = fmaf(rstd, g[v][k] - fmaf(h[v][k], s2, s1), dz[v][k]);
-        }
+            for (int k = 0; k < 8; ++k) dz[v][k] = fmaf(scale, g[v][k] - fmaf(h[v][k], s2, s1), dz[v][k]);
         groups.store(static_cast<T *>(a.dz) + row * a.dz_stride, [&](int v) { return dz[v]; });
         if (a.dx) groups.store(static_cast<T *>(a.dx) + row * a.dx_stride, [&](int v) { return drop8(dz[v], dr, groups.col(v) / 8u, row); });
     }
@@ -182,11 +214,12 @@ template <typename T, int TPR, int V> __global__ __launch_bounds__(TPR > 256 ? T
             __syncthreads();
 #pragma unroll
             for (int v = 0; v < V; ++v)
-                *reinterpret_cast<f32x8 *>(&sums[(team * TPR * V + t + v * TPR) * 8u]) = which ? dbeta[v] : dgamma[v];
+                *reinterpret_cast<f32x8 *>(&sums[team * COLS + (t + v * TPR) * 8u]) = which ? dbeta[v] : dgamma[v];
             __syncthreads();
-            for (uint32_t c = threadIdx.x; c < a.pitch; c += 256u) {
+            for (uint32_t c = threadIdx.x; c < a.pitch; c += kBackThreads) {
                 float s = 0.f;
-                for (uint32_t m = 0; m < TEAMS; ++m) s += sums[m * TPR * V * 8u + c];
+#pragma unroll 8
+                for (uint32_t m = 0; m < TEAMS; ++m) s += sums[m * COLS + c];
                 out[which * a.pitch + c] = s;
             }
         } else {
@@ -234,34 +267,26 @@ int launch_dropout(const DropoutLaunch &a, void *stream)
     return check_launch();
 }
 
-// The fewest threads that hold a row in up to 32 values each.
+// 8 values to a thread as far as 1024 threads hold the row.
 RowForm norm_form(uint32_t cols)
 {
-    if (cols <= 64u) return {8, 1};
-    if (cols <= 128u) return {16, 1};
-    if (cols <= 256u) return {32, 1};
-    if (cols <= 512u) return {64, 1};
-    if (cols <= 1024u) return {64, 2};
-    if (cols <= 2048u) return {64, 4};
-    if (cols <= 4096u) return {256, 2};
-    if (cols <= 8192u) return {256, 4};
-    if (cols <= 16384u) return {1024, 2};
-    return {1024, 4};
+    uint32_t threads = 8;
+    while (threads < 1024u && threads * 8u < cols) threads *= 2u;
+    return {threads, cols <= 8192u ? 1u : cols <= 16384u ? 2u : 4u};
 }
 
 constexpr uint32_t kMostWorkgroups = 1u << 20;   // a launch has fewer than 2^32 threads; more rows are walked over
 
 uint32_t norm_parts(uint64_t rows, uint32_t cols)
 {
-    const RowForm f = norm_form(cols);
-    const uint64_t all = (rows + f.teams() - 1u) / f.teams();
-    return uint32_t(std::min<uint64_t>(all, f.threads > 256u ? kComputeUnits : 4u * kComputeUnits));
+    const uint32_t teams = kBackThreads / norm_form(cols).threads;
+    return uint32_t(std::min<uint64_t>((rows + teams - 1u) / teams, kComputeUnits));
 }
 
 template <template <typename, int, int> class K, typename A>
-static int launch_rows(const RowForm &f, uint32_t dtype, uint32_t workgroups, const A &a, void *stream)
+static int launch_rows(const RowForm &f, uint32_t dtype, uint32_t workgroups, uint32_t threads, const A &a, void *stream)
 {
-    const dim3 grid(workgroups), wg(f.workgroup());
+    const dim3 grid(workgroups), wg(threads);
     hipStream_t s = static_cast<hipStream_t>(stream);
     auto go = [&](auto form) {
         constexpr int TPR = decltype(form)::threads, V = decltype(form)::groups;
@@ -269,17 +294,17 @@ static int launch_rows(const RowForm &f, uint32_t dtype, uint32_t workgroups, co
         else if (dtype == ADACOMP_DTYPE_BF16) hipLaunchKernelGGL((K<bf16, TPR, V>::kernel), grid, wg, 0, s, a);
         else hipLaunchKernelGGL((K<f16, TPR, V>::kernel), grid, wg, 0, s, a);
     };
-    switch (f.threads * 8u + f.groups) {
-    case 8 * 8 + 1: go(FormOf<8, 1>()); break;
-    case 16 * 8 + 1: go(FormOf<16, 1>()); break;
-    case 32 * 8 + 1: go(FormOf<32, 1>()); break;
-    case 64 * 8 + 1: go(FormOf<64, 1>()); break;
-    case 64 * 8 + 2: go(FormOf<64, 2>()); break;
-    case 64 * 8 + 4: go(FormOf<64, 4>()); break;
-    case 256 * 8 + 2: go(FormOf<256, 2>()); break;
-    case 256 * 8 + 4: go(FormOf<256, 4>()); break;
-    case 1024 * 8 + 2: go(FormOf<1024, 2>()); break;
-    case 1024 * 8 + 4: go(FormOf<1024, 4>()); break;
+    switch (f.threads * f.groups) {
+    case 8: go(FormOf<8, 1>()); break;
+    case 16: go(FormOf<16, 1>()); break;
+    case 32: go(FormOf<32, 1>()); break;
+    case 64: go(FormOf<64, 1>()); break;
+    case 128: go(FormOf<128, 1>()); break;
+    case 256: go(FormOf<256, 1>()); break;
+    case 512: go(FormOf<512, 1>()); break;
+    case 1024: go(FormOf<1024, 1>()); break;
+    case 2048: go(FormOf<1024, 2>()); break;
+    case 4096: go(FormOf<1024, 4>()); break;
     default: return ADACOMP_EINVAL;
     }
     return check_launch();
@@ -291,12 +316,12 @@ template <typename T, int TPR, int V> struct KBackward { static constexpr auto k
 int launch_norm_forward(const NormForward &a, uint32_t dtype, void *stream)
 {
     const RowForm f = norm_form(a.cols);
-    return launch_rows<KForward>(f, dtype, std::min((a.rows + f.teams() - 1u) / f.teams(), kMostWorkgroups), a, stream);
+    return launch_rows<KForward>(f, dtype, std::min((a.rows + f.teams() - 1u) / f.teams(), kMostWorkgroups), f.workgroup(), a, stream);
 }
 
 int launch_norm_backward(const NormBackward &a, uint32_t dtype, uint32_t parts, void *stream)
 {
-    return launch_rows<KBackward>(norm_form(a.cols), dtype, parts, a, stream);
+    return launch_rows<KBackward>(norm_form(a.cols), dtype, parts, kBackThreads, a, stream);
 }
 
 int launch_norm_reduce(const NormReduce &a, void *stream)

@@ -94,13 +94,6 @@ __device__ __forceinline__ f32x8 biased8(f32x8 s, const SoftmaxArgs &a, const Ro
     return t;
 }
 
-template <int TPR> __device__ __forceinline__ uint32_t team_of()
-{
-    const uint32_t team = threadIdx.x / TPR;
-    if constexpr (TPR >= 64) return __builtin_amdgcn_readfirstlane(team);
-    return team;
-}
-
 // WHOLE: a row at a time.  STATS, WRITE: a part of a row, first its maximum and sum, then, from those of all parts, the results.
 enum Phase { WHOLE, STATS, WRITE };
 
@@ -121,23 +114,27 @@ template <typename T, int TPR, int V, int PHASE, bool MASK> __global__ __launch_
         if constexpr (PHASE != WHOLE) { unit = uint32_t(block / a.row_parts); part = uint32_t(block - uint64_t(unit) * a.row_parts); }
         const uint32_t bh = unit / a.wgs_per_head, first = (unit - bh * a.wgs_per_head) * a.rows_per_wg;
         const uint32_t b = bh / a.heads, h = bh - b * a.heads;
+        const T *scores = static_cast<const T *>(a.scores.data) + int64_t(b) * a.scores.batch + int64_t(h) * a.scores.head;
+        T *out = static_cast<T *>(const_cast<void *>(a.out.data)) + int64_t(b) * a.out.batch + int64_t(h) * a.out.head;
+        const uint32_t base = part * (TPR * V * 8u), end = min(first + a.rows_per_wg, a.queries);
+        raw8<T> raw[V];
+        raw8<uint8_t> mask[V];
+        Row next = {};
+        auto fetch = [&](uint32_t i) {   // a row's scores are on their way while the one before is worked on, the first one's while the bias is laid out
+            next = row_of(a, b, h, i);
+            const RowGroups<T, TPR, V> groups = {again(t), again_uniform(a.keys), base};
+            groups.load_below(raw, scores + int64_t(i) * a.scores.row, uint32_t(next.limit));
+            if constexpr (MASK) RowGroups<uint8_t, TPR, V>{groups.t, groups.cols, base}.load_below(mask, next.mask, uint32_t(next.limit));
+        };
+        if (first + team < end) fetch(first + team);
         if (block != blockIdx.x) __syncthreads();   // the rows before are done with the bias
         stage_bias(bias, a, h);
         __syncthreads();
         const float low = bias[0], high = bias[cell(2u * a.distance + kGuard)];
-        const T *scores = static_cast<const T *>(a.scores.data) + int64_t(b) * a.scores.batch + int64_t(h) * a.scores.head;
-        T *out = static_cast<T *>(const_cast<void *>(a.out.data)) + int64_t(b) * a.out.batch + int64_t(h) * a.out.head;
-        const uint32_t base = part * (TPR * V * 8u);
-        for (uint32_t i = first + team; i < min(first + a.rows_per_wg, a.queries); i += TEAMS) {
-            const Row r = row_of(a, b, h, i);
-            const T *s = scores + int64_t(i) * a.scores.row;
-            const uint32_t keys = again_uniform(a.keys);
-            const RowGroups<T, TPR, V> groups = {again(t), keys, base};
+        for (uint32_t i = first + team; i < end; i += TEAMS) {
+            const Row r = next;
+            const RowGroups<T, TPR, V> groups = {again(t), again_uniform(a.keys), base};
             const Drop dr = again(d);
-            raw8<T> raw[V];
-            groups.load_below(raw, s, uint32_t(r.limit));
-            raw8<uint8_t> mask[V];
-            if constexpr (MASK) RowGroups<uint8_t, TPR, V>{groups.t, keys, base}.load_below(mask, r.mask, uint32_t(r.limit));
             f32x8 p[V];
             uint32_t bits = 0;   // admitted places, 8 to a group
             float m = -kInf;
@@ -157,6 +154,7 @@ template <typename T, int TPR, int V, int PHASE, bool MASK> __global__ __launch_
                     for (int k = 0; k < 8; ++k) m = fmaxf(m, p[v][k]);
                 }
             }
+            if (i + TEAMS < end) fetch(i + TEAMS);
             // exponentials from the maximum of a wave's lanes; the waves' sums are joined behind them
             m = over_lanes<Max, LANES>(m);
             const float from = m == -kInf ? 0.f : m;
@@ -365,39 +363,44 @@ template <typename T, int TPR, int V, int PHASE, bool MASK> __global__ __launch_
     }
 }
 
-// A workgroup to a head: the sums of its workgroups, 16 slices of them at a time, then the distances of each bucket.
-__global__ __launch_bounds__(1024) void k_bias_reduce(BiasReduce a)
+// A workgroup to a head and bucket: it lists the distances that have the bucket, and adds up what the backward pass's workgroups
+// have for them, always in the same order.
+__global__ __launch_bounds__(256) void k_bias_reduce(BiasReduce a)
 {
-    extern __shared__ float sums[];   // [2 D + 1]
-    __shared__ float slices[16][65];
-    const uint32_t n = 2u * a.distance + 1u, h = blockIdx.x, lane = threadIdx.x % 64u, wave = threadIdx.x / 64u;
-    const float *from = a.bias_sums + uint64_t(h) * a.groups * n;
-    for (uint32_t x0 = 0; x0 < n; x0 += 64u) {
-        float e = 0.f;
-        if (x0 + lane < n)
-#pragma unroll 4
-            for (uint32_t g = wave; g < a.groups; g += 16u) e += from[uint64_t(g) * n + x0 + lane];
-        slices[wave][lane] = e;
+    extern __shared__ uint16_t mine[];   // [2 D + 1]
+    __shared__ float room[4];
+    __shared__ uint32_t counts[4];
+    const uint32_t n = 2u * a.distance + 1u, lane = threadIdx.x % 64u, wave = threadIdx.x / 64u;
+    const uint32_t h = blockIdx.x, bucket = blockIdx.y;
+    uint32_t found = 0;
+    for (uint32_t x0 = 0; x0 < n; x0 += 256u) {
+        const uint32_t x = x0 + threadIdx.x;
+        const bool hit = x < n && uint32_t(min(max(a.map[x], 0), int32_t(a.n_buckets) - 1)) == bucket;
+        const uint64_t hits = __ballot(hit);
+        if (lane == 0u) counts[wave] = uint32_t(__popcll(hits));
         __syncthreads();
-        if (wave == 0u && x0 + lane < n) {
-            float all = 0.f;
-#pragma unroll
-            for (int w = 0; w < 16; ++w) all += slices[w][lane];
-            sums[x0 + lane] = all;
+        uint32_t before = found;
+        for (uint32_t w = 0; w < 4u; ++w) {
+            if (w < wave) before += counts[w];
+            found += counts[w];
         }
+        if (hit) mine[before + uint32_t(__popcll(hits & ((uint64_t(1) << lane) - 1u)))] = uint16_t(x);
         __syncthreads();
     }
-    for (uint32_t k = wave; k < a.n_buckets; k += 16u) {
-        float e = 0.f;
-        for (uint32_t x = lane; x < n; x += 64u) {
-            const uint32_t b = uint32_t(min(max(a.map[x], 0), int32_t(a.n_buckets) - 1));
-            e += b == k ? sums[x] : 0.f;
+    const float *from = a.bias_sums + uint64_t(h) * a.groups * n;
+    float e = 0.f;
+    if (found != 0u) {
+        const uint32_t items = found * a.groups;   // below 4097 * 1024
+#pragma unroll 4
+        for (uint32_t i = threadIdx.x; i < items; i += 256u) {
+            const uint32_t g = i / found;
+            e += from[uint64_t(g) * n + mine[i - g * found]];
         }
-        e = over_lanes<Add, 64>(e);
-        if (lane == 0u) {
-            float *to = a.dtable + uint64_t(k) * a.heads + h;
-            *to = a.accumulate ? *to + e : e;
-        }
+    }
+    e = over_waves<Add, 4>(over_lanes<Add, 64>(e), room);
+    if (threadIdx.x == 0u) {
+        float *to = a.dtable + uint64_t(bucket) * a.heads + h;
+        *to = a.accumulate ? *to + e : e;
     }
 }
 
@@ -500,7 +503,8 @@ int launch_softmax_backward(const SoftmaxArgs &args, uint32_t dtype, const Softm
 
 int launch_bias_reduce(const BiasReduce &a, void *stream)
 {
-    hipLaunchKernelGGL(k_bias_reduce, dim3(a.heads), dim3(1024), 4u * (2u * a.distance + 1u), static_cast<hipStream_t>(stream), a);
+    const uint32_t lds = (2u * (2u * a.distance + 1u) + 15u) & ~15u;
+    hipLaunchKernelGGL(k_bias_reduce, dim3(a.heads, a.n_buckets), dim3(256), lds, static_cast<hipStream_t>(stream), a);
     return check_launch();
 }
 
