@@ -158,7 +158,7 @@ int adacomp_norm_forward(const adacomp_norm_t *norm, const void *x, const void *
     a.z = z; a.y = y; a.mean = mean; a.rstd = rstd;
     a.x_stride = norm->x_stride; a.residual_stride = norm->residual_stride;
     a.z_stride = norm->z_stride; a.y_stride = norm->y_stride;
-    a.rows = uint32_t(norm->rows); a.cols = norm->cols; a.eps = eps;
+    a.all_rows = norm->rows; a.cols = norm->cols; a.eps = eps;
     return launch_norm_forward(a, norm->dtype, hip_stream);
 }
 

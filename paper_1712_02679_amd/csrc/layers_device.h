@@ -49,75 +49,91 @@ template <typename T> __device__ __forceinline__ void store_some(T *p, uint32_t 
         if (k < n) p[k] = v[k];
 }
 
-// The groups of a row that a thread has: group t + v TPR in round v, `cols` columns in all.  At most one group of a row is
-// incomplete; it is handled apart, once, so that the rounds have one form.
+template <typename T> __device__ __forceinline__ f32x8 widen(raw8<T> v) { return __builtin_convertvector(v, f32x8); }
+
+// x without its first n < 8 values, zeros behind the rest; n is the same for all lanes.
+__device__ __forceinline__ f32x8 shifted(f32x8 x, uint32_t n)
+{
+#pragma unroll
+    for (uint32_t step = 1; step < 8u; step *= 2u)
+        if (n & step) {
+#pragma unroll
+            for (uint32_t k = 0; k < 8u; ++k) x[k] = k + step < 8u ? x[k + step] : 0.f;
+        }
+    return x;
+}
+
+// The groups of a row that a thread has: group t + v TPR in round v, `cols` columns in all.  A row whose length is no multiple of 8 ends
+// with an incomplete group.  Its thread reads the row's last 8 values instead, and moves them into place when it uses them: reading values
+// one by one would make the wave wait for them there and then, and with them for everything that is on its way.
 template <typename T, int TPR, int V> struct RowGroups {
+    static constexpr bool kShort = TPR == 8;   // rows of less than 8 values come to the form with the fewest threads
     uint32_t t, cols, first;   // first: column of the part of the row that the threads hold
     __device__ __forceinline__ uint32_t col(int v) const { return first + (t + uint32_t(v) * TPR) * 8u; }
     __device__ __forceinline__ bool whole(int v) const { return col(v) + 8u <= cols; }
-    // the round in which this thread has the incomplete group; V: it has none
-    __device__ __forceinline__ uint32_t tail() const
+    // groups before the incomplete one, in this part
+    __device__ __forceinline__ uint32_t before_last() const { return cols / 8u - first / 8u; }
+    __device__ __forceinline__ bool ends_in(int v) const { return cols % 8u != 0u && before_last() / TPR == uint32_t(v); }
+    __device__ __forceinline__ bool ends_here() const { return before_last() % TPR == t; }
+    // round v of the row's values, for columns that the row has
+    __device__ __forceinline__ raw8<T> load_round(const T *row, int v) const
     {
-        const uint32_t g = cols / 8u - first / 8u;
-        return cols % 8u != 0u && cols > first && g % TPR == t ? g / TPR : uint32_t(V);
+        raw8<T> raw = {};
+        if constexpr (kShort)
+            if (cols < 8u) {
+                if (col(v) == 0u) raw = load_some(row, cols);
+                return raw;
+            }
+        if (col(v) < cols) raw = load8(at(row, min(col(v), cols - 8u)));
+        return raw;
     }
-    // the row's values, zeros behind its end
     __device__ __forceinline__ void load(raw8<T> (&raw)[V], const T *row) const
     {
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            raw[v] = raw8<T>{};
-            if (whole(v)) raw[v] = load8(at(row, col(v)));
-        }
-        load_tail(raw, row, cols);
+        for (int v = 0; v < V; ++v) raw[v] = load_round(row, v);
     }
-    // values of columns below `upto` and of their groups, anything elsewhere: no branch, what is not wanted is read where the row begins
+    // the same for groups that begin below `upto`, anything elsewhere: no branch, what is not wanted is read where the row begins
     __device__ __forceinline__ void load_below(raw8<T> (&raw)[V], const T *row, uint32_t upto) const
     {
-        if (cols >= 8u) {
+        if constexpr (kShort)
+            if (cols < 8u) {
+                raw[0] = col(0) < upto ? load_some(row, cols) : raw8<T>{};
+                return;
+            }
 #pragma unroll
-            for (int v = 0; v < V; ++v) raw[v] = load8(at(row, whole(v) && col(v) < upto ? col(v) : 0u));
-        } else {
-#pragma unroll
-            for (int v = 0; v < V; ++v) raw[v] = raw8<T>{};
-        }
-        load_tail(raw, row, upto);
+        for (int v = 0; v < V; ++v) raw[v] = load8(at(row, col(v) < upto ? min(col(v), cols - 8u) : 0u));
     }
-    // the rounds one by one: the values of round v, of which `some` are the incomplete group's
-    __device__ __forceinline__ raw8<T> some(const T *row) const
+    // what was loaded for round v, in its place
+    __device__ __forceinline__ f32x8 values(const raw8<T> &raw, int v) const
     {
-        return cols % 8u != 0u && tail() < uint32_t(V) ? load_some(at(row, cols & ~7u), cols % 8u) : raw8<T>{};
-    }
-    __device__ __forceinline__ raw8<T> round(const T *row, int v, const raw8<T> &some) const { return whole(v) ? load8(at(row, col(v))) : some; }
-    __device__ __forceinline__ void load_tail(raw8<T> (&raw)[V], const T *row, uint32_t upto) const
-    {
-        if (cols % 8u == 0u) return;
-        const uint32_t mine = tail();
-        if (mine < uint32_t(V) && (cols & ~7u) < upto) {
-            const raw8<T> some = load_some(at(row, cols & ~7u), cols % 8u);
-#pragma unroll
-            for (int v = 0; v < V; ++v)
-                if (uint32_t(v) == mine) raw[v] = some;
+        f32x8 x = widen<T>(raw);
+        if (ends_in(v) && !(kShort && cols < 8u)) {
+            const f32x8 y = shifted(x, 8u - cols % 8u);
+            if (ends_here()) x = y;
         }
+        return x;
     }
-    // x[v] of every round, by a function that makes it
+    __device__ __forceinline__ void store_round(T *row, int v, f32x8 x) const
+    {
+        if (whole(v)) store8(at(row, col(v)), x);
+        else if (col(v) < cols) store_some(at(row, col(v)), cols % 8u, x);
+    }
+    // x(v) of every round, to its place
     template <typename F> __device__ __forceinline__ void store(T *row, F &&x) const
     {
-        const uint32_t mine = cols % 8u == 0u ? uint32_t(V) : tail();
         f32x8 some = {};
+        bool mine = false;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             if (col(v) < cols) {
                 const f32x8 y = x(v);
                 if (whole(v)) store8(at(row, col(v)), y);
-                else some = y;
+                else { some = y; mine = true; }
             }
         }
-        if (mine < uint32_t(V)) store_some(at(row, cols & ~7u), cols % 8u, some);
+        if (cols % 8u != 0u && mine) store_some(at(row, cols & ~7u), cols % 8u, some);
     }
 };
-
-template <typename T> __device__ __forceinline__ f32x8 widen(raw8<T> v) { return __builtin_convertvector(v, f32x8); }
 
 // A value that the compiler takes for a new one: what is made from it inside a loop is made there.  Otherwise everything about
 // a row that its threads and length decide moves in front of the loop over rows, and costs it its registers: scalar ones

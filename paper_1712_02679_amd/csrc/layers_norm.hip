@@ -7,34 +7,33 @@ namespace adacomp {
 // y = [residual +] D(x).  One group of 8 columns to a thread and round; rows are cut into groups of their own, so that a
 // group is one counter wherever it lies.
 
-constexpr uint32_t kDropRounds = 4;
-
 template <typename T> __global__ __launch_bounds__(256) void k_dropout(DropoutLaunch a)
 {
     const Drop d = drop_of(a.drop);
-    const uint32_t total = a.rows * a.groups;
-#pragma unroll
-    for (uint32_t u = 0; u < kDropRounds; ++u) {
-        const uint32_t g = (blockIdx.x * kDropRounds + u) * 256u + threadIdx.x;
-        if (g >= total) break;
-        const uint32_t r = g / a.groups, c = g - r * a.groups;
-        const uint64_t row = a.first_row + r;
-        const uint32_t n = a.cols - c * 8u;
-        const T *x = static_cast<const T *>(a.x) + row * a.x_stride + c * 8ull, *res = static_cast<const T *>(a.residual) + row * a.residual_stride + c * 8ull;
-        T *y = static_cast<T *>(a.y) + row * a.y_stride + c * 8ull;
-        raw8<T> raw = {}, raw_res = {};
-        if (n >= 8u) {
-            raw = load8(x);
-            if (a.residual) raw_res = load8(res);
-        } else {
-            raw = load_some(x, n);
-            if (a.residual) raw_res = load_some(res, n);
-        }
-        f32x8 v = drop8(widen<T>(raw), d, c, uint32_t(row));
-        if (a.residual) v += widen<T>(raw_res);
-        if (n >= 8u) store8(y, v);
-        else store_some(y, n, v);
+    const uint32_t g = blockIdx.x * 256u + threadIdx.x;
+    if (g >= a.rows * a.groups) return;
+    const uint32_t r = g / a.groups, c = g - r * a.groups;
+    const uint64_t row = a.first_row + r, col = c * 8ull;
+    const uint32_t n = a.cols - c * 8u, back = a.cols < 8u || n >= 8u ? 0u : 8u - n;   // an incomplete group reads the row's last 8 values
+    const T *x = static_cast<const T *>(a.x) + row * a.x_stride + col - back, *res = static_cast<const T *>(a.residual) + row * a.residual_stride + col - back;
+    raw8<T> raw, raw_res = {};
+    if (a.cols >= 8u) {
+        raw = load8(x);
+        if (a.residual) raw_res = load8(res);
+    } else {
+        raw = load_some(x, n);
+        if (a.residual) raw_res = load_some(res, n);
     }
+    f32x8 v = widen<T>(raw), w = widen<T>(raw_res);
+    if (back) {
+        v = shifted(v, 8u - a.cols % 8u);
+        w = shifted(w, 8u - a.cols % 8u);
+    }
+    v = drop8(v, d, c, uint32_t(row));
+    if (a.residual) v += w;
+    T *y = static_cast<T *>(a.y) + row * a.y_stride + col;
+    if (n >= 8u) store8(y, v);
+    else store_some(y, n, v);
 }
 
 // ---- layer norm, forward ------------------------------------------------------------------------------------------
@@ -60,68 +59,51 @@ template <typename T, int TPR, int V> __global__ __launch_bounds__(TPR > 256 ? T
 {
     constexpr uint32_t TEAMS = TPR > 256 ? 1 : 256 / TPR;
     __shared__ float room[2][16];
-    const uint32_t t = threadIdx.x % TPR, team = team_of<TPR>();
-    const Drop d = drop_of(a.drop);
-    for (uint32_t first = blockIdx.x * TEAMS; first < a.rows; first += gridDim.x * TEAMS) {
-        const bool live = first + team < a.rows;
-        const uint32_t row = live ? first + team : a.rows - 1u;   // the last rows' workgroup has teams without one: they go along
-        const T *x = static_cast<const T *>(a.x) + row * a.x_stride;
-        const uint32_t cols = again_uniform(a.cols);
-        const RowGroups<T, TPR, V> groups = {again(t), cols, 0};
-        const RowGroups<float, TPR, V> params = {groups.t, cols, 0};
-        const Drop dr = again(d);
-        raw8<T> raw[V], raw_res[V];
-        groups.load(raw, x);
+    const uint32_t t = threadIdx.x % TPR, team = team_of<TPR>(), row = blockIdx.x * TEAMS + team;
+    const bool live = row < a.rows;   // the last workgroup may have teams without a row: they go along to the barriers
+    const RowGroups<T, TPR, V> groups = {t, a.cols, 0};
+    raw8<T> raw[V] = {}, raw_res[V] = {};
+    if (live) {
+        groups.load(raw, static_cast<const T *>(a.x) + row * a.x_stride);
         if (a.residual) groups.load(raw_res, static_cast<const T *>(a.residual) + row * a.residual_stride);
-        raw8<float> some_gamma, some_beta;
-        if (a.gamma) some_gamma = params.some(a.gamma);
-        if (a.beta) some_beta = params.some(a.beta);
-        raw8<float> gamma[V], beta[V];   // up to 8192 columns on their way together with the row, in wider rows behind its sums
-        if constexpr (V == 1) {
-            if (a.gamma) gamma[0] = params.round(a.gamma, 0, some_gamma);
-            if (a.beta) beta[0] = params.round(a.beta, 0, some_beta);
-        }
-        f32x8 z[V];
-        float sum = 0.f;
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            z[v] = widen<T>(raw[v]);
-            if (a.drop.on) z[v] = drop8(z[v], dr, groups.col(v) / 8u, row);
-            if (a.residual) z[v] += widen<T>(raw_res[v]);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) sum += z[v][k];
-        }
-        const float mean = over_row<TPR>(sum, room[0], team) / float(a.cols);
-        float squares = 0.f;
-        f32x8 c[V];
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            c[v] = z[v] - mean;
-            if (!groups.whole(v)) {   // nothing behind the row's end counts
-#pragma unroll
-                for (int k = 0; k < 8; ++k) c[v][k] = groups.col(v) + k < cols ? c[v][k] : 0.f;
-            }
-#pragma unroll
-            for (int k = 0; k < 8; ++k) squares = fmaf(c[v][k], c[v][k], squares);
-        }
-        const float rstd = 1.f / sqrtf(over_row<TPR>(squares, room[1], team) / float(a.cols) + a.eps);
-        if (!live) continue;
-        if (t == 0u) {
-            if (a.mean) a.mean[row] = mean;
-            if (a.rstd) a.rstd[row] = rstd;
-        }
-        if (a.z) groups.store(static_cast<T *>(a.z) + row * a.z_stride, [&](int v) { return z[v]; });
-        groups.store(static_cast<T *>(a.y) + row * a.y_stride, [&](int v) {
-            f32x8 y = c[v] * rstd;
-            if constexpr (V > 1) {
-                if (a.gamma) gamma[v] = params.round(a.gamma, v, some_gamma);
-                if (a.beta) beta[v] = params.round(a.beta, v, some_beta);
-            }
-            if (a.gamma) y *= gamma[v];
-            if (a.beta) y += beta[v];
-            return y;
-        });
     }
+    const Drop d = drop_of(a.drop);
+    f32x8 z[V];
+    float sum = 0.f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        z[v] = groups.values(raw[v], v);
+        if (a.drop.on) z[v] = drop8(z[v], d, groups.col(v) / 8u, uint32_t(a.first_row) + row);
+        if (a.residual) z[v] += groups.values(raw_res[v], v);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum += z[v][k];
+    }
+    const float mean = over_row<TPR>(sum, room[0], team) / float(a.cols);
+    float squares = 0.f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        f32x8 c = z[v] - mean;
+        if (!groups.whole(v)) {   // nothing behind the row's end counts
+#pragma unroll
+            for (int k = 0; k < 8; ++k) c[k] = groups.col(v) + k < a.cols ? c[k] : 0.f;
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) squares = fmaf(c[k], c[k], squares);
+    }
+    const float rstd = 1.f / sqrtf(over_row<TPR>(squares, room[1], team) / float(a.cols) + a.eps);
+    if (!live) return;
+    if (t == 0u) {
+        if (a.mean) a.mean[row] = mean;
+        if (a.rstd) a.rstd[row] = rstd;
+    }
+    if (a.z) groups.store(static_cast<T *>(a.z) + row * a.z_stride, [&](int v) { return z[v]; });
+    const RowGroups<float, TPR, V> params = {t, a.cols, 0};
+    groups.store(static_cast<T *>(a.y) + row * a.y_stride, [&](int v) {
+        f32x8 y = (z[v] - mean) * rstd;
+        if (a.gamma) y *= params.values(params.load_round(a.gamma, v), v);
+        if (a.beta) y += params.values(params.load_round(a.beta, v), v);
+        return y;
+    });
 }
 
 // ---- layer norm, backward -----------------------------------------------------------------------------------------
@@ -131,27 +113,28 @@ template <typename T, int TPR, int V> __global__ __launch_bounds__(TPR > 256 ? T
 
 constexpr uint32_t kBackThreads = 1024;
 
-template <typename T, int TPR, int V> __global__ __launch_bounds__(kBackThreads) void k_norm_backward(NormBackward a)
+template <typename T, int TPR> __global__ __launch_bounds__(kBackThreads) void k_norm_backward(NormBackward a)
 {
-    constexpr uint32_t TEAMS = kBackThreads / TPR, COLS = TPR * V * 8;
+    constexpr uint32_t TEAMS = kBackThreads / TPR, COLS = TPR * 8;
     __shared__ float room[2][2][16];
     __shared__ float sums[TEAMS > 1 ? TEAMS * COLS : 1];
     const uint32_t t = threadIdx.x % TPR, team = team_of<TPR>();
     const Drop d = drop_of(a.drop);
     const float per_col = 1.f / float(a.cols);
-    f32x8 dgamma[V] = {}, dbeta[V] = {};
-    raw8<float> gamma[V];
-    if (a.gamma) RowGroups<float, TPR, V>{t, a.cols, 0}.load(gamma, a.gamma);
-    raw8<T> raw_dy[V], raw_z[V], raw_add[V];
+    f32x8 dgamma = 0.f, dbeta = 0.f, gamma = 1.f;
+    if (a.gamma) {
+        const RowGroups<float, TPR, 1> params = {t, a.cols, 0};
+        gamma = params.values(params.load_round(a.gamma, 0), 0);
+    }
+    raw8<T> raw_dy, raw_z, raw_add;
     float mean = 0.f, rstd = 0.f;
     auto fetch = [&](uint32_t row) {
-        const RowGroups<T, TPR, V> groups = {again(t), again_uniform(a.cols), 0};
-#pragma unroll
-        for (int v = 0; v < V; ++v) raw_dy[v] = raw_z[v] = raw_add[v] = raw8<T>{};
+        const RowGroups<T, TPR, 1> groups = {again(t), again_uniform(a.cols), 0};
+        raw_dy = raw_z = raw_add = raw8<T>{};
         if (row < a.rows) {
-            groups.load(raw_dy, static_cast<const T *>(a.dy) + row * a.dy_stride);
-            groups.load(raw_z, static_cast<const T *>(a.z) + row * a.z_stride);
-            if (a.dz_add) groups.load(raw_add, static_cast<const T *>(a.dz_add) + row * a.dz_add_stride);
+            raw_dy = groups.load_round(static_cast<const T *>(a.dy) + row * a.dy_stride, 0);
+            raw_z = groups.load_round(static_cast<const T *>(a.z) + row * a.z_stride, 0);
+            if (a.dz_add) raw_add = groups.load_round(static_cast<const T *>(a.dz_add) + row * a.dz_add_stride, 0);
             mean = a.mean[row];
             rstd = a.rstd[row];
         }
@@ -161,24 +144,19 @@ template <typename T, int TPR, int V> __global__ __launch_bounds__(kBackThreads)
     for (uint32_t first = blockIdx.x * TEAMS; first < a.rows; first += gridDim.x * TEAMS) {
         const uint32_t row = first + team;
         const float scale = rstd;
-        f32x8 g[V], h[V], dz[V];
-        float s1 = 0.f, s2 = 0.f;
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            g[v] = widen<T>(raw_dy[v]);
-            h[v] = (widen<T>(raw_z[v]) - mean) * scale;
-            dz[v] = widen<T>(raw_add[v]);
-            dbeta[v] += g[v];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) dgamma[v][k] = fmaf(g[v][k], h[v][k], dgamma[v][k]);
-            if (a.gamma) g[v] *= gamma[v];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                s1 += g[v][k];   // behind the row's end, and in teams without a row, g is 0
-                s2 = fmaf(g[v][k], h[v][k], s2);
-            }
-        }
+        const RowGroups<T, TPR, 1> groups = {again(t), again_uniform(a.cols), 0};
+        f32x8 g = groups.values(raw_dy, 0), dz = groups.values(raw_add, 0);
+        const f32x8 h = (groups.values(raw_z, 0) - mean) * scale;
         fetch(row + gridDim.x * TEAMS);
+        float s1 = 0.f, s2 = 0.f;
+        dbeta += g;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            dgamma[k] = fmaf(g[k], h[k], dgamma[k]);
+            g[k] *= gamma[k];   // behind the row's end, and in teams without a row, g is 0
+            s1 += g[k];
+            s2 = fmaf(g[k], h[k], s2);
+        }
         if constexpr (TPR <= 64) {
             s1 = over_lanes<Add, TPR>(s1);
             s2 = over_lanes<Add, TPR>(s2);
@@ -196,25 +174,18 @@ template <typename T, int TPR, int V> __global__ __launch_bounds__(kBackThreads)
         if (row >= a.rows) continue;
         s1 *= per_col;
         s2 *= per_col;
-        const RowGroups<T, TPR, V> groups = {again(t), again_uniform(a.cols), 0};
-        const Drop dr = again(d);
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-#pragma unroll
-            for (int k = 0; k < 8; ++k) dz[v][k] = fmaf(scale, g[v][k] - fmaf(h[v][k], s2, s1), dz[v][k]);
-        groups.store(static_cast<T *>(a.dz) + row * a.dz_stride, [&](int v) { return dz[v]; });
-        if (a.dx) groups.store(static_cast<T *>(a.dx) + row * a.dx_stride, [&](int v) { return drop8(dz[v], dr, groups.col(v) / 8u, row); });
+        for (int k = 0; k < 8; ++k) dz[k] = fmaf(scale, g[k] - fmaf(h[k], s2, s1), dz[k]);
+        groups.store(static_cast<T *>(a.dz) + row * a.dz_stride, [&](int) { return dz; });
+        if (a.dx) groups.store(static_cast<T *>(a.dx) + row * a.dx_stride, [&](int) { return drop8(dz, again(d), groups.col(0) / 8u, row); });
     }
-    float *out = a.partial;
-    if (!out) return;
-    out += uint64_t(blockIdx.x) * 2u * a.pitch;
+    if (!a.partial) return;
+    float *out = a.partial + uint64_t(blockIdx.x) * 2u * a.pitch;
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
         if constexpr (TEAMS > 1) {
             __syncthreads();
-#pragma unroll
-            for (int v = 0; v < V; ++v)
-                *reinterpret_cast<f32x8 *>(&sums[team * COLS + (t + v * TPR) * 8u]) = which ? dbeta[v] : dgamma[v];
+            *reinterpret_cast<f32x8 *>(&sums[team * COLS + t * 8u]) = which ? dbeta : dgamma;
             __syncthreads();
             for (uint32_t c = threadIdx.x; c < a.pitch; c += kBackThreads) {
                 float s = 0.f;
@@ -222,13 +193,66 @@ template <typename T, int TPR, int V> __global__ __launch_bounds__(kBackThreads)
                 for (uint32_t m = 0; m < TEAMS; ++m) s += sums[m * COLS + c];
                 out[which * a.pitch + c] = s;
             }
-        } else {
+        } else if (t * 8u < a.pitch) {
+            *reinterpret_cast<f32x8 *>(out + which * a.pitch + t * 8u) = which ? dbeta : dgamma;
+        }
+    }
+}
+
+// Rows of more than 8192 columns: the sums of V groups of columns leave no registers for the row, which is read a second time, from
+// the caches, for dz.
+template <typename T, int V> __global__ __launch_bounds__(kBackThreads) void k_norm_backward_wide(NormBackward a)
+{
+    constexpr int TPR = kBackThreads;
+    __shared__ float room[2][16];
+    const uint32_t t = threadIdx.x;
+    const Drop d = drop_of(a.drop);
+    const float per_col = 1.f / float(a.cols);
+    f32x8 dgamma[V] = {}, dbeta[V] = {};
+    for (uint32_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const T *dy = static_cast<const T *>(a.dy) + row * a.dy_stride, *z = static_cast<const T *>(a.z) + row * a.z_stride;
+        const float mean = a.mean[row], rstd = a.rstd[row];
+        float s1 = 0.f, s2 = 0.f;
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const uint32_t c = (t + v * TPR) * 8u;
-                if (c < a.pitch) *reinterpret_cast<f32x8 *>(out + which * a.pitch + c) = which ? dbeta[v] : dgamma[v];
+        for (int v = 0; v < V; ++v) {
+            const RowGroups<T, TPR, V> groups = {again(t), again_uniform(a.cols), 0};
+            const RowGroups<float, TPR, V> params = {groups.t, groups.cols, 0};
+            f32x8 g = groups.values(groups.load_round(dy, v), v);
+            const f32x8 h = (groups.values(groups.load_round(z, v), v) - mean) * rstd;
+            dbeta[v] += g;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) dgamma[v][k] = fmaf(g[k], h[k], dgamma[v][k]);
+            if (a.gamma) g *= params.values(params.load_round(a.gamma, v), v);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                s1 += g[k];
+                s2 = fmaf(g[k], h[k], s2);
             }
         }
+        s1 = over_waves<Add, TPR / 64>(over_lanes<Add, 64>(s1), room[0]) * per_col;
+        s2 = over_waves<Add, TPR / 64>(over_lanes<Add, 64>(s2), room[1]) * per_col;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const RowGroups<T, TPR, V> groups = {again(t), again_uniform(a.cols), 0};
+            const RowGroups<float, TPR, V> params = {groups.t, groups.cols, 0};
+            f32x8 g = groups.values(groups.load_round(dy, v), v), dz = 0.f;
+            const f32x8 h = (groups.values(groups.load_round(z, v), v) - mean) * rstd;
+            if (a.gamma) g *= params.values(params.load_round(a.gamma, v), v);
+            if (a.dz_add) dz = groups.values(groups.load_round(static_cast<const T *>(a.dz_add) + row * a.dz_add_stride, v), v);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) dz[k] = fmaf(rstd, g[k] - fmaf(h[k], s2, s1), dz[k]);
+            groups.store_round(static_cast<T *>(a.dz) + row * a.dz_stride, v, dz);
+            if (a.dx) groups.store_round(static_cast<T *>(a.dx) + row * a.dx_stride, v, drop8(dz, again(d), groups.col(v) / 8u, row));
+        }
+    }
+    if (!a.partial) return;
+    float *out = a.partial + uint64_t(blockIdx.x) * 2u * a.pitch;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const uint32_t c = (t + v * TPR) * 8u;
+        if (c >= a.pitch) continue;
+        *reinterpret_cast<f32x8 *>(out + c) = dgamma[v];
+        *reinterpret_cast<f32x8 *>(out + a.pitch + c) = dbeta[v];
     }
 }
 
@@ -258,8 +282,7 @@ static int check_launch() { return hipGetLastError() == hipSuccess ? ADACOMP_OK 
 
 int launch_dropout(const DropoutLaunch &a, void *stream)
 {
-    const uint32_t total = a.rows * a.groups, per = 256u * kDropRounds;
-    const dim3 grid((total + per - 1u) / per), wg(256);
+    const dim3 grid((a.rows * a.groups + 255u) / 256u), wg(256);
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (a.dtype == ADACOMP_DTYPE_F32) hipLaunchKernelGGL(k_dropout<float>, grid, wg, 0, s, a);
     else if (a.dtype == ADACOMP_DTYPE_BF16) hipLaunchKernelGGL(k_dropout<bf16>, grid, wg, 0, s, a);
@@ -267,61 +290,90 @@ int launch_dropout(const DropoutLaunch &a, void *stream)
     return check_launch();
 }
 
-// 8 values to a thread as far as 1024 threads hold the row.
-RowForm norm_form(uint32_t cols)
+// Forward: 16 values to a thread, or up to 32 in the widest rows (16 and not 8: twice the bytes on their way for a wave, at no more
+// than 64 registers).  Backward: 8, of columns whose sums a thread keeps.
+static uint32_t forward_threads(uint32_t cols)
+{
+    uint32_t threads = 8;
+    while (threads < 1024u && threads * (cols <= 64u ? 8u : 16u) < cols) threads *= 2u;
+    return threads;
+}
+
+static uint32_t backward_threads(uint32_t cols)
 {
     uint32_t threads = 8;
     while (threads < 1024u && threads * 8u < cols) threads *= 2u;
-    return {threads, cols <= 8192u ? 1u : cols <= 16384u ? 2u : 4u};
+    return threads;
 }
-
-constexpr uint32_t kMostWorkgroups = 1u << 20;   // a launch has fewer than 2^32 threads; more rows are walked over
 
 uint32_t norm_parts(uint64_t rows, uint32_t cols)
 {
-    const uint32_t teams = kBackThreads / norm_form(cols).threads;
+    const uint32_t teams = kBackThreads / backward_threads(cols);
     return uint32_t(std::min<uint64_t>((rows + teams - 1u) / teams, kComputeUnits));
 }
 
-template <template <typename, int, int> class K, typename A>
-static int launch_rows(const RowForm &f, uint32_t dtype, uint32_t workgroups, uint32_t threads, const A &a, void *stream)
+// Calls f with a type, and with the number of threads.
+template <typename F> static int with_type(uint32_t dtype, F &&f)
 {
-    const dim3 grid(workgroups), wg(threads);
-    hipStream_t s = static_cast<hipStream_t>(stream);
-    auto go = [&](auto form) {
-        constexpr int TPR = decltype(form)::threads, V = decltype(form)::groups;
-        if (dtype == ADACOMP_DTYPE_F32) hipLaunchKernelGGL((K<float, TPR, V>::kernel), grid, wg, 0, s, a);
-        else if (dtype == ADACOMP_DTYPE_BF16) hipLaunchKernelGGL((K<bf16, TPR, V>::kernel), grid, wg, 0, s, a);
-        else hipLaunchKernelGGL((K<f16, TPR, V>::kernel), grid, wg, 0, s, a);
-    };
-    switch (f.threads * f.groups) {
-    case 8: go(FormOf<8, 1>()); break;
-    case 16: go(FormOf<16, 1>()); break;
-    case 32: go(FormOf<32, 1>()); break;
-    case 64: go(FormOf<64, 1>()); break;
-    case 128: go(FormOf<128, 1>()); break;
-    case 256: go(FormOf<256, 1>()); break;
-    case 512: go(FormOf<512, 1>()); break;
-    case 1024: go(FormOf<1024, 1>()); break;
-    case 2048: go(FormOf<1024, 2>()); break;
-    case 4096: go(FormOf<1024, 4>()); break;
-    default: return ADACOMP_EINVAL;
-    }
+    if (dtype == ADACOMP_DTYPE_F32) f(float());
+    else if (dtype == ADACOMP_DTYPE_BF16) f(bf16());
+    else f(f16());
     return check_launch();
 }
 
-template <typename T, int TPR, int V> struct KForward { static constexpr auto kernel = k_norm_forward<T, TPR, V>; };
-template <typename T, int TPR, int V> struct KBackward { static constexpr auto kernel = k_norm_backward<T, TPR, V>; };
-
-int launch_norm_forward(const NormForward &a, uint32_t dtype, void *stream)
+template <typename F> static void with_threads(uint32_t threads, F &&f)
 {
-    const RowForm f = norm_form(a.cols);
-    return launch_rows<KForward>(f, dtype, std::min((a.rows + f.teams() - 1u) / f.teams(), kMostWorkgroups), f.workgroup(), a, stream);
+    switch (threads) {
+    case 8: return f(std::integral_constant<int, 8>());
+    case 16: return f(std::integral_constant<int, 16>());
+    case 32: return f(std::integral_constant<int, 32>());
+    case 64: return f(std::integral_constant<int, 64>());
+    case 128: return f(std::integral_constant<int, 128>());
+    case 256: return f(std::integral_constant<int, 256>());
+    case 512: return f(std::integral_constant<int, 512>());
+    default: return f(std::integral_constant<int, 1024>());
+    }
+}
+
+int launch_norm_forward(const NormForward &args, uint32_t dtype, void *stream)
+{
+    const uint32_t threads = forward_threads(args.cols), wg = std::max(threads, 256u), teams = wg / threads;
+    const uint64_t step = uint64_t(1) << 22;   // rows of a launch: it has fewer than 2^32 threads
+    const uint64_t size = dtype == ADACOMP_DTYPE_F32 ? 4u : 2u;
+    for (uint64_t first = 0; first < args.all_rows; first += step) {
+        NormForward a = args;
+        const auto on = [first, size](const void *p, uint64_t stride) { return p ? static_cast<const char *>(p) + first * stride * size : nullptr; };
+        a.first_row = first;
+        a.rows = uint32_t(std::min(step, args.all_rows - first));
+        a.x = on(a.x, a.x_stride);
+        a.residual = on(a.residual, a.residual_stride);
+        a.z = const_cast<char *>(on(a.z, a.z_stride));
+        a.y = const_cast<char *>(on(a.y, a.y_stride));
+        if (a.mean) a.mean += first;
+        if (a.rstd) a.rstd += first;
+        const dim3 grid((a.rows + teams - 1u) / teams);
+        hipStream_t s = static_cast<hipStream_t>(stream);
+        const int rc = with_type(dtype, [&](auto of) {
+            using T = decltype(of);
+            if (a.cols <= 64u) hipLaunchKernelGGL((k_norm_forward<T, 8, 1>), grid, dim3(wg), 0, s, a);
+            else if (a.cols > 16384u) hipLaunchKernelGGL((k_norm_forward<T, 1024, 4>), grid, dim3(wg), 0, s, a);
+            else with_threads(threads, [&](auto n) { hipLaunchKernelGGL((k_norm_forward<T, decltype(n)::value, 2>), grid, dim3(wg), 0, s, a); });
+        });
+        if (rc) return rc;
+    }
+    return ADACOMP_OK;
 }
 
 int launch_norm_backward(const NormBackward &a, uint32_t dtype, uint32_t parts, void *stream)
 {
-    return launch_rows<KBackward>(norm_form(a.cols), dtype, parts, kBackThreads, a, stream);
+    const dim3 grid(parts), wg(kBackThreads);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return with_type(dtype, [&](auto of) {
+        using T = decltype(of);
+        if (a.cols > 16384u) hipLaunchKernelGGL((k_norm_backward_wide<T, 4>), grid, wg, 0, s, a);
+        else if (a.cols > 8192u) hipLaunchKernelGGL((k_norm_backward_wide<T, 2>), grid, wg, 0, s, a);
+        else with_threads(backward_threads(a.cols), [&](auto n) { hipLaunchKernelGGL((k_norm_backward<T, decltype(n)::value>), grid, wg, 0, s, a); });
+    });
 }
 
 int launch_norm_reduce(const NormReduce &a, void *stream)

@@ -41,6 +41,7 @@ struct NormForward {
     void *z, *y;
     float *mean, *rstd;
     uint64_t x_stride, residual_stride, z_stride, y_stride;
+    uint64_t all_rows, first_row;   // of the call; of a launch, whose pointers begin there
     uint32_t rows, cols;
     float eps;
     DropArgs drop;
@@ -62,7 +63,6 @@ struct NormReduce {
     uint32_t parts, pitch, cols, accumulate;
 };
 
-RowForm norm_form(uint32_t cols);
 uint32_t norm_parts(uint64_t rows, uint32_t cols);   // workgroups of the backward pass
 inline uint32_t norm_pitch(uint32_t cols) { return (cols + 7u) & ~7u; }
 

@@ -78,6 +78,13 @@ template <bool MASK> __device__ __forceinline__ uint32_t admitted8(uint64_t mask
     return bits;
 }
 
+// The mask's bytes that were loaded for round v, in their place.
+template <typename G> __device__ __forceinline__ uint64_t mask_of(const G &groups, raw8<uint8_t> raw, int v)
+{
+    const uint64_t m = __builtin_bit_cast(uint64_t, raw);
+    return groups.ends_in(v) && !(G::kShort && groups.cols < 8u) && groups.ends_here() ? m >> 8u * (8u - groups.cols % 8u) : m;
+}
+
 // scale2 * s + bias - less of 8 keys.
 __device__ __forceinline__ f32x8 biased8(f32x8 s, const SoftmaxArgs &a, const Row &r, const Window &w, const float *bias, float low, float high, float less)
 {
@@ -143,9 +150,9 @@ template <typename T, int TPR, int V, int PHASE, bool MASK> __global__ __launch_
                 const int j = int(groups.col(v)), n = r.limit - j;
                 p[v] = -kInf;
                 if (n > 0) {
-                    const uint32_t here = admitted8<MASK>(MASK ? __builtin_bit_cast(uint64_t, mask[v]) : 0, n);
+                    const uint32_t here = admitted8<MASK>(MASK ? mask_of(groups, mask[v], v) : 0, n);
                     bits |= here << (8 * v);
-                    p[v] = biased8(widen<T>(raw[v]), a, r, Window(r, j), bias, low, high, 0.f);
+                    p[v] = biased8(groups.values(raw[v], v), a, r, Window(r, j), bias, low, high, 0.f);
                     if (here != 0xFFu) {
 #pragma unroll
                         for (int k = 0; k < 8; ++k) p[v][k] = here >> k & 1u ? p[v][k] : -kInf;
@@ -274,8 +281,8 @@ template <typename T, int TPR, int V, int PHASE, bool MASK> __global__ __launch_
             p[v] = 0.f;
             dp[v] = 0.f;
             if (n > 0) {
-                const uint32_t bits = admitted8<MASK>(MASK ? __builtin_bit_cast(uint64_t, mask[v]) : 0, n);
-                p[v] = biased8(widen<T>(raw[v]), a, r, Window(r, j), bias, bias_low, bias_high, less);
+                const uint32_t bits = admitted8<MASK>(MASK ? mask_of(groups, mask[v], v) : 0, n);
+                p[v] = biased8(groups.values(raw[v], v), a, r, Window(r, j), bias, bias_low, bias_high, less);
                 if (coarse) {
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
@@ -283,7 +290,7 @@ template <typename T, int TPR, int V, int PHASE, bool MASK> __global__ __launch_
                         p[v][k] = x > fabsf(lse2) * -0x1p-21f ? 0.f : x;
                     }
                 }
-                dp[v] = widen<T>(raw_up[v]);
+                dp[v] = groups.values(raw_up[v], v);
                 if (a.drop.on) dp[v] = kept8(dp[v], dr, uint32_t(j) / 8u, uint32_t(row));
 #pragma unroll
                 for (int k = 0; k < 8; ++k) p[v][k] = __builtin_amdgcn_exp2f(p[v][k]);
