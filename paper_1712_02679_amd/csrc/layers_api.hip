@@ -64,7 +64,7 @@ static SoftmaxRoom softmax_room(uint64_t batch, uint64_t heads, uint64_t queries
     const SoftmaxForm form = softmax_form(keys, distance, backward);
     SoftmaxRoom room = {0, 0};
     if (form.parts > 1u) room.stats = pad256(size_t(batch * heads * queries) * form.parts * 8u);
-    if (backward && heads) room.sums = pad256(size_t(heads) * softmax_back_groups(batch * queries, uint32_t(heads), form) * (2u * distance + 1u) * 4u);
+    if (backward && heads) room.sums = pad256(size_t(heads) * softmax_back_groups_most(batch * queries, uint32_t(heads), form) * (2u * distance + 1u) * 4u);
     return room;
 }
 
@@ -256,17 +256,17 @@ int adacomp_bias_softmax_backward(const adacomp_bias_softmax_t *op, const adacom
     SoftmaxRoom room = softmax_room(a.batch, a.heads, a.queries, a.keys, a.distance, true);
     if (!dtable) room.sums = 0;
     char *base = static_cast<char *>(workspace);
+    uint32_t groups = 0;
     if (rows_of_head != 0) {
         if (!lse) return ADACOMP_EINVAL;
         if (int rc = workspace_check(workspace, workspace_bytes, room.all())) return rc;
         a.lse = const_cast<float *>(lse);
         a.part_stats = reinterpret_cast<float *>(base);
         a.bias_sums = dtable ? reinterpret_cast<float *>(base + room.stats) : nullptr;
-        if (int rc = launch_softmax_backward(a, op->dtype, form, hip_stream)) return rc;
+        if (int rc = launch_softmax_backward(a, op->dtype, form, groups, hip_stream)) return rc;
     }
     if (!dtable) return ADACOMP_OK;
-    const BiasReduce r = {reinterpret_cast<const float *>(base + room.stats), a.map, dtable, a.heads,
-                          softmax_back_groups(rows_of_head, a.heads, form), a.distance, a.n_buckets, accumulate != 0};
+    const BiasReduce r = {reinterpret_cast<const float *>(base + room.stats), a.map, dtable, a.heads, groups, a.distance, a.n_buckets, accumulate != 0};
     return launch_bias_reduce(r, hip_stream);
 }
 

@@ -335,6 +335,16 @@ template <typename F> static void with_threads(uint32_t threads, F &&f)
     }
 }
 
+// Idle LDS of a workgroup, to have fewer of them on a compute unit.  Memory serves large calls with a residual best while about 96 KB a
+// unit are on their way to it; all that fit would ask for 128 (16 bits) or 256.  All / so many, in us: 16384 x 4096 bf16 105 / 99, f32 203 / 188, 8192 x 8192
+// bf16 101 / 97; smaller calls, narrower rows and calls without a residual lose (2000 x 4096 bf16 13.6 / 14.5; 165536 x 300 95 / 106; without 58 / 60).
+static uint32_t idle_lds(const NormForward &a, uint32_t size, uint32_t wg)
+{
+    if (!a.residual || a.cols <= 1024u || uint64_t(a.rows) * a.cols * size * 4u < (uint64_t(256) << 20)) return 0;
+    const uint32_t fit = std::max(2u, (96u << 10) / (wg * 2u * 8u * size * 2u));   // two groups of 8 from two tensors to a thread
+    return fit * wg >= 2048u ? 0u : (160u << 10) / (fit + 1u) + 256u;
+}
+
 int launch_norm_forward(const NormForward &args, uint32_t dtype, void *stream)
 {
     const uint32_t threads = forward_threads(args.cols), wg = std::max(threads, 256u), teams = wg / threads;
@@ -352,12 +362,13 @@ int launch_norm_forward(const NormForward &args, uint32_t dtype, void *stream)
         if (a.mean) a.mean += first;
         if (a.rstd) a.rstd += first;
         const dim3 grid((a.rows + teams - 1u) / teams);
+        const uint32_t lds = idle_lds(a, uint32_t(size), wg);
         hipStream_t s = static_cast<hipStream_t>(stream);
         const int rc = with_type(dtype, [&](auto of) {
             using T = decltype(of);
-            if (a.cols <= 64u) hipLaunchKernelGGL((k_norm_forward<T, 8, 1>), grid, dim3(wg), 0, s, a);
-            else if (a.cols > 16384u) hipLaunchKernelGGL((k_norm_forward<T, 1024, 4>), grid, dim3(wg), 0, s, a);
-            else with_threads(threads, [&](auto n) { hipLaunchKernelGGL((k_norm_forward<T, decltype(n)::value, 2>), grid, dim3(wg), 0, s, a); });
+            if (a.cols <= 64u) hipLaunchKernelGGL((k_norm_forward<T, 8, 1>), grid, dim3(wg), lds, s, a);
+            else if (a.cols > 16384u) hipLaunchKernelGGL((k_norm_forward<T, 1024, 4>), grid, dim3(wg), lds, s, a);
+            else with_threads(threads, [&](auto n) { hipLaunchKernelGGL((k_norm_forward<T, decltype(n)::value, 2>), grid, dim3(wg), lds, s, a); });
         });
         if (rc) return rc;
     }

@@ -106,10 +106,10 @@ struct SoftmaxForm {
     uint32_t parts;   // 1: whole rows
 };
 SoftmaxForm softmax_form(uint32_t keys, uint32_t distance, bool backward);
-uint32_t softmax_back_groups(uint64_t rows_of_head, uint32_t heads, const SoftmaxForm &form);   // workgroups to a head
+uint32_t softmax_back_groups_most(uint64_t rows_of_head, uint32_t heads, const SoftmaxForm &form);
 
 int launch_softmax_forward(const SoftmaxArgs &a, uint32_t dtype, const SoftmaxForm &form, void *stream);
-int launch_softmax_backward(const SoftmaxArgs &a, uint32_t dtype, const SoftmaxForm &form, void *stream);
+int launch_softmax_backward(const SoftmaxArgs &a, uint32_t dtype, const SoftmaxForm &form, uint32_t &groups, void *stream);   // groups: workgroups to a head, of the bias_sums
 int launch_bias_reduce(const BiasReduce &a, void *stream);
 
 }  // namespace adacomp

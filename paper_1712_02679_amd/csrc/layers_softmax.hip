@@ -5,7 +5,10 @@
 // beyond D on one side cost none.  The gradient goes the same way back: sums by distance, added up in LDS (inside a row all
 // distances differ, so no two threads of a row meet, and rows follow each other), those beyond D in registers; k_bias_reduce
 // adds the workgroups' sums and only then turns distances into buckets.
+#include <atomic>
+
 #include "layers_device.h"
+
 
 namespace adacomp {
 
@@ -337,9 +340,14 @@ template <typename T, int TPR, int V, int PHASE, bool MASK> __global__ __launch_
                         low += w.below() ? e : 0.f;
                         high += w.below() ? 0.f : e;
                     } else {
-                        // no two lanes of a row have one distance, and a wave's additions stay in order: the sums repeat bit for bit
+                        // No two threads of a row have one distance, and a wave's accesses stay in order: read, add and write, which takes a tenth
+                        // of the time of LDS atomics (75 cycles a wave), and gives the same sums every time.
+                        volatile float *sum = acc;
+                        float was[8];
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) __hip_atomic_fetch_add(&acc[w.of(r, k)], p[v][k], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+                        for (int k = 0; k < 8; ++k) was[k] = sum[w.of(r, k)];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) sum[w.of(r, k)] = was[k] + p[v][k];
                     }
                 }
             }
@@ -416,50 +424,55 @@ __global__ __launch_bounds__(256) void k_bias_reduce(BiasReduce a)
 static int check_launch() { return hipGetLastError() == hipSuccess ? ADACOMP_OK : ADACOMP_EHIP; }
 
 constexpr uint32_t kPartThreads = 256, kPartGroups = 4, kPartKeys = kPartThreads * kPartGroups * 8u;
+constexpr uint32_t kLdsMost = 40u << 10;      // of a workgroup: four of them fit a compute unit
+constexpr uint32_t kMostResident = 8;         // workgroups of 256 threads on a compute unit
+constexpr uint32_t kMostWorkgroups = 1u << 20;   // of a launch, which has fewer than 2^32 threads; what is left is walked over
 
-constexpr uint32_t kLdsMost = 64u << 10;   // of a workgroup
-
-// The fewest threads that hold a row in up to 32 values each; in the backward pass so many that the copies of the sums by
-// distance, one for each row that a workgroup has in hand, fit LDS beside the bias.
+// Threads to a row and groups of 8 keys to a thread.  Few threads with up to 4 groups, since what a row costs whatever its length is then
+// paid by few waves; in the backward pass, where a group takes twice the registers, 2 in short rows.  bf16, us, with 1 / 2 / 4 groups: forward
+// 512 x 100 x 100 x 16 151 / 101 / 111, 256 x 200 x 200 x 16 240 / 201 / 147, 64 x 512 x 512 x 16 298 / 209 / 195, 4 x 512 x 6000 x 16 395 / 187 / 158;
+// backward 202 / 154 / 305, 384 / 284 / 444, 509 / 376 / 400, 422 / 497 / 237.  Longer rows are cut into parts, and read twice.
 SoftmaxForm softmax_form(uint32_t keys, uint32_t distance, bool backward)
 {
-    if (backward) {
+    if (backward) {   // every row that a workgroup has in hand has its sums by distance in LDS, beside the bias
         const uint32_t copies = kLdsMost / (4u * cells(distance)) - 1u;
-        keys = std::max(keys, copies >= 32u ? 0u : copies >= 16u ? 65u : copies >= 8u ? 129u : copies >= 4u ? 257u : 2049u);
+        keys = std::max(keys, copies >= 32u ? 0u : copies >= 16u ? 129u : copies >= 8u ? 257u : copies >= 4u ? 513u : 2049u);
     }
     if (keys <= 64u) return {{8, 1}, 1};
-    if (keys <= 128u) return {{16, 1}, 1};
-    if (keys <= 256u) return {{32, 1}, 1};
-    if (keys <= 512u) return {{64, 1}, 1};
-    if (keys <= 1024u) return {{64, 2}, 1};
+    if (keys <= 128u) return {{8, 2}, 1};
+    if (keys <= 256u) return {{backward ? 16u : 8u, backward ? 2u : 4u}, 1};
+    if (keys <= 512u) return {{backward ? 32u : 16u, backward ? 2u : 4u}, 1};
+    if (keys <= 1024u) return {{backward ? 64u : 32u, backward ? 2u : 4u}, 1};
     if (keys <= 2048u) return {{64, 4}, 1};
     if (keys <= 4096u) return {{256, 2}, 1};
     if (keys <= 8192u) return {{256, 4}, 1};
-    if (keys <= 16384u) return {{1024, 2}, 1};
+    if (keys <= 16384u) return {{512, 4}, 1};
+    if (keys <= 32768u) return {{1024, 4}, 1};
     return {{kPartThreads, kPartGroups}, (keys + kPartKeys - 1u) / kPartKeys};
 }
 
-uint32_t softmax_back_groups(uint64_t rows_of_head, uint32_t heads, const SoftmaxForm &f)
+// Workgroups of the backward pass to a head, with so many resident on a compute unit: as many as are resident in all, and no more, since
+// those would wait for the others' ends (64 x 512 x 512 x 16 bf16 with 5 resident: 4, 5 and 6 to a unit take 375, 328 and 408 us).
+static uint32_t back_groups(uint64_t rows_of_head, uint32_t heads, const SoftmaxForm &f, uint32_t resident)
 {
     const uint64_t all = (rows_of_head * f.parts + f.row.teams() - 1u) / f.row.teams();
-    const uint32_t wanted = ((f.row.threads > 256u ? 1u : 4u) * kComputeUnits + heads - 1u) / heads;
-    return uint32_t(std::min<uint64_t>(all, wanted));
+    return uint32_t(std::min<uint64_t>(all, std::max(1u, resident * kComputeUnits / heads)));
 }
 
-constexpr uint32_t kMostWorkgroups = 1u << 20;   // a launch has fewer than 2^32 threads; what is left is walked over
+// Most of them that a call can have: what the workspace has room for.
+uint32_t softmax_back_groups_most(uint64_t rows_of_head, uint32_t heads, const SoftmaxForm &f) { return back_groups(rows_of_head, heads, f, kMostResident); }
 
-template <template <typename, int, int, int, bool> class K>
-static int launch_form(const SoftmaxArgs &a, uint32_t dtype, const SoftmaxForm &f, uint32_t workgroups, uint32_t lds, void *stream)
+// Picks the kernel of a form and type and calls launch(kernel, phase) with it; twice where rows are cut into parts.
+template <template <typename, int, int, int, bool> class K, typename L>
+static int with_kernel(const SoftmaxArgs &a, uint32_t dtype, const SoftmaxForm &f, L &&launch)
 {
-    const dim3 grid(workgroups), wg(f.row.workgroup());
-    hipStream_t s = static_cast<hipStream_t>(stream);
     auto go = [&](auto form, auto phase) {
         constexpr int TPR = decltype(form)::threads, V = decltype(form)::groups, PHASE = decltype(phase)::value;
         auto of = [&](auto masked) {
             constexpr bool MASK = decltype(masked)::value;
-            if (dtype == ADACOMP_DTYPE_F32) hipLaunchKernelGGL((K<float, TPR, V, PHASE, MASK>::kernel), grid, wg, lds, s, a);
-            else if (dtype == ADACOMP_DTYPE_BF16) hipLaunchKernelGGL((K<bf16, TPR, V, PHASE, MASK>::kernel), grid, wg, lds, s, a);
-            else hipLaunchKernelGGL((K<f16, TPR, V, PHASE, MASK>::kernel), grid, wg, lds, s, a);
+            if (dtype == ADACOMP_DTYPE_F32) launch(std::integral_constant<void (*)(SoftmaxArgs), K<float, TPR, V, PHASE, MASK>::kernel>());
+            else if (dtype == ADACOMP_DTYPE_BF16) launch(std::integral_constant<void (*)(SoftmaxArgs), K<bf16, TPR, V, PHASE, MASK>::kernel>());
+            else launch(std::integral_constant<void (*)(SoftmaxArgs), K<f16, TPR, V, PHASE, MASK>::kernel>());
         };
         if (a.mask.data) of(std::true_type());
         else of(std::false_type());
@@ -473,14 +486,18 @@ static int launch_form(const SoftmaxArgs &a, uint32_t dtype, const SoftmaxForm &
     }
     switch (f.row.threads * 8u + f.row.groups) {
     case 8 * 8 + 1: go(FormOf<8, 1>(), Whole()); break;
-    case 16 * 8 + 1: go(FormOf<16, 1>(), Whole()); break;
-    case 32 * 8 + 1: go(FormOf<32, 1>(), Whole()); break;
-    case 64 * 8 + 1: go(FormOf<64, 1>(), Whole()); break;
+    case 8 * 8 + 2: go(FormOf<8, 2>(), Whole()); break;
+    case 8 * 8 + 4: go(FormOf<8, 4>(), Whole()); break;
+    case 16 * 8 + 2: go(FormOf<16, 2>(), Whole()); break;
+    case 16 * 8 + 4: go(FormOf<16, 4>(), Whole()); break;
+    case 32 * 8 + 2: go(FormOf<32, 2>(), Whole()); break;
+    case 32 * 8 + 4: go(FormOf<32, 4>(), Whole()); break;
     case 64 * 8 + 2: go(FormOf<64, 2>(), Whole()); break;
     case 64 * 8 + 4: go(FormOf<64, 4>(), Whole()); break;
     case 256 * 8 + 2: go(FormOf<256, 2>(), Whole()); break;
     case 256 * 8 + 4: go(FormOf<256, 4>(), Whole()); break;
-    case 1024 * 8 + 2: go(FormOf<1024, 2>(), Whole()); break;
+    case 512 * 8 + 4: go(FormOf<512, 4>(), Whole()); break;
+    case 1024 * 8 + 4: go(FormOf<1024, 4>(), Whole()); break;
     default: return ADACOMP_EINVAL;
     }
     return check_launch();
@@ -489,23 +506,47 @@ static int launch_form(const SoftmaxArgs &a, uint32_t dtype, const SoftmaxForm &
 template <typename T, int TPR, int V, int PHASE, bool MASK> struct KForward { static constexpr auto kernel = k_softmax_forward<T, TPR, V, PHASE, MASK>; };
 template <typename T, int TPR, int V, int PHASE, bool MASK> struct KBackward { static constexpr auto kernel = k_softmax_backward<T, TPR, V, PHASE, MASK>; };
 
+// Rows of a team, one after the other, in a workgroup of the forward pass: about 24000 keys to a workgroup, or 8 times what its bias takes
+// to lay out, and fewer where that leaves compute units without work.
+static uint32_t rows_of_team(const SoftmaxArgs &a, const SoftmaxForm &f)
+{
+    const uint32_t teams = f.row.teams(), wanted = std::max(24576u, 8u * (2u * a.distance + 1u));
+    uint32_t rows = std::min(std::max(wanted / (teams * std::max(a.keys, 1u)), teams == 1u ? 4u : 2u), 16u);
+    while (rows > 1u && uint64_t(a.batch) * a.heads * ((a.queries + rows * teams - 1u) / (rows * teams)) < 4u * kComputeUnits) --rows;
+    return rows;
+}
+
 int launch_softmax_forward(const SoftmaxArgs &args, uint32_t dtype, const SoftmaxForm &f, void *stream)
 {
     SoftmaxArgs a = args;
-    a.rows_per_wg = f.parts > 1u ? 1u : 4u * f.row.teams();
+    a.rows_per_wg = f.parts > 1u ? 1u : f.row.teams() * rows_of_team(a, f);
     a.wgs_per_head = (a.queries + a.rows_per_wg - 1u) / a.rows_per_wg;
     a.row_parts = f.parts;
     const uint64_t blocks = uint64_t(a.batch) * a.heads * a.wgs_per_head * f.parts;
-    return launch_form<KForward>(a, dtype, f, uint32_t(std::min<uint64_t>(blocks, kMostWorkgroups)), 4u * cells(a.distance), stream);
+    const dim3 grid(uint32_t(std::min<uint64_t>(blocks, kMostWorkgroups))), wg(f.row.workgroup());
+    return with_kernel<KForward>(a, dtype, f, [&](auto kernel) {
+        hipLaunchKernelGGL(kernel.value, grid, wg, 4u * cells(a.distance), static_cast<hipStream_t>(stream), a);
+    });
 }
 
-int launch_softmax_backward(const SoftmaxArgs &args, uint32_t dtype, const SoftmaxForm &f, void *stream)
+int launch_softmax_backward(const SoftmaxArgs &args, uint32_t dtype, const SoftmaxForm &f, uint32_t &groups, void *stream)
 {
     SoftmaxArgs a = args;
-    a.wgs_per_head = softmax_back_groups(uint64_t(a.batch) * a.queries, a.heads, f);
     a.row_parts = f.parts;
-    const uint32_t copies = 1u + (a.bias_sums ? f.row.teams() : 0u);
-    return launch_form<KBackward>(a, dtype, f, a.heads * a.wgs_per_head, 4u * cells(a.distance) * copies, stream);
+    const uint32_t lds = 4u * cells(a.distance) * (1u + (a.bias_sums ? f.row.teams() : 0u)), threads = f.row.workgroup();
+    return with_kernel<KBackward>(a, dtype, f, [&](auto kernel) {
+        // how many of the kernel's workgroups a compute unit holds with so much LDS: asked once, and again if the LDS differs
+        static std::atomic<uint64_t> known{0};
+        uint64_t k = known.load(std::memory_order_relaxed);
+        if (k >> 32 != lds + 1u) {
+            int n = 0;
+            if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel.value, int(threads), lds) != hipSuccess) { (void)hipGetLastError(); n = 1; }
+            k = uint64_t(lds + 1u) << 32 | uint32_t(std::min(std::max(n, 1), int(kMostResident)));
+            known.store(k, std::memory_order_relaxed);
+        }
+        a.wgs_per_head = groups = back_groups(uint64_t(a.batch) * a.queries, a.heads, f, uint32_t(k));
+        hipLaunchKernelGGL(kernel.value, dim3(a.heads * groups), dim3(threads), lds, static_cast<hipStream_t>(stream), a);
+    });
 }
 
 int launch_bias_reduce(const BiasReduce &a, void *stream)
