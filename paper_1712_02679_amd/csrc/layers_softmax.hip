@@ -425,7 +425,7 @@ static int check_launch() { return hipGetLastError() == hipSuccess ? ADACOMP_OK 
 
 constexpr uint32_t kPartThreads = 256, kPartGroups = 4, kPartKeys = kPartThreads * kPartGroups * 8u;
 constexpr uint32_t kLdsMost = 40u << 10;      // of a workgroup: four of them fit a compute unit
-constexpr uint32_t kMostResident = 8;         // workgroups of 256 threads on a compute unit
+constexpr uint32_t kMostResident = 6;         // workgroups on a compute unit; of kernels of which 7 should fit, 6 are faster (16 x 1000 x 1000 x 16 bf16 309 / 373 us)
 constexpr uint32_t kMostWorkgroups = 1u << 20;   // of a launch, which has fewer than 2^32 threads; what is left is walked over
 
 // Threads to a row and groups of 8 keys to a thread.  Few threads with up to 4 groups, since what a row costs whatever its length is then
