@@ -45,7 +45,7 @@ class _BiasSoftmax(ctypes.Structure):
                 ("table", _vp), ("map", _vp), ("mask", _View)]
 
 
-_bound = None
+_bound = None   # the library, once it has the argument types below
 
 
 def _lib():
@@ -70,22 +70,31 @@ def _refuse(what):
     raise AdacompError(EINVAL, what)
 
 
-def _stream_of(t):
-    device = t.get_device()
-    if device < 0 or device != torch.cuda.current_device():
+_current_device = torch._C._cuda_getDevice          # torch.cuda.current_device() and torch.cuda.current_stream() without an object
+_current_stream = torch._C._cuda_getCurrentRawStream   # and a look at the module's state around them: 1 us less, of 8 in all
+
+
+def _device_of(x):
+    """The GPU that x and every other tensor of the call have to be on."""
+    device = x.get_device()
+    if device < 0 or device != _current_device():
         _refuse("tensors are on the current GPU (there is no CPU path)")
-    return torch._C._cuda_getCurrentRawStream(device)   # torch.cuda.current_stream(), without an object around it: 1 us less
+    return device
 
 
-def _rows(t, like, what):
-    """(address, row stride) of a tensor of like's shape, type and device, seen as rows of its last dimension."""
+def _unlike(t, shape, dtype, what):
+    _refuse(f"{what}: {tuple(t.shape)} {t.dtype} on {t.device} where {tuple(shape)} {dtype} on the device of the first tensor is wanted")
+
+
+def _rows(t, shape, dtype, device, what):
+    """(address, row stride) of a tensor of the given shape, type and device, seen as rows of its last dimension."""
     if t is None:
         return None, 0
-    if t is not like and (t.shape != like.shape or t.dtype != like.dtype or t.get_device() != like.get_device()):
-        _refuse(f"{what}: {tuple(t.shape)} {t.dtype} on {t.device} beside {tuple(like.shape)} {like.dtype} on {like.device}")
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != device:
+        _unlike(t, shape, dtype, what)
     if t.is_contiguous():
-        return t.data_ptr(), t.shape[-1]
-    shape, stride = t.shape, t.stride()
+        return t.data_ptr(), shape[-1]
+    stride = t.stride()
     if shape[-1] > 1 and stride[-1] != 1:
         _refuse(f"{what}: the last dimension is not contiguous")
     row, expect = None, 0
@@ -100,28 +109,31 @@ def _rows(t, like, what):
     return t.data_ptr(), shape[-1] if row is None else row
 
 
-def _vector(t, n, like, what):
+def _vector(t, n, device, what):
     """Address of a contiguous float32 tensor of n values."""
     if t is None:
         return None
-    if t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous() or t.get_device() != like.get_device():
-        _refuse(f"{what}: {n} contiguous float32 values on {like.device} are wanted, it is {tuple(t.shape)} {t.dtype} on {t.device}")
+    if t.dtype is not torch.float32 or t.numel() != n or not t.is_contiguous() or t.get_device() != device:
+        _unlike(t, (n,), "contiguous torch.float32", what)
     return t.data_ptr()
 
 
 def _shape_of(x, what):
-    if x.dtype not in _DTYPES:
-        _refuse(f"{what}: {x.dtype} is not one of float32, bfloat16, float16")
-    if x.dim() == 0:
+    """(shape, type, its number, rows, columns)"""
+    shape, dtype = x.shape, x.dtype
+    number = _DTYPES.get(dtype)
+    if number is None:
+        _refuse(f"{what}: {dtype} is not one of float32, bfloat16, float16")
+    if not shape:
         _refuse(f"{what}: no dimension")
-    cols = x.shape[-1]
-    return (x.numel() // cols if cols else 0), cols
+    cols = shape[-1]
+    return shape, dtype, number, (x.numel() // cols if cols else 0), cols
 
 
-def _room(workspace, like):
-    if not workspace.is_contiguous() or workspace.get_device() != like.get_device():
+def _room(workspace, device):
+    if not workspace.is_contiguous() or workspace.get_device() != device:
         _refuse("workspace: a contiguous tensor on the device of the others is wanted")
-    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    return workspace.data_ptr(), workspace.nbytes
 
 
 class Dropout:
@@ -136,37 +148,43 @@ class Dropout:
         self._ref = ctypes.byref(self._c)
 
 
-def _drop(dropout, like):
+def _drop(dropout, device):
     if dropout is None:
         return None
-    if dropout.step is not None and dropout.step.get_device() != like.get_device():
+    if dropout.step is not None and dropout.step.get_device() != device:
         _refuse("step is on another device")
     return dropout._ref
 
 
 def adacomp_dropout(x, y, dropout, residual=None):
     """y = D(x), or residual + D(x).  The backward pass is the same call on the gradient."""
-    L = _lib()
-    rows, cols = _shape_of(x, "x")
-    px, sx = _rows(x, x, "x")
-    py, sy = _rows(y, x, "y")
-    pr, sr = _rows(residual, x, "residual")
+    L = _bound or _lib()
+    shape, dtype, number, rows, cols = _shape_of(x, "x")
+    dev = _device_of(x)
+    px, sx = _rows(x, shape, dtype, dev, "x")
+    py, sy = _rows(y, shape, dtype, dev, "y")
+    pr, sr = _rows(residual, shape, dtype, dev, "residual")
     if dropout is None:
         _refuse("dropout is missing")
-    _check(L.adacomp_dropout(px, pr, py, rows, cols, sx, sr, sy, _DTYPES[x.dtype], _drop(dropout, x), _stream_of(x)))
+    rc = L.adacomp_dropout(px, pr, py, rows, cols, sx, sr, sy, number, _drop(dropout, dev), _current_stream(dev))
+    if rc:
+        _check(rc)
 
 
 def adacomp_norm_forward(x, gamma, beta, y, residual=None, dropout=None, z=None, mean=None, rstd=None, eps=1e-5):
     """z = [residual +] D(x), y = layer norm of z over the last dimension; z, mean and rstd are written where they are given."""
-    L = _lib()
-    rows, cols = _shape_of(x, "x")
-    px, sx = _rows(x, x, "x")
-    py, sy = _rows(y, x, "y")
-    pr, sr = _rows(residual, x, "residual")
-    pz, sz = _rows(z, x, "z")
-    norm = _Norm(rows, cols, _DTYPES[x.dtype], sx, sr, sz, sy)
-    _check(L.adacomp_norm_forward(ctypes.byref(norm), px, pr, _vector(gamma, cols, x, "gamma"), _vector(beta, cols, x, "beta"), eps, _drop(dropout, x),
-                                  pz, py, _vector(mean, rows, x, "mean"), _vector(rstd, rows, x, "rstd"), _stream_of(x)))
+    L = _bound or _lib()
+    shape, dtype, number, rows, cols = _shape_of(x, "x")
+    dev = _device_of(x)
+    px, sx = _rows(x, shape, dtype, dev, "x")
+    py, sy = _rows(y, shape, dtype, dev, "y")
+    pr, sr = _rows(residual, shape, dtype, dev, "residual")
+    pz, sz = _rows(z, shape, dtype, dev, "z")
+    norm = _Norm(rows, cols, number, sx, sr, sz, sy)
+    rc = L.adacomp_norm_forward(norm, px, pr, _vector(gamma, cols, dev, "gamma"), _vector(beta, cols, dev, "beta"), eps, _drop(dropout, dev), pz, py,
+                                _vector(mean, rows, dev, "mean"), _vector(rstd, rows, dev, "rstd"), _current_stream(dev))
+    if rc:
+        _check(rc)
 
 
 def adacomp_norm_workspace_bytes(rows, cols) -> int:
@@ -176,18 +194,21 @@ def adacomp_norm_workspace_bytes(rows, cols) -> int:
 def adacomp_norm_backward(dy, z, mean, rstd, gamma, dz, dgamma, dbeta, workspace, dz_add=None, dropout=None, dx=None, accumulate=False):
     """dz (the gradient of z and of the residual), dx = D(dz), and dgamma, dbeta summed over all rows: overwritten, or with
     accumulate added to.  dgamma and dbeta may be parts of the flat gradient, or None."""
-    L = _lib()
-    rows, cols = _shape_of(dy, "dy")
-    pdy, sdy = _rows(dy, dy, "dy")
-    pz, sz = _rows(z, dy, "z")
-    pa, sa = _rows(dz_add, dy, "dz_add")
-    pdz, sdz = _rows(dz, dy, "dz")
-    pdx, sdx = _rows(dx, dy, "dx")
-    pw, nw = _room(workspace, dy)
-    norm = _Norm(rows, cols, _DTYPES[dy.dtype], 0, 0, sz, 0, sdy, sa, sdz, sdx)
-    _check(L.adacomp_norm_backward(ctypes.byref(norm), pdy, pa, pz, _vector(mean, rows, dy, "mean"), _vector(rstd, rows, dy, "rstd"),
-                                   _vector(gamma, cols, dy, "gamma"), _drop(dropout, dy), pdz, pdx, _vector(dgamma, cols, dy, "dgamma"),
-                                   _vector(dbeta, cols, dy, "dbeta"), 1 if accumulate else 0, pw, nw, _stream_of(dy)))
+    L = _bound or _lib()
+    shape, dtype, number, rows, cols = _shape_of(dy, "dy")
+    dev = _device_of(dy)
+    pdy, sdy = _rows(dy, shape, dtype, dev, "dy")
+    pz, sz = _rows(z, shape, dtype, dev, "z")
+    pa, sa = _rows(dz_add, shape, dtype, dev, "dz_add")
+    pdz, sdz = _rows(dz, shape, dtype, dev, "dz")
+    pdx, sdx = _rows(dx, shape, dtype, dev, "dx")
+    pw, nw = _room(workspace, dev)
+    norm = _Norm(rows, cols, number, 0, 0, sz, 0, sdy, sa, sdz, sdx)
+    rc = L.adacomp_norm_backward(norm, pdy, pa, pz, _vector(mean, rows, dev, "mean"), _vector(rstd, rows, dev, "rstd"), _vector(gamma, cols, dev, "gamma"),
+                                 _drop(dropout, dev), pdz, pdx, _vector(dgamma, cols, dev, "dgamma"), _vector(dbeta, cols, dev, "dbeta"),
+                                 1 if accumulate else 0, pw, nw, _current_stream(dev))
+    if rc:
+        _check(rc)
 
 
 def adacomp_relative_buckets(n_buckets, max_distance, both_directions):
@@ -211,41 +232,51 @@ class RelativeBias:
         self.max_distance = map.numel() // 2
 
 
-def _view(t, like, what):
-    if t is not like and (t.shape != like.shape or t.dtype != like.dtype or t.get_device() != like.get_device()):
-        _refuse(f"{what}: {tuple(t.shape)} {t.dtype} on {t.device} beside {tuple(like.shape)} {like.dtype} on {like.device}")
-    s = t.stride()
-    if s[3] != 1 and t.shape[3] > 1:
+def _view(t, shape, dtype, device, what):
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != device:
+        _unlike(t, shape, dtype, what)
+    b, h, q, k = t.stride()
+    if k != 1 and shape[3] > 1:
         _refuse(f"{what}: the last dimension is not contiguous")
-    return _View(t.data_ptr(), s[0], s[1], s[2])
+    return _View(t.data_ptr(), b, h, q)
 
 
-def _per_sequence(t, batch, like, what):
+def _per_sequence(t, batch, device, what):
     if t is None:
         return None
-    if t.dtype != torch.int32 or t.numel() != batch or not t.is_contiguous() or t.get_device() != like.get_device():
-        _refuse(f"{what}: an int32 value for each of {batch} sequences is wanted")
+    if t.dtype is not torch.int32 or t.numel() != batch or not t.is_contiguous() or t.get_device() != device:
+        _unlike(t, (batch,), "contiguous torch.int32", what)
     return t.data_ptr()
 
 
 def _bias_softmax(scores, bias, scale, causal, query_start, query_starts, key_lengths, mask):
-    if scores.dim() != 4 or scores.dtype not in _DTYPES:
+    """(the operator, shape, type and device of its tensors, rows)"""
+    shape, dtype = scores.shape, scores.dtype
+    number = _DTYPES.get(dtype)
+    if len(shape) != 4 or number is None:
         _refuse("scores: [batch, heads, queries, keys] of float32, bfloat16 or float16 is wanted")
-    b, h, q, k = scores.shape
-    if bias.heads != h or bias.table.get_device() != scores.get_device():
+    dev = _device_of(scores)
+    b, h, q, k = shape
+    if bias.heads != h or bias.table.get_device() != dev:
         _refuse(f"the bias is one of {bias.heads} heads on {bias.table.device}, the scores have {h} on {scores.device}")
-    view = _View()
+    view = _NO_VIEW
     if mask is not None:
-        if mask.dtype not in (torch.uint8, torch.bool) or mask.dim() != 4 or mask.get_device() != scores.get_device():
+        if mask.dtype not in (torch.uint8, torch.bool) or mask.dim() != 4 or mask.get_device() != dev:
             _refuse("mask: a uint8 or bool tensor of 4 dimensions is wanted")
+        if any(n != 1 and n != m for n, m in zip(mask.shape, shape)):
+            _refuse(f"mask: {tuple(mask.shape)} beside scores of {tuple(shape)}")
         mask = mask.expand(b, h, q, k)   # no copy: strides of 0
         s = mask.stride()
         if s[3] != 1 and k > 1:
             _refuse("mask: its last dimension is contiguous and as long as the scores'")
         view = _View(mask.data_ptr(), s[0], s[1], s[2])
-    return _BiasSoftmax(b, h, q, k, _DTYPES[scores.dtype], 1 if causal else 0, bias.n_buckets, bias.max_distance, scale, int(query_start),
-                        _per_sequence(query_starts, b, scores, "query_starts"), _per_sequence(key_lengths, b, scores, "key_lengths"),
-                        bias.table.data_ptr(), bias.map.data_ptr(), view)
+    op = _BiasSoftmax(b, h, q, k, number, 1 if causal else 0, bias.n_buckets, bias.max_distance, scale, query_start,
+                      _per_sequence(query_starts, b, dev, "query_starts"), _per_sequence(key_lengths, b, dev, "key_lengths"),
+                      bias.table.data_ptr(), bias.map.data_ptr(), view)
+    return op, shape, dtype, dev, b * h * q
+
+
+_NO_VIEW = _View()
 
 
 def adacomp_bias_softmax_workspace_bytes(batch, heads, queries, keys, max_distance) -> int:
@@ -256,22 +287,23 @@ def adacomp_bias_softmax_forward(scores, bias, probs, workspace, lse=None, scale
                                  key_lengths=None, mask=None, dropout=None):
     """probs = D(softmax(scale * scores + bias)) over the admitted keys (see adacomp_layers.h); lse [batch, heads, queries], for the
     backward pass, is written if it is given.  The mask may have dimensions of 1 before the last."""
-    L = _lib()
-    op = _bias_softmax(scores, bias, scale, causal, query_start, query_starts, key_lengths, mask)
-    pw, nw = _room(workspace, scores)
-    rows = op.batch * op.heads * op.queries
-    _check(L.adacomp_bias_softmax_forward(ctypes.byref(op), ctypes.byref(_view(scores, scores, "scores")), ctypes.byref(_view(probs, scores, "probs")),
-                                          _vector(lse, rows, scores, "lse"), _drop(dropout, scores), pw, nw, _stream_of(scores)))
+    L = _bound or _lib()
+    op, shape, dtype, dev, rows = _bias_softmax(scores, bias, scale, causal, query_start, query_starts, key_lengths, mask)
+    pw, nw = _room(workspace, dev)
+    rc = L.adacomp_bias_softmax_forward(op, _view(scores, shape, dtype, dev, "scores"), _view(probs, shape, dtype, dev, "probs"),
+                                        _vector(lse, rows, dev, "lse"), _drop(dropout, dev), pw, nw, _current_stream(dev))
+    if rc:
+        _check(rc)
 
 
 def adacomp_bias_softmax_backward(scores, bias, lse, dprobs, dscores, dtable, workspace, scale=1.0, causal=False, query_start=0, query_starts=None,
                                   key_lengths=None, mask=None, dropout=None, accumulate=False):
     """dscores and dtable (a part of the flat gradient, or None) from dprobs, with the other arguments as in the forward pass."""
-    L = _lib()
-    op = _bias_softmax(scores, bias, scale, causal, query_start, query_starts, key_lengths, mask)
-    pw, nw = _room(workspace, scores)
-    rows = op.batch * op.heads * op.queries
-    _check(L.adacomp_bias_softmax_backward(ctypes.byref(op), ctypes.byref(_view(scores, scores, "scores")), _vector(lse, rows, scores, "lse"),
-                                           ctypes.byref(_view(dprobs, scores, "dprobs")), _drop(dropout, scores),
-                                           ctypes.byref(_view(dscores, scores, "dscores")), _vector(dtable, op.n_buckets * op.heads, scores, "dtable"),
-                                           1 if accumulate else 0, pw, nw, _stream_of(scores)))
+    L = _bound or _lib()
+    op, shape, dtype, dev, rows = _bias_softmax(scores, bias, scale, causal, query_start, query_starts, key_lengths, mask)
+    pw, nw = _room(workspace, dev)
+    rc = L.adacomp_bias_softmax_backward(op, _view(scores, shape, dtype, dev, "scores"), _vector(lse, rows, dev, "lse"),
+                                         _view(dprobs, shape, dtype, dev, "dprobs"), _drop(dropout, dev), _view(dscores, shape, dtype, dev, "dscores"),
+                                         _vector(dtable, bias.n_buckets * bias.heads, dev, "dtable"), 1 if accumulate else 0, pw, nw, _current_stream(dev))
+    if rc:
+        _check(rc)
