@@ -378,39 +378,45 @@ template <typename T, int TPR, int V, int PHASE, bool MASK> __global__ __launch_
     }
 }
 
-// A workgroup to a head and bucket: it lists the distances that have the bucket, and adds up what the backward pass's workgroups
-// have for them, always in the same order.
+// A workgroup to a head and bucket: its first wave lists the distances that have the bucket, and all add up what the backward pass's
+// workgroups have for them, always in the same order.
 __global__ __launch_bounds__(256) void k_bias_reduce(BiasReduce a)
 {
     extern __shared__ uint16_t mine[];   // [2 D + 1]
     __shared__ float room[4];
-    __shared__ uint32_t counts[4];
-    const uint32_t n = 2u * a.distance + 1u, lane = threadIdx.x % 64u, wave = threadIdx.x / 64u;
-    const uint32_t h = blockIdx.x, bucket = blockIdx.y;
-    uint32_t found = 0;
-    for (uint32_t x0 = 0; x0 < n; x0 += 256u) {
-        const uint32_t x = x0 + threadIdx.x;
-        const bool hit = x < n && uint32_t(min(max(a.map[x], 0), int32_t(a.n_buckets) - 1)) == bucket;
-        const uint64_t hits = __ballot(hit);
-        if (lane == 0u) counts[wave] = uint32_t(__popcll(hits));
-        __syncthreads();
-        uint32_t before = found;
-        for (uint32_t w = 0; w < 4u; ++w) {
-            if (w < wave) before += counts[w];
-            found += counts[w];
+    __shared__ uint32_t found_room;
+    constexpr uint32_t AHEAD = 8;        // loads on their way
+    const uint32_t n = 2u * a.distance + 1u, h = blockIdx.x, bucket = blockIdx.y;
+    if (threadIdx.x < 64u) {
+        const uint32_t lane = threadIdx.x;
+        uint32_t found = 0;
+        for (uint32_t x0 = 0; x0 < n; x0 += 64u * AHEAD) {
+            int32_t b[AHEAD];
+#pragma unroll
+            for (uint32_t u = 0; u < AHEAD; ++u) b[u] = x0 + u * 64u + lane < n ? min(max(a.map[x0 + u * 64u + lane], 0), int32_t(a.n_buckets) - 1) : -1;
+#pragma unroll
+            for (uint32_t u = 0; u < AHEAD; ++u) {
+                const bool hit = b[u] == int32_t(bucket);
+                const uint64_t hits = __ballot(hit);
+                if (hit) mine[found + uint32_t(__popcll(hits & ((uint64_t(1) << lane) - 1u)))] = uint16_t(x0 + u * 64u + lane);
+                found += uint32_t(__popcll(hits));
+            }
         }
-        if (hit) mine[before + uint32_t(__popcll(hits & ((uint64_t(1) << lane) - 1u)))] = uint16_t(x);
-        __syncthreads();
+        if (lane == 0u) found_room = found;
     }
+    __syncthreads();
+    const uint32_t found = found_room, items = found * a.groups;   // below 4097 * 6 * 256
     const float *from = a.bias_sums + uint64_t(h) * a.groups * n;
     float e = 0.f;
-    if (found != 0u) {
-        const uint32_t items = found * a.groups;   // below 4097 * 1024
-#pragma unroll 4
-        for (uint32_t i = threadIdx.x; i < items; i += 256u) {
-            const uint32_t g = i / found;
-            e += from[uint64_t(g) * n + mine[i - g * found]];
+    for (uint32_t i0 = threadIdx.x; i0 < items; i0 += 256u * AHEAD) {
+        float part[AHEAD];
+#pragma unroll
+        for (uint32_t u = 0; u < AHEAD; ++u) {
+            const uint32_t i = min(i0 + u * 256u, items - 1u), g = i / found;
+            part[u] = from[uint64_t(g) * n + mine[i - g * found]];
         }
+#pragma unroll
+        for (uint32_t u = 0; u < AHEAD; ++u) e += i0 + u * 256u < items ? part[u] : 0.f;
     }
     e = over_waves<Add, 4>(over_lanes<Add, 64>(e), room);
     if (threadIdx.x == 0u) {
