@@ -30,9 +30,13 @@ template <typename T> __device__ __forceinline__ T *at(T *row, uint32_t col)
 template <typename T> __device__ __forceinline__ raw8<T> load8(const T *p) { return *reinterpret_cast<const typename Raw<T>::at *>(p); }
 template <typename T> __device__ __forceinline__ raw8<T> narrow(f32x8 x) { return __builtin_convertvector(x, raw8<T>); }
 template <typename T> __device__ __forceinline__ raw8<T> load8_once(const T *p) { return __builtin_nontemporal_load(reinterpret_cast<const typename Raw<T>::at *>(p)); }
-// Past the caches of the XCD, whose contents a kernel's end writes out in any case: 2 to 12 % of every call (16384 x 4096 bf16, us: residual sum
-// 70.9 / 68.3, norm 99.8 / 97.0, backward 127.5 / 122.2; 2000 x 4096 norm 13.5 / 11.6; softmax 4 x 16 x 2048 x 2048 171 / 165, backward 306 / 296).
-template <typename T> __device__ __forceinline__ void store8(T *p, f32x8 x) { __builtin_nontemporal_store(narrow<T>(x), reinterpret_cast<typename Raw<T>::at *>(p)); }
+template <typename T> __device__ __forceinline__ void store8(T *p, f32x8 x) { *reinterpret_cast<typename Raw<T>::at *>(p) = narrow<T>(x); }
+// Past the caches of the XCD, whose contents a kernel's end writes out in any case: for 16-bit values of which a wave stores neighbouring
+// ones, where every line is written whole (16384 x 4096 bf16, us: residual sum 70.9 / 68.3, norm 99.8 / 97.0, backward 127.5 / 122.2; softmax
+// 4 x 16 x 2048 x 2048 171 / 165, backward 306 / 296).  Two stores for 8 32-bit values, and rows that a part of a wave stores, write halves
+// of lines: they lose where memory is what bounds (backward norm f32 255 / 291, backward softmax f32 4 x 16 x 2048 x 2048 579 / 613, bf16 512 x 16 x 100 x 100 153 / 182), and
+// 32-bit ones win in calls that the memory-side cache holds (norm f32 6007 x 577 9.7 / 8.8, backward 16.3 / 15.5).
+template <typename T> __device__ __forceinline__ void store8_past(T *p, f32x8 x) { __builtin_nontemporal_store(narrow<T>(x), reinterpret_cast<typename Raw<T>::at *>(p)); }
 
 // The first n of 8 values, 0 < n < 8, zeros behind them.
 template <typename T> __device__ __forceinline__ raw8<T> load_some(const T *p, uint32_t n)
@@ -69,7 +73,8 @@ __device__ __forceinline__ f32x8 shifted(f32x8 x, uint32_t n)
 // The groups of a row that a thread has: group t + v TPR in round v, `cols` columns in all.  A row whose length is no multiple of 8 ends
 // with an incomplete group.  Its thread reads the row's last 8 values instead, and moves them into place when it uses them: reading values
 // one by one would make the wave wait for them there and then, and with them for everything that is on its way.
-template <typename T, int TPR, int V> struct RowGroups {
+// PAST: results go past the caches (store8_past) where a wave stores neighbouring groups.
+template <typename T, int TPR, int V, bool PAST = sizeof(T) == 2> struct RowGroups {
     static constexpr bool kShort = TPR == 8;   // rows of less than 8 values come to the form with the fewest threads
     uint32_t t, cols, first;   // first: column of the part of the row that the threads hold
     __device__ __forceinline__ uint32_t col(int v) const { return first + (t + uint32_t(v) * TPR) * 8u; }
@@ -116,9 +121,14 @@ template <typename T, int TPR, int V> struct RowGroups {
         }
         return x;
     }
+    static __device__ __forceinline__ void store_whole(T *p, f32x8 x)
+    {
+        if constexpr (TPR >= 64 && PAST) store8_past(p, x);
+        else store8(p, x);
+    }
     __device__ __forceinline__ void store_round(T *row, int v, f32x8 x) const
     {
-        if (whole(v)) store8(at(row, col(v)), x);
+        if (whole(v)) store_whole(at(row, col(v)), x);
         else if (col(v) < cols) store_some(at(row, col(v)), cols % 8u, x);
     }
     // x(v) of every round, to its place
@@ -130,7 +140,7 @@ template <typename T, int TPR, int V> struct RowGroups {
         for (int v = 0; v < V; ++v) {
             if (col(v) < cols) {
                 const f32x8 y = x(v);
-                if (whole(v)) store8(at(row, col(v)), y);
+                if (whole(v)) store_whole(at(row, col(v)), y);
                 else { some = y; mine = true; }
             }
         }

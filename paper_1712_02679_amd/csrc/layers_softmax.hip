@@ -12,7 +12,7 @@
 
 namespace adacomp {
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLog2e = 1.4426950408889634f, kLog2eRest = float(1.4426950408889634 - double(kLog2e)), kLn2 = 0.6931471805599453f;
 constexpr float kInf = __builtin_huge_valf();
 
 // The bias by distance index x = key - query + D, and the sums of its gradient, lie in LDS with 8 more places at either end, so that a
@@ -22,13 +22,31 @@ constexpr uint32_t kGuard = 8;
 __host__ __device__ constexpr uint32_t cell(uint32_t X) { return X + (X >> 3); }
 __host__ __device__ constexpr uint32_t cells(uint32_t distance) { return (cell(2u * distance + 2u * kGuard) + 3u) & ~3u; }
 
-// A workgroup's copy of its head's bias, times log2(e).
-__device__ __forceinline__ void stage_bias(float *bias, const SoftmaxArgs &a, uint32_t head)
+// What exponents are made of.  16-bit tensors: everything in units of log2, one v_exp_f32 a value, whose argument has been rounded
+// where it is about 10: 5e-7 of the result at most, far below their own rounding.  32-bit ones: natural units, as in the formula, and the
+// rounding of the product with log2(e) is made good to first order (softmax_back_odd_777's values: 3.1e-7 -> 2e-7 off).
+template <typename T> struct Unit {
+    static constexpr bool kNatural = sizeof(T) == 4;
+    static __device__ __forceinline__ float scale(const SoftmaxArgs &a) { return kNatural ? a.scale : a.scale2; }
+    static __device__ __forceinline__ float from_natural(float x) { return kNatural ? x : x * kLog2e; }
+    static __device__ __forceinline__ float exp(float x)
+    {
+        if constexpr (!kNatural) return __builtin_amdgcn_exp2f(x);
+        const float y = x * kLog2e;
+        const float off = fabsf(x) < 200.f ? fmaf(x, kLog2e, -y) + x * kLog2eRest : 0.f;   // infinities have none
+        const float p = __builtin_amdgcn_exp2f(y);
+        return fmaf(p, off * kLn2, p);
+    }
+    static __device__ __forceinline__ float lse(float top, float total) { return kNatural ? top + logf(total) : (top + log2f(total)) * kLn2; }
+};
+
+// A workgroup's copy of its head's bias.
+template <typename T> __device__ __forceinline__ void stage_bias(float *bias, const SoftmaxArgs &a, uint32_t head)
 {
     const int last = 2 * int(a.distance);
     for (int X = threadIdx.x; X <= last + 2 * int(kGuard) - 1; X += blockDim.x) {
         const int32_t b = min(max(a.map[min(max(X - int(kGuard), 0), last)], 0), int32_t(a.n_buckets) - 1);
-        bias[cell(X)] = a.table[uint64_t(b) * a.heads + head] * kLog2e;
+        bias[cell(X)] = Unit<T>::from_natural(a.table[uint64_t(b) * a.heads + head]);
     }
 }
 
@@ -88,18 +106,18 @@ template <typename G> __device__ __forceinline__ uint64_t mask_of(const G &group
     return groups.ends_in(v) && !(G::kShort && groups.cols < 8u) && groups.ends_here() ? m >> 8u * (8u - groups.cols % 8u) : m;
 }
 
-// scale2 * s + bias - less of 8 keys.
-__device__ __forceinline__ f32x8 biased8(f32x8 s, const SoftmaxArgs &a, const Row &r, const Window &w, const float *bias, float low, float high, float less)
+// scale * s + bias - less of 8 keys.
+__device__ __forceinline__ f32x8 biased8(f32x8 s, const SoftmaxArgs &a, float scale, const Row &r, const Window &w, const float *bias, float low, float high, float less)
 {
     f32x8 t;
     const int last = 2 * int(a.distance);
     if (w.above(last) || w.below()) {
         const float b = (w.below() ? low : high) - less;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) t[k] = fmaf(s[k], a.scale2, b);
+        for (int k = 0; k < 8; ++k) t[k] = fmaf(s[k], scale, b);
     } else {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) t[k] = fmaf(s[k], a.scale2, bias[w.of(r, k)] - less);
+        for (int k = 0; k < 8; ++k) t[k] = fmaf(s[k], scale, bias[w.of(r, k)] - less);
     }
     return t;
 }
@@ -138,7 +156,7 @@ template <typename T, int TPR, int V, int PHASE, bool MASK> __global__ __launch_
         };
         if (first + team < end) fetch(first + team);
         if (block != blockIdx.x) __syncthreads();   // the rows before are done with the bias
-        stage_bias(bias, a, h);
+        stage_bias<T>(bias, a, h);
         __syncthreads();
         const float low = bias[0], high = bias[cell(2u * a.distance + kGuard)];
         for (uint32_t i = first + team; i < end; i += TEAMS) {
@@ -155,7 +173,7 @@ template <typename T, int TPR, int V, int PHASE, bool MASK> __global__ __launch_
                 if (n > 0) {
                     const uint32_t here = admitted8<MASK>(MASK ? mask_of(groups, mask[v], v) : 0, n);
                     bits |= here << (8 * v);
-                    p[v] = biased8(groups.values(raw[v], v), a, r, Window(r, j), bias, low, high, 0.f);
+                    p[v] = biased8(groups.values(raw[v], v), a, Unit<T>::scale(a), r, Window(r, j), bias, low, high, 0.f);
                     if (here != 0xFFu) {
 #pragma unroll
                         for (int k = 0; k < 8; ++k) p[v][k] = here >> k & 1u ? p[v][k] : -kInf;
@@ -174,7 +192,7 @@ template <typename T, int TPR, int V, int PHASE, bool MASK> __global__ __launch_
                 if (bits >> (8 * v) & 0xFFu) {
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
-                        p[v][k] = __builtin_amdgcn_exp2f(p[v][k] - from);
+                        p[v][k] = Unit<T>::exp(p[v][k] - from);
                         l += p[v][k];
                     }
                 }
@@ -189,7 +207,7 @@ template <typename T, int TPR, int V, int PHASE, bool MASK> __global__ __launch_
                 const float from_top = top == -kInf ? 0.f : top;
                 total = 0.f;
 #pragma unroll
-                for (int w = 0; w < TPR / 64; ++w) total = fmaf(room[turn][1][w], __builtin_amdgcn_exp2f(room[turn][0][w] - from_top), total);
+                for (int w = 0; w < TPR / 64; ++w) total = fmaf(room[turn][1][w], Unit<T>::exp(room[turn][0][w] - from_top), total);
                 turn ^= 1u;
             }
             const uint64_t row = uint64_t(bh) * a.queries + i;
@@ -207,11 +225,11 @@ template <typename T, int TPR, int V, int PHASE, bool MASK> __global__ __launch_
                 for (uint32_t q = 0; q < a.row_parts; ++q) top = fmaxf(top, of[2u * q]);
                 const float from_top = top == -kInf ? 0.f : top;
                 total = 0.f;
-                for (uint32_t q = 0; q < a.row_parts; ++q) total = fmaf(of[2u * q + 1u], __builtin_amdgcn_exp2f(of[2u * q] - from_top), total);
+                for (uint32_t q = 0; q < a.row_parts; ++q) total = fmaf(of[2u * q + 1u], Unit<T>::exp(of[2u * q] - from_top), total);
             }
-            float factor = total == 0.f ? 0.f : __builtin_amdgcn_exp2f(from - (top == -kInf ? 0.f : top)) / total;
+            float factor = total == 0.f ? 0.f : Unit<T>::exp(from - (top == -kInf ? 0.f : top)) / total;
             if (a.drop.on) factor *= d.factor;
-            if (a.lse && t == 0u && part == 0u) a.lse[row] = total == 0.f ? -kInf : (top + log2f(total)) * kLn2;
+            if (a.lse && t == 0u && part == 0u) a.lse[row] = total == 0.f ? -kInf : Unit<T>::lse(top, total);
             groups.store(out + int64_t(i) * a.out.row, [&](int v) {
                 f32x8 y = {};
                 const uint32_t here = bits >> (8 * v) & 0xFFu;
@@ -245,7 +263,7 @@ template <typename T, int TPR, int V, int PHASE, bool MASK> __global__ __launch_
     const uint32_t h = blockIdx.x / a.wgs_per_head, group = blockIdx.x - h * a.wgs_per_head;
     const Drop d = drop_of(a.drop);
     const float up_factor = a.drop.on ? d.factor : 1.f;
-    stage_bias(bias, a, h);
+    stage_bias<T>(bias, a, h);
     if (sums)
         for (uint32_t x = threadIdx.x; x < size * TEAMS; x += WG) lds[size + x] = 0.f;
     __syncthreads();
@@ -271,11 +289,11 @@ template <typename T, int TPR, int V, int PHASE, bool MASK> __global__ __launch_
         groups.load_below(raw_up, up, uint32_t(r.limit));
         raw8<uint8_t> mask[V];
         if constexpr (MASK) RowGroups<uint8_t, TPR, V>{groups.t, keys, base}.load_below(mask, r.mask, uint32_t(r.limit));
-        const float lse = a.lse[row], lse2 = lse == -kInf ? kInf : lse * kLog2e;
+        const float lse = a.lse[row], lse2 = lse == -kInf ? kInf : Unit<T>::from_natural(lse);
         // Beyond 2^22 an lse has no fraction left, and its roundings alone would make exponents of any size: there, places that are as
         // near to it as that have P = 1 (rows of the type's lowest value, say; their number is lost in lse).
         const bool coarse = !(fabsf(lse2) < 4194304.f);
-        const float less = coarse ? 0.f : lse2;
+        const float less = coarse || Unit<T>::kNatural ? 0.f : lse2;
         f32x8 p[V], dp[V];
         float inner = 0.f;
 #pragma unroll
@@ -285,7 +303,11 @@ template <typename T, int TPR, int V, int PHASE, bool MASK> __global__ __launch_
             dp[v] = 0.f;
             if (n > 0) {
                 const uint32_t bits = admitted8<MASK>(MASK ? mask_of(groups, mask[v], v) : 0, n);
-                p[v] = biased8(groups.values(raw[v], v), a, r, Window(r, j), bias, bias_low, bias_high, less);
+                p[v] = biased8(groups.values(raw[v], v), a, Unit<T>::scale(a), r, Window(r, j), bias, bias_low, bias_high, less);
+                if (Unit<T>::kNatural && !coarse) {   // the difference as the formula has it: exact where it is small
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) p[v][k] -= lse2;
+                }
                 if (coarse) {
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
@@ -296,7 +318,7 @@ template <typename T, int TPR, int V, int PHASE, bool MASK> __global__ __launch_
                 dp[v] = groups.values(raw_up[v], v);
                 if (a.drop.on) dp[v] = kept8(dp[v], dr, uint32_t(j) / 8u, uint32_t(row));
 #pragma unroll
-                for (int k = 0; k < 8; ++k) p[v][k] = __builtin_amdgcn_exp2f(p[v][k]);
+                for (int k = 0; k < 8; ++k) p[v][k] = Unit<T>::exp(p[v][k]);
                 if (bits != 0xFFu) {
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
@@ -380,10 +402,10 @@ template <typename T, int TPR, int V, int PHASE, bool MASK> __global__ __launch_
 
 // A workgroup to a head and bucket: its first wave lists the distances that have the bucket, and all add up what the backward pass's
 // workgroups have for them, always in the same order.
-__global__ __launch_bounds__(256) void k_bias_reduce(BiasReduce a)
+__global__ __launch_bounds__(1024) void k_bias_reduce(BiasReduce a)
 {
     extern __shared__ uint16_t mine[];   // [2 D + 1]
-    __shared__ float room[4];
+    __shared__ float room[16];
     __shared__ uint32_t found_room;
     constexpr uint32_t AHEAD = 8;        // loads on their way
     const uint32_t n = 2u * a.distance + 1u, h = blockIdx.x, bucket = blockIdx.y;
@@ -408,17 +430,17 @@ __global__ __launch_bounds__(256) void k_bias_reduce(BiasReduce a)
     const uint32_t found = found_room, items = found * a.groups;   // below 4097 * 6 * 256
     const float *from = a.bias_sums + uint64_t(h) * a.groups * n;
     float e = 0.f;
-    for (uint32_t i0 = threadIdx.x; i0 < items; i0 += 256u * AHEAD) {
+    for (uint32_t i0 = threadIdx.x; i0 < items; i0 += 1024u * AHEAD) {
         float part[AHEAD];
 #pragma unroll
         for (uint32_t u = 0; u < AHEAD; ++u) {
-            const uint32_t i = min(i0 + u * 256u, items - 1u), g = i / found;
+            const uint32_t i = min(i0 + u * 1024u, items - 1u), g = i / found;
             part[u] = from[uint64_t(g) * n + mine[i - g * found]];
         }
 #pragma unroll
-        for (uint32_t u = 0; u < AHEAD; ++u) e += i0 + u * 256u < items ? part[u] : 0.f;
+        for (uint32_t u = 0; u < AHEAD; ++u) e += i0 + u * 1024u < items ? part[u] : 0.f;
     }
-    e = over_waves<Add, 4>(over_lanes<Add, 64>(e), room);
+    e = over_waves<Add, 16>(over_lanes<Add, 64>(e), room);
     if (threadIdx.x == 0u) {
         float *to = a.dtable + uint64_t(bucket) * a.heads + h;
         *to = a.accumulate ? *to + e : e;
@@ -558,7 +580,7 @@ int launch_softmax_backward(const SoftmaxArgs &args, uint32_t dtype, const Softm
 int launch_bias_reduce(const BiasReduce &a, void *stream)
 {
     const uint32_t lds = (2u * (2u * a.distance + 1u) + 15u) & ~15u;
-    hipLaunchKernelGGL(k_bias_reduce, dim3(a.heads, a.n_buckets), dim3(256), lds, static_cast<hipStream_t>(stream), a);
+    hipLaunchKernelGGL(k_bias_reduce, dim3(a.heads, a.n_buckets), dim3(1024), lds, static_cast<hipStream_t>(stream), a);
     return check_launch();
 }
 
