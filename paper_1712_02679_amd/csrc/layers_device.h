@@ -73,9 +73,10 @@ __device__ __forceinline__ f32x8 shifted(f32x8 x, uint32_t n)
 // The groups of a row that a thread has: group t + v TPR in round v, `cols` columns in all.  A row whose length is no multiple of 8 ends
 // with an incomplete group.  Its thread reads the row's last 8 values instead, and moves them into place when it uses them: reading values
 // one by one would make the wave wait for them there and then, and with them for everything that is on its way.
-// PAST: results go past the caches (store8_past) where a wave stores neighbouring groups.
-template <typename T, int TPR, int V, bool PAST = sizeof(T) == 2> struct RowGroups {
-    static constexpr bool kShort = TPR == 8;   // rows of less than 8 values come to the form with the fewest threads
+// PAST: results go past the caches (store8_past) where a wave stores neighbouring groups.  SHORT: the row may have fewer than 8 values;
+// otherwise it must have 8.
+template <typename T, int TPR, int V, bool PAST = sizeof(T) == 2, bool SHORT = TPR == 8> struct RowGroups {
+    static constexpr bool kShort = SHORT;
     uint32_t t, cols, first;   // first: column of the part of the row that the threads hold
     __device__ __forceinline__ uint32_t col(int v) const { return first + (t + uint32_t(v) * TPR) * 8u; }
     __device__ __forceinline__ bool whole(int v) const { return col(v) + 8u <= cols; }

@@ -99,6 +99,16 @@ template <bool MASK> __device__ __forceinline__ uint32_t admitted8(uint64_t mask
     return bits;
 }
 
+// The mask's bytes for the groups of a row; ones without a mask.
+template <typename T, int TPR, int V, bool PAST, bool SHORT>
+__device__ __forceinline__ void load_mask(const RowGroups<T, TPR, V, PAST, SHORT> &groups, raw8<uint8_t> (&mask)[V], const Row &r)
+{
+    if (r.mask) RowGroups<uint8_t, TPR, V, false, SHORT>{groups.t, groups.cols, groups.first}.load_below(mask, r.mask, uint32_t(r.limit));
+    else
+#pragma unroll
+        for (int v = 0; v < V; ++v) mask[v] = raw8<uint8_t>(uint8_t(1));
+}
+
 // The mask's bytes that were loaded for round v, in their place.
 template <typename G> __device__ __forceinline__ uint64_t mask_of(const G &groups, raw8<uint8_t> raw, int v)
 {
@@ -124,10 +134,13 @@ __device__ __forceinline__ f32x8 biased8(f32x8 s, const SoftmaxArgs &a, float sc
 
 // WHOLE: a row at a time.  STATS, WRITE: a part of a row, first its maximum and sum, then, from those of all parts, the results.
 enum Phase { WHOLE, STATS, WRITE };
+// MASKED: with a mask.  SHORT: rows shorter than a group, with or without one, in forms of more than 8 threads to a row, which only the
+// backward pass gives to such rows, where the distances are many.
+enum Kind { PLAIN, MASKED, SHORT };
 
 // ---- forward ------------------------------------------------------------------------------------------------------
 
-template <typename T, int TPR, int V, int PHASE, bool MASK> __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_softmax_forward(SoftmaxArgs a)
+template <typename T, int TPR, int V, int PHASE, int KIND> __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_softmax_forward(SoftmaxArgs a)
 {
     constexpr uint32_t TEAMS = TPR > 256 ? 1 : 256 / TPR;
     constexpr int LANES = TPR > 64 ? 64 : TPR;
@@ -150,9 +163,9 @@ template <typename T, int TPR, int V, int PHASE, bool MASK> __global__ __launch_
         Row next = {};
         auto fetch = [&](uint32_t i) {   // a row's scores are on their way while the one before is worked on, the first one's while the bias is laid out
             next = row_of(a, b, h, i);
-            const RowGroups<T, TPR, V> groups = {again(t), again_uniform(a.keys), base};
+            const RowGroups<T, TPR, V, sizeof(T) == 2, TPR == 8 || KIND == SHORT> groups = {again(t), again_uniform(a.keys), base};
             groups.load_below(raw, scores + int64_t(i) * a.scores.row, uint32_t(next.limit));
-            if constexpr (MASK) RowGroups<uint8_t, TPR, V>{groups.t, groups.cols, base}.load_below(mask, next.mask, uint32_t(next.limit));
+            if constexpr (KIND != PLAIN) load_mask(groups, mask, next);
         };
         if (first + team < end) fetch(first + team);
         if (block != blockIdx.x) __syncthreads();   // the rows before are done with the bias
@@ -161,7 +174,7 @@ template <typename T, int TPR, int V, int PHASE, bool MASK> __global__ __launch_
         const float low = bias[0], high = bias[cell(2u * a.distance + kGuard)];
         for (uint32_t i = first + team; i < end; i += TEAMS) {
             const Row r = next;
-            const RowGroups<T, TPR, V> groups = {again(t), again_uniform(a.keys), base};
+            const RowGroups<T, TPR, V, sizeof(T) == 2, TPR == 8 || KIND == SHORT> groups = {again(t), again_uniform(a.keys), base};
             const Drop dr = again(d);
             f32x8 p[V];
             uint32_t bits = 0;   // admitted places, 8 to a group
@@ -171,7 +184,7 @@ template <typename T, int TPR, int V, int PHASE, bool MASK> __global__ __launch_
                 const int j = int(groups.col(v)), n = r.limit - j;
                 p[v] = -kInf;
                 if (n > 0) {
-                    const uint32_t here = admitted8<MASK>(MASK ? mask_of(groups, mask[v], v) : 0, n);
+                    const uint32_t here = admitted8<KIND != PLAIN>(KIND != PLAIN ? mask_of(groups, mask[v], v) : 0, n);
                     bits |= here << (8 * v);
                     p[v] = biased8(groups.values(raw[v], v), a, Unit<T>::scale(a), r, Window(r, j), bias, low, high, 0.f);
                     if (here != 0xFFu) {
@@ -249,7 +262,7 @@ template <typename T, int TPR, int V, int PHASE, bool MASK> __global__ __launch_
 
 // ---- backward -----------------------------------------------------------------------------------------------------
 
-template <typename T, int TPR, int V, int PHASE, bool MASK> __global__ __launch_bounds__(TPR > 256 ? TPR : 256, 4) void k_softmax_backward(SoftmaxArgs a)
+template <typename T, int TPR, int V, int PHASE, int KIND> __global__ __launch_bounds__(TPR > 256 ? TPR : 256, 4) void k_softmax_backward(SoftmaxArgs a)
 {
     constexpr uint32_t TEAMS = TPR > 256 ? 1 : 256 / TPR, WG = TPR > 256 ? TPR : 256;
     constexpr int LANES = TPR > 64 ? 64 : TPR;
@@ -282,13 +295,13 @@ template <typename T, int TPR, int V, int PHASE, bool MASK> __global__ __launch_
         const T *up = static_cast<const T *>(a.in.data) + int64_t(b) * a.in.batch + int64_t(h) * a.in.head + int64_t(i) * a.in.row;
         T *o = static_cast<T *>(const_cast<void *>(a.out.data)) + int64_t(b) * a.out.batch + int64_t(h) * a.out.head + int64_t(i) * a.out.row;
         const uint32_t keys = again_uniform(a.keys);
-        const RowGroups<T, TPR, V> groups = {again(t), keys, base};
+        const RowGroups<T, TPR, V, sizeof(T) == 2, TPR == 8 || KIND == SHORT> groups = {again(t), keys, base};
         const Drop dr = again(d);
         raw8<T> raw[V], raw_up[V];
         groups.load_below(raw, s, uint32_t(r.limit));
         groups.load_below(raw_up, up, uint32_t(r.limit));
         raw8<uint8_t> mask[V];
-        if constexpr (MASK) RowGroups<uint8_t, TPR, V>{groups.t, keys, base}.load_below(mask, r.mask, uint32_t(r.limit));
+        if constexpr (KIND != PLAIN) load_mask(groups, mask, r);
         const float lse = a.lse[row], lse2 = lse == -kInf ? kInf : Unit<T>::from_natural(lse);
         // Beyond 2^22 an lse has no fraction left, and its roundings alone would make exponents of any size: there, places that are as
         // near to it as that have P = 1 (rows of the type's lowest value, say; their number is lost in lse).
@@ -302,7 +315,7 @@ template <typename T, int TPR, int V, int PHASE, bool MASK> __global__ __launch_
             p[v] = 0.f;
             dp[v] = 0.f;
             if (n > 0) {
-                const uint32_t bits = admitted8<MASK>(MASK ? mask_of(groups, mask[v], v) : 0, n);
+                const uint32_t bits = admitted8<KIND != PLAIN>(KIND != PLAIN ? mask_of(groups, mask[v], v) : 0, n);
                 p[v] = biased8(groups.values(raw[v], v), a, Unit<T>::scale(a), r, Window(r, j), bias, bias_low, bias_high, less);
                 if (Unit<T>::kNatural && !coarse) {   // the difference as the formula has it: exact where it is small
 #pragma unroll
@@ -484,26 +497,29 @@ SoftmaxForm softmax_form(uint32_t keys, uint32_t distance, bool backward)
 static uint32_t back_groups(uint64_t rows_of_head, uint32_t heads, const SoftmaxForm &f, uint32_t resident)
 {
     const uint64_t all = (rows_of_head * f.parts + f.row.teams() - 1u) / f.row.teams();
-    return uint32_t(std::min<uint64_t>(all, std::max(1u, resident * kComputeUnits / heads)));
+    const uint64_t most = std::max(1u, resident * kComputeUnits / heads), rounds = (all + most - 1u) / most;
+    return rounds ? uint32_t((all + rounds - 1u) / rounds) : 0u;   // all with as many rows, up to one
 }
 
 // Most of them that a call can have: what the workspace has room for.
 uint32_t softmax_back_groups_most(uint64_t rows_of_head, uint32_t heads, const SoftmaxForm &f) { return back_groups(rows_of_head, heads, f, kMostResident); }
 
 // Picks the kernel of a form and type and calls launch(kernel, phase) with it; twice where rows are cut into parts.
-template <template <typename, int, int, int, bool> class K, typename L>
+template <template <typename, int, int, int, int> class K, typename L>
 static int with_kernel(const SoftmaxArgs &a, uint32_t dtype, const SoftmaxForm &f, L &&launch)
 {
     auto go = [&](auto form, auto phase) {
         constexpr int TPR = decltype(form)::threads, V = decltype(form)::groups, PHASE = decltype(phase)::value;
-        auto of = [&](auto masked) {
-            constexpr bool MASK = decltype(masked)::value;
-            if (dtype == ADACOMP_DTYPE_F32) launch(std::integral_constant<void (*)(SoftmaxArgs), K<float, TPR, V, PHASE, MASK>::kernel>());
-            else if (dtype == ADACOMP_DTYPE_BF16) launch(std::integral_constant<void (*)(SoftmaxArgs), K<bf16, TPR, V, PHASE, MASK>::kernel>());
-            else launch(std::integral_constant<void (*)(SoftmaxArgs), K<f16, TPR, V, PHASE, MASK>::kernel>());
+        auto of = [&](auto kind) {
+            constexpr int KIND = decltype(kind)::value;
+            if (dtype == ADACOMP_DTYPE_F32) launch(std::integral_constant<void (*)(SoftmaxArgs), K<float, TPR, V, PHASE, KIND>::kernel>());
+            else if (dtype == ADACOMP_DTYPE_BF16) launch(std::integral_constant<void (*)(SoftmaxArgs), K<bf16, TPR, V, PHASE, KIND>::kernel>());
+            else launch(std::integral_constant<void (*)(SoftmaxArgs), K<f16, TPR, V, PHASE, KIND>::kernel>());
         };
-        if (a.mask.data) of(std::true_type());
-        else of(std::false_type());
+        if constexpr (TPR > 8 && V == 2 && PHASE == WHOLE)
+            if (a.keys < 8u) return of(std::integral_constant<int, SHORT>());
+        if (a.mask.data) of(std::integral_constant<int, MASKED>());
+        else of(std::integral_constant<int, PLAIN>());
     };
     using Whole = std::integral_constant<int, WHOLE>;
     if (f.parts > 1u) {
@@ -531,8 +547,8 @@ static int with_kernel(const SoftmaxArgs &a, uint32_t dtype, const SoftmaxForm &
     return check_launch();
 }
 
-template <typename T, int TPR, int V, int PHASE, bool MASK> struct KForward { static constexpr auto kernel = k_softmax_forward<T, TPR, V, PHASE, MASK>; };
-template <typename T, int TPR, int V, int PHASE, bool MASK> struct KBackward { static constexpr auto kernel = k_softmax_backward<T, TPR, V, PHASE, MASK>; };
+template <typename T, int TPR, int V, int PHASE, int KIND> struct KForward { static constexpr auto kernel = k_softmax_forward<T, TPR, V, PHASE, KIND>; };
+template <typename T, int TPR, int V, int PHASE, int KIND> struct KBackward { static constexpr auto kernel = k_softmax_backward<T, TPR, V, PHASE, KIND>; };
 
 // Rows of a team, one after the other, in a workgroup of the forward pass: about 24000 keys to a workgroup, or 8 times what its bias takes
 // to lay out, and fewer where that leaves compute units without work.

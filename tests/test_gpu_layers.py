@@ -368,6 +368,35 @@ def test_softmax(A, shape, dtype):
             untouched(c.out, 3, 1)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("far,buckets", [(3, 4), (128, 32), (250, 64), (800, 320), (2048, 32)])
+def test_softmax_of_few_keys(A, far, buckets, dtype):
+    """Rows shorter than a group of 8, and just longer ones, whatever form the distances make them take."""
+    for keys in (1, 2, 5, 7, 8, 9, 15, 16, 17):
+        for mask in (None, "single"):
+            c = Case(A, (2, 3, 21, keys, mask is None, 0 if mask else [keys - 21, 4], None if mask else [keys, (keys + 1) // 2], mask, buckets, far), dtype, 0.1, "odd")
+            c.forward()
+            c.backward()
+            untouched(c.out, 3, 1)
+
+
+@pytest.mark.parametrize("keys", [65, 129, 200, 257, 511, 513, 900, 1025, 1500, 2049, 3500, 4097, 8193, 12001, 16385, 30001, 32769])
+def test_softmax_at_the_bounds_of_its_forms(A, keys):
+    for far, buckets, dtype, mask in ((128, 32, torch.bfloat16, None), (800, 320, torch.float32, "single"), (2048, 33, torch.float16, "row")):
+        queries = 40 if keys < 1000 else 7
+        c = Case(A, (2, 2, queries, keys, True, [keys - queries, keys // 2], [keys, keys // 2 + 1], mask, buckets, far), dtype, 0.1)
+        c.forward()
+        c.backward()
+
+
+def test_softmax_of_many_short_sequences(A):
+    """More (batch, head) pairs than workgroups fit the GPU, and heads without rows for every workgroup."""
+    for shape in ((300, 7, 3, 20, True, 17, None, None, 32, 128), (1, 600, 2, 40, False, 0, None, None, 32, 128), (50, 1, 90, 33, False, 0, None, None, 32, 128)):
+        c = Case(A, shape, torch.bfloat16, 0.1)
+        c.forward()
+        c.backward()
+
+
 def test_softmax_in_place_and_without_the_table_gradient(A):
     for shape in (SHAPES[4], SHAPES[12], SHAPES[18]):
         c = Case(A, shape, torch.bfloat16, 0.1)
