@@ -59,13 +59,13 @@ template <int TPR> __device__ __forceinline__ float over_row(float x, float *roo
     }
 }
 
-template <typename T, int TPR, int V, bool PAST> __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_norm_forward(NormForward a)
+template <typename T, int TPR, int V, int FLOW> __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_norm_forward(NormForward a)
 {
     constexpr uint32_t TEAMS = TPR > 256 ? 1 : 256 / TPR;
     __shared__ float room[2][16];
     const uint32_t t = threadIdx.x % TPR, team = team_of<TPR>(), row = blockIdx.x * TEAMS + team;
     const bool live = row < a.rows;   // the last workgroup may have teams without a row: they go along to the barriers
-    const RowGroups<T, TPR, V, PAST> groups = {t, a.cols, 0};
+    const RowGroups<T, TPR, V, FLOW> groups = {t, a.cols, 0};
     raw8<T> raw[V] = {}, raw_res[V] = {};
     if (live) {
         groups.load(raw, static_cast<const T *>(a.x) + row * a.x_stride);
@@ -117,7 +117,7 @@ template <typename T, int TPR, int V, bool PAST> __global__ __launch_bounds__(TP
 
 constexpr uint32_t kBackThreads = 1024;
 
-template <typename T, int TPR, bool PAST> __global__ __launch_bounds__(kBackThreads) void k_norm_backward(NormBackward a)
+template <typename T, int TPR, int FLOW> __global__ __launch_bounds__(kBackThreads) void k_norm_backward(NormBackward a)
 {
     constexpr uint32_t TEAMS = kBackThreads / TPR, COLS = TPR * 8;
     __shared__ float room[2][2][16];
@@ -133,7 +133,7 @@ template <typename T, int TPR, bool PAST> __global__ __launch_bounds__(kBackThre
     raw8<T> raw_dy, raw_z, raw_add;
     float mean = 0.f, rstd = 0.f;
     auto fetch = [&](uint32_t row) {
-        const RowGroups<T, TPR, 1, PAST> groups = {again(t), again_uniform(a.cols), 0};
+        const RowGroups<T, TPR, 1, FLOW> groups = {again(t), again_uniform(a.cols), 0};
         raw_dy = raw_z = raw_add = raw8<T>{};
         if (row < a.rows) {
             raw_dy = groups.load_round(static_cast<const T *>(a.dy) + row * a.dy_stride, 0);
@@ -148,7 +148,7 @@ template <typename T, int TPR, bool PAST> __global__ __launch_bounds__(kBackThre
     for (uint32_t first = blockIdx.x * TEAMS; first < a.rows; first += gridDim.x * TEAMS) {
         const uint32_t row = first + team;
         const float scale = rstd;
-        const RowGroups<T, TPR, 1, PAST> groups = {again(t), again_uniform(a.cols), 0};
+        const RowGroups<T, TPR, 1, FLOW> groups = {again(t), again_uniform(a.cols), 0};
         f32x8 g = groups.values(raw_dy, 0), dz = groups.values(raw_add, 0);
         const f32x8 h = (groups.values(raw_z, 0) - mean) * scale;
         fetch(row + gridDim.x * TEAMS);
@@ -205,7 +205,7 @@ template <typename T, int TPR, bool PAST> __global__ __launch_bounds__(kBackThre
 
 // Rows of more than 8192 columns: the sums of V groups of columns leave no registers for the row, which is read a second time, from
 // the caches, for dz.
-template <typename T, int V, bool PAST> __global__ __launch_bounds__(kBackThreads) void k_norm_backward_wide(NormBackward a)
+template <typename T, int V> __global__ __launch_bounds__(kBackThreads) void k_norm_backward_wide(NormBackward a)
 {
     constexpr int TPR = kBackThreads;
     __shared__ float room[2][16];
@@ -219,7 +219,7 @@ template <typename T, int V, bool PAST> __global__ __launch_bounds__(kBackThread
         float s1 = 0.f, s2 = 0.f;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const RowGroups<T, TPR, V, PAST> groups = {again(t), again_uniform(a.cols), 0};
+            const RowGroups<T, TPR, V> groups = {again(t), again_uniform(a.cols), 0};
             const RowGroups<float, TPR, V> params = {groups.t, groups.cols, 0};
             f32x8 g = groups.values(groups.load_round(dy, v), v);
             const f32x8 h = (groups.values(groups.load_round(z, v), v) - mean) * rstd;
@@ -237,7 +237,7 @@ template <typename T, int V, bool PAST> __global__ __launch_bounds__(kBackThread
         s2 = over_waves<Add, TPR / 64>(over_lanes<Add, 64>(s2), room[1]) * per_col;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const RowGroups<T, TPR, V, PAST> groups = {again(t), again_uniform(a.cols), 0};
+            const RowGroups<T, TPR, V> groups = {again(t), again_uniform(a.cols), 0};
             const RowGroups<float, TPR, V> params = {groups.t, groups.cols, 0};
             f32x8 g = groups.values(groups.load_round(dy, v), v), dz = 0.f;
             const f32x8 h = (groups.values(groups.load_round(z, v), v) - mean) * rstd;
@@ -293,15 +293,16 @@ template <typename F> static int with_type(uint32_t dtype, F &&f)
     return check_launch();
 }
 
+// Whether all of a tensor's rows begin with a line of memory.
+static bool lines(const void *p, uint64_t stride, uint64_t size) { return !p || (reinterpret_cast<uintptr_t>(p) | stride * size) % 64u == 0u; }
+
 int launch_dropout(const DropoutLaunch &a, void *stream)
 {
     const dim3 grid((a.rows * a.groups + 255u) / 256u), wg(256);
     hipStream_t s = static_cast<hipStream_t>(stream);
     const uint64_t size = a.dtype == ADACOMP_DTYPE_F32 ? 4u : 2u;
-    // Inputs past the caches too, where they are larger than those and no two groups share a line: 16384 x 4096 bf16 with residual 68.3 / 63.8 us, but
-    // 5003 x 5999 f16 22.0 / 23.5, 2000 x 4096 8.8 / 9.5.
-    const bool lines = a.cols % 8u == 0u && (reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.residual) | a.x_stride * size | a.residual_stride * size) % 64u == 0u;
-    const bool once = lines && size == 2u && uint64_t(a.rows) * a.cols * size * (a.residual ? 2u : 1u) >= uint64_t(192) << 20;
+    const bool once = size == 2u && a.cols % 32u == 0u && lines(a.x, a.x_stride, size) && lines(a.residual, a.residual_stride, size) &&
+                      uint64_t(a.rows) * a.cols * size * (a.residual ? 2u : 1u) >= kInputsPast;
     return with_type(a.dtype, [&](auto of) {
         using T = decltype(of);
         if (once) hipLaunchKernelGGL((k_dropout<T, true>), grid, wg, 0, s, a);
@@ -331,12 +332,13 @@ uint32_t norm_parts(uint64_t rows, uint32_t cols)
     return uint32_t(std::min<uint64_t>((rows + teams - 1u) / teams, kComputeUnits));
 }
 
-// Calls f with whether results go past the caches: 16-bit ones do, and 32-bit ones of calls that the memory-side cache holds.
-template <typename T, typename F> static void with_past(uint64_t values, F &&f)
+// Calls f with what goes past the caches; inputs: so many tensors of `values` values, whole lines of them or not.
+template <typename T, typename F> static void with_flow(uint64_t values, uint32_t inputs, bool whole_lines, F &&f)
 {
-    if constexpr (sizeof(T) == 4)
-        if (values > uint64_t(16) << 20) return f(std::false_type());
-    f(std::true_type());
+    if constexpr (sizeof(T) == 4) {
+        if (values > uint64_t(16) << 20) return f(std::integral_constant<int, CACHED>());
+    } else if (whole_lines && values * sizeof(T) * inputs >= kInputsPast) return f(std::integral_constant<int, ALL_PAST>());
+    f(std::integral_constant<int, RESULTS_PAST>());
 }
 
 // Calls f with the number of threads.
@@ -382,14 +384,15 @@ int launch_norm_forward(const NormForward &args, uint32_t dtype, void *stream)
         if (a.rstd) a.rstd += first;
         const dim3 grid((a.rows + teams - 1u) / teams);
         const uint32_t lds = idle_lds(a, uint32_t(size), wg);
+        const bool whole_lines = a.cols % 32u == 0u && lines(a.x, a.x_stride, size) && lines(a.residual, a.residual_stride, size);
         hipStream_t s = static_cast<hipStream_t>(stream);
         const int rc = with_type(dtype, [&](auto of) {
             using T = decltype(of);
-            with_past<T>(args.all_rows * a.cols, [&](auto past) {
-                constexpr bool PAST = decltype(past)::value;
-                if (a.cols <= 64u) hipLaunchKernelGGL((k_norm_forward<T, 8, 1, PAST>), grid, dim3(wg), lds, s, a);
-                else if (a.cols > 16384u) hipLaunchKernelGGL((k_norm_forward<T, 1024, 4, PAST>), grid, dim3(wg), lds, s, a);
-                else with_threads(threads, [&](auto n) { hipLaunchKernelGGL((k_norm_forward<T, decltype(n)::value, 2, PAST>), grid, dim3(wg), lds, s, a); });
+            with_flow<T>(args.all_rows * a.cols, a.residual ? 2u : 1u, whole_lines, [&](auto flow) {
+                constexpr int FLOW = decltype(flow)::value;
+                if (a.cols <= 64u) hipLaunchKernelGGL((k_norm_forward<T, 8, 1, FLOW>), grid, dim3(wg), lds, s, a);
+                else if (a.cols > 16384u) hipLaunchKernelGGL((k_norm_forward<T, 1024, 4, FLOW>), grid, dim3(wg), lds, s, a);
+                else with_threads(threads, [&](auto n) { hipLaunchKernelGGL((k_norm_forward<T, decltype(n)::value, 2, FLOW>), grid, dim3(wg), lds, s, a); });
             });
         });
         if (rc) return rc;
@@ -403,11 +406,12 @@ int launch_norm_backward(const NormBackward &a, uint32_t dtype, uint32_t parts, 
     hipStream_t s = static_cast<hipStream_t>(stream);
     return with_type(dtype, [&](auto of) {
         using T = decltype(of);
-        with_past<T>(uint64_t(a.rows) * a.cols, [&](auto past) {
-            constexpr bool PAST = decltype(past)::value;
-            if (a.cols > 16384u) hipLaunchKernelGGL((k_norm_backward_wide<T, 4, PAST>), grid, wg, 0, s, a);
-            else if (a.cols > 8192u) hipLaunchKernelGGL((k_norm_backward_wide<T, 2, PAST>), grid, wg, 0, s, a);
-            else with_threads(backward_threads(a.cols), [&](auto n) { hipLaunchKernelGGL((k_norm_backward<T, decltype(n)::value, PAST>), grid, wg, 0, s, a); });
+        if (a.cols > 16384u) { hipLaunchKernelGGL((k_norm_backward_wide<T, 4>), grid, wg, 0, s, a); return; }
+        if (a.cols > 8192u) { hipLaunchKernelGGL((k_norm_backward_wide<T, 2>), grid, wg, 0, s, a); return; }
+        const bool whole_lines = a.cols % 32u == 0u && lines(a.dy, a.dy_stride, sizeof(T)) && lines(a.z, a.z_stride, sizeof(T)) && lines(a.dz_add, a.dz_add_stride, sizeof(T));
+        with_flow<T>(uint64_t(a.rows) * a.cols, a.dz_add ? 3u : 2u, whole_lines, [&](auto flow) {
+            constexpr int FLOW = decltype(flow)::value;
+            with_threads(backward_threads(a.cols), [&](auto n) { hipLaunchKernelGGL((k_norm_backward<T, decltype(n)::value, FLOW>), grid, wg, 0, s, a); });
         });
     });
 }

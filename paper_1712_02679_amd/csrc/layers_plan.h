@@ -18,6 +18,8 @@ struct DropArgs {
     float factor;
 };
 
+constexpr uint64_t kInputsPast = uint64_t(192) << 20;   // bytes of 16-bit inputs that go past the caches, where their rows are whole lines
+
 // A thread takes groups of 8 columns, each one counter of the generator: threads to a row (a part of a wave, a wave, or a
 // workgroup) times groups to a thread cover the row.
 struct RowForm {

@@ -100,10 +100,10 @@ template <bool MASK> __device__ __forceinline__ uint32_t admitted8(uint64_t mask
 }
 
 // The mask's bytes for the groups of a row; ones without a mask.
-template <typename T, int TPR, int V, bool PAST, bool SHORT>
-__device__ __forceinline__ void load_mask(const RowGroups<T, TPR, V, PAST, SHORT> &groups, raw8<uint8_t> (&mask)[V], const Row &r)
+template <typename T, int TPR, int V, int FLOW, bool SHORT>
+__device__ __forceinline__ void load_mask(const RowGroups<T, TPR, V, FLOW, SHORT> &groups, raw8<uint8_t> (&mask)[V], const Row &r)
 {
-    if (r.mask) RowGroups<uint8_t, TPR, V, false, SHORT>{groups.t, groups.cols, groups.first}.load_below(mask, r.mask, uint32_t(r.limit));
+    if (r.mask) RowGroups<uint8_t, TPR, V, CACHED, SHORT>{groups.t, groups.cols, groups.first}.load_below(mask, r.mask, uint32_t(r.limit));
     else
 #pragma unroll
         for (int v = 0; v < V; ++v) mask[v] = raw8<uint8_t>(uint8_t(1));
@@ -136,7 +136,9 @@ __device__ __forceinline__ f32x8 biased8(f32x8 s, const SoftmaxArgs &a, float sc
 enum Phase { WHOLE, STATS, WRITE };
 // MASKED: with a mask.  SHORT: rows shorter than a group, with or without one, in forms of more than 8 threads to a row, which only the
 // backward pass gives to such rows, where the distances are many.
-enum Kind { PLAIN, MASKED, SHORT };
+// ONCE: large inputs without a mask, in whole lines, past the caches.
+enum Kind { PLAIN, MASKED, SHORT, ONCE };
+template <int KIND> constexpr bool kMasked = KIND == MASKED || KIND == SHORT;
 
 // ---- forward ------------------------------------------------------------------------------------------------------
 
@@ -163,9 +165,9 @@ template <typename T, int TPR, int V, int PHASE, int KIND> __global__ __launch_b
         Row next = {};
         auto fetch = [&](uint32_t i) {   // a row's scores are on their way while the one before is worked on, the first one's while the bias is laid out
             next = row_of(a, b, h, i);
-            const RowGroups<T, TPR, V, sizeof(T) == 2, TPR == 8 || KIND == SHORT> groups = {again(t), again_uniform(a.keys), base};
+            const RowGroups<T, TPR, V, KIND == ONCE ? int(ALL_PAST) : kFlow<T>, TPR == 8 || KIND == SHORT> groups = {again(t), again_uniform(a.keys), base};
             groups.load_below(raw, scores + int64_t(i) * a.scores.row, uint32_t(next.limit));
-            if constexpr (KIND != PLAIN) load_mask(groups, mask, next);
+            if constexpr (kMasked<KIND>) load_mask(groups, mask, next);
         };
         if (first + team < end) fetch(first + team);
         if (block != blockIdx.x) __syncthreads();   // the rows before are done with the bias
@@ -174,7 +176,7 @@ template <typename T, int TPR, int V, int PHASE, int KIND> __global__ __launch_b
         const float low = bias[0], high = bias[cell(2u * a.distance + kGuard)];
         for (uint32_t i = first + team; i < end; i += TEAMS) {
             const Row r = next;
-            const RowGroups<T, TPR, V, sizeof(T) == 2, TPR == 8 || KIND == SHORT> groups = {again(t), again_uniform(a.keys), base};
+            const RowGroups<T, TPR, V, KIND == ONCE ? int(ALL_PAST) : kFlow<T>, TPR == 8 || KIND == SHORT> groups = {again(t), again_uniform(a.keys), base};
             const Drop dr = again(d);
             f32x8 p[V];
             uint32_t bits = 0;   // admitted places, 8 to a group
@@ -184,7 +186,7 @@ template <typename T, int TPR, int V, int PHASE, int KIND> __global__ __launch_b
                 const int j = int(groups.col(v)), n = r.limit - j;
                 p[v] = -kInf;
                 if (n > 0) {
-                    const uint32_t here = admitted8<KIND != PLAIN>(KIND != PLAIN ? mask_of(groups, mask[v], v) : 0, n);
+                    const uint32_t here = admitted8<kMasked<KIND>>(kMasked<KIND> ? mask_of(groups, mask[v], v) : 0, n);
                     bits |= here << (8 * v);
                     p[v] = biased8(groups.values(raw[v], v), a, Unit<T>::scale(a), r, Window(r, j), bias, low, high, 0.f);
                     if (here != 0xFFu) {
@@ -295,13 +297,13 @@ template <typename T, int TPR, int V, int PHASE, int KIND> __global__ __launch_b
         const T *up = static_cast<const T *>(a.in.data) + int64_t(b) * a.in.batch + int64_t(h) * a.in.head + int64_t(i) * a.in.row;
         T *o = static_cast<T *>(const_cast<void *>(a.out.data)) + int64_t(b) * a.out.batch + int64_t(h) * a.out.head + int64_t(i) * a.out.row;
         const uint32_t keys = again_uniform(a.keys);
-        const RowGroups<T, TPR, V, sizeof(T) == 2, TPR == 8 || KIND == SHORT> groups = {again(t), keys, base};
+        const RowGroups<T, TPR, V, KIND == ONCE ? int(ALL_PAST) : kFlow<T>, TPR == 8 || KIND == SHORT> groups = {again(t), keys, base};
         const Drop dr = again(d);
         raw8<T> raw[V], raw_up[V];
         groups.load_below(raw, s, uint32_t(r.limit));
         groups.load_below(raw_up, up, uint32_t(r.limit));
         raw8<uint8_t> mask[V];
-        if constexpr (KIND != PLAIN) load_mask(groups, mask, r);
+        if constexpr (kMasked<KIND>) load_mask(groups, mask, r);
         const float lse = a.lse[row], lse2 = lse == -kInf ? kInf : Unit<T>::from_natural(lse);
         // Beyond 2^22 an lse has no fraction left, and its roundings alone would make exponents of any size: there, places that are as
         // near to it as that have P = 1 (rows of the type's lowest value, say; their number is lost in lse).
@@ -315,7 +317,7 @@ template <typename T, int TPR, int V, int PHASE, int KIND> __global__ __launch_b
             p[v] = 0.f;
             dp[v] = 0.f;
             if (n > 0) {
-                const uint32_t bits = admitted8<KIND != PLAIN>(KIND != PLAIN ? mask_of(groups, mask[v], v) : 0, n);
+                const uint32_t bits = admitted8<kMasked<KIND>>(kMasked<KIND> ? mask_of(groups, mask[v], v) : 0, n);
                 p[v] = biased8(groups.values(raw[v], v), a, Unit<T>::scale(a), r, Window(r, j), bias, bias_low, bias_high, less);
                 if (Unit<T>::kNatural && !coarse) {   // the difference as the formula has it: exact where it is small
 #pragma unroll
@@ -508,16 +510,24 @@ uint32_t softmax_back_groups_most(uint64_t rows_of_head, uint32_t heads, const S
 template <template <typename, int, int, int, int> class K, typename L>
 static int with_kernel(const SoftmaxArgs &a, uint32_t dtype, const SoftmaxForm &f, L &&launch)
 {
+    constexpr bool BACK = K<float, 8, 1, WHOLE, PLAIN>::kBackward;
+    const auto lines = [](const ViewArgs &v) { return (reinterpret_cast<uintptr_t>(v.data) | uint64_t(v.batch * 2) | uint64_t(v.head * 2) | uint64_t(v.row * 2)) % 64u == 0u; };
+    // the backward pass, whose inputs are two thirds of its traffic: 320 us instead of 329; the forward pass gains nothing
+    const bool once = BACK && !a.mask.data && dtype != ADACOMP_DTYPE_F32 && a.keys % 32u == 0u && lines(a.scores) && lines(a.in) &&
+                      uint64_t(a.batch) * a.heads * a.queries * a.keys * 4u >= kInputsPast;
     auto go = [&](auto form, auto phase) {
         constexpr int TPR = decltype(form)::threads, V = decltype(form)::groups, PHASE = decltype(phase)::value;
         auto of = [&](auto kind) {
             constexpr int KIND = decltype(kind)::value;
-            if (dtype == ADACOMP_DTYPE_F32) launch(std::integral_constant<void (*)(SoftmaxArgs), K<float, TPR, V, PHASE, KIND>::kernel>());
-            else if (dtype == ADACOMP_DTYPE_BF16) launch(std::integral_constant<void (*)(SoftmaxArgs), K<bf16, TPR, V, PHASE, KIND>::kernel>());
+            if constexpr (KIND != ONCE)
+                if (dtype == ADACOMP_DTYPE_F32) return launch(std::integral_constant<void (*)(SoftmaxArgs), K<float, TPR, V, PHASE, KIND>::kernel>());
+            if (dtype == ADACOMP_DTYPE_BF16) launch(std::integral_constant<void (*)(SoftmaxArgs), K<bf16, TPR, V, PHASE, KIND>::kernel>());
             else launch(std::integral_constant<void (*)(SoftmaxArgs), K<f16, TPR, V, PHASE, KIND>::kernel>());
         };
-        if constexpr (TPR > 8 && V == 2 && PHASE == WHOLE)
+        if constexpr (BACK && TPR > 8 && V == 2 && PHASE == WHOLE)
             if (a.keys < 8u) return of(std::integral_constant<int, SHORT>());
+        if constexpr (BACK && V * TPR >= 256 && PHASE == WHOLE)
+            if (once) return of(std::integral_constant<int, ONCE>());
         if (a.mask.data) of(std::integral_constant<int, MASKED>());
         else of(std::integral_constant<int, PLAIN>());
     };
@@ -531,12 +541,12 @@ static int with_kernel(const SoftmaxArgs &a, uint32_t dtype, const SoftmaxForm &
     switch (f.row.threads * 8u + f.row.groups) {
     case 8 * 8 + 1: go(FormOf<8, 1>(), Whole()); break;
     case 8 * 8 + 2: go(FormOf<8, 2>(), Whole()); break;
-    case 8 * 8 + 4: go(FormOf<8, 4>(), Whole()); break;
-    case 16 * 8 + 2: go(FormOf<16, 2>(), Whole()); break;
-    case 16 * 8 + 4: go(FormOf<16, 4>(), Whole()); break;
-    case 32 * 8 + 2: go(FormOf<32, 2>(), Whole()); break;
-    case 32 * 8 + 4: go(FormOf<32, 4>(), Whole()); break;
-    case 64 * 8 + 2: go(FormOf<64, 2>(), Whole()); break;
+    case 8 * 8 + 4: if constexpr (!BACK) go(FormOf<8, 4>(), Whole()); break;
+    case 16 * 8 + 2: if constexpr (BACK) go(FormOf<16, 2>(), Whole()); break;
+    case 16 * 8 + 4: if constexpr (!BACK) go(FormOf<16, 4>(), Whole()); break;
+    case 32 * 8 + 2: if constexpr (BACK) go(FormOf<32, 2>(), Whole()); break;
+    case 32 * 8 + 4: if constexpr (!BACK) go(FormOf<32, 4>(), Whole()); break;
+    case 64 * 8 + 2: if constexpr (BACK) go(FormOf<64, 2>(), Whole()); break;
     case 64 * 8 + 4: go(FormOf<64, 4>(), Whole()); break;
     case 256 * 8 + 2: go(FormOf<256, 2>(), Whole()); break;
     case 256 * 8 + 4: go(FormOf<256, 4>(), Whole()); break;
@@ -547,8 +557,8 @@ static int with_kernel(const SoftmaxArgs &a, uint32_t dtype, const SoftmaxForm &
     return check_launch();
 }
 
-template <typename T, int TPR, int V, int PHASE, int KIND> struct KForward { static constexpr auto kernel = k_softmax_forward<T, TPR, V, PHASE, KIND>; };
-template <typename T, int TPR, int V, int PHASE, int KIND> struct KBackward { static constexpr auto kernel = k_softmax_backward<T, TPR, V, PHASE, KIND>; };
+template <typename T, int TPR, int V, int PHASE, int KIND> struct KForward { static constexpr bool kBackward = false; static constexpr auto kernel = k_softmax_forward<T, TPR, V, PHASE, KIND>; };
+template <typename T, int TPR, int V, int PHASE, int KIND> struct KBackward { static constexpr bool kBackward = true; static constexpr auto kernel = k_softmax_backward<T, TPR, V, PHASE, KIND>; };
 
 // Rows of a team, one after the other, in a workgroup of the forward pass: about 24000 keys to a workgroup, or 8 times what its bias takes
 // to lay out, and fewer where that leaves compute units without work.

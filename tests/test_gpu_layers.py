@@ -480,6 +480,60 @@ def test_softmax_offsets_beyond_32_bits(A):
     assert torch.equal(s, want)
 
 
+# ---- large calls ----------------------------------------------------------------------------------------------------
+
+def test_large_calls_agree_with_small_ones(A):
+    """Calls beyond the caches, whose inputs and results go past them, give their first rows what a call of those rows alone gives."""
+    few = 700
+    for rows, cols in ((26000, 4096), (110000, 1024), (13000, 8192)):
+        g = torch.Generator(device=DEV).manual_seed(cols)
+        new = lambda: torch.randn(rows, cols, generator=g, device=DEV).to(torch.bfloat16)
+        x, res, drop = new(), new(), A.Dropout(0.1, 4, 5)
+        y, part = torch.empty_like(x), torch.empty(few, cols, dtype=torch.bfloat16, device=DEV)
+        A.adacomp_dropout(x, y, drop, residual=res)
+        A.adacomp_dropout(x[:few], part, drop, residual=res[:few])
+        assert torch.equal(y[:few], part)
+        gamma, beta = torch.randn(cols, generator=g, device=DEV), torch.randn(cols, generator=g, device=DEV)
+        z, mean, rstd = torch.empty_like(x), torch.empty(rows, device=DEV), torch.empty(rows, device=DEV)
+        A.adacomp_norm_forward(x, gamma, beta, y, residual=res, dropout=drop, z=z, mean=mean, rstd=rstd)
+        A.adacomp_norm_forward(x[:few], gamma, beta, part, residual=res[:few], dropout=drop)
+        assert torch.equal(y[:few], part)
+        dz, dx, dgamma, dbeta = torch.empty_like(x), torch.empty_like(x), torch.empty_like(gamma), torch.empty_like(beta)
+        ws = torch.empty(A.adacomp_norm_workspace_bytes(rows, cols), dtype=torch.uint8, device=DEV)
+        A.adacomp_norm_backward(x, z, mean, rstd, gamma, dz, dgamma, dbeta, ws, dz_add=res, dropout=drop, dx=dx)
+        part_x = torch.empty_like(part)
+        A.adacomp_norm_backward(x[:few], z[:few], mean[:few], rstd[:few], gamma, part, None, None, ws, dz_add=res[:few], dropout=drop, dx=part_x)
+        assert torch.equal(dz[:few], part) and torch.equal(dx[:few], part_x)
+        h = (z.double() - mean.double()[:, None]) * rstd.double()[:, None]
+        within(dgamma, (x.double() * h).sum(0).cpu(), U * 400 * (x.double() * h).abs().sum(0).cpu(), "dgamma")   # up to 110000 / 2048 rows a thread
+        within(dbeta, x.double().sum(0).cpu(), U * 400 * x.double().abs().sum(0).cpu(), "dbeta")
+        del h
+    for keys in (1024, 2048, 4096, 8192, 16384, 32768):
+        batch, heads, queries = 4, 4, (1 << 22) // keys
+        g = torch.Generator(device=DEV).manual_seed(keys)
+        s, up = (torch.randn(batch, heads, queries, keys, generator=g, device=DEV).to(torch.float16) for _ in range(2))
+        bias = A.RelativeBias(torch.randn(32, heads, generator=g, device=DEV), torch.from_numpy(A.adacomp_relative_buckets(32, 128, True)).to(DEV))
+        ws = torch.empty(A.adacomp_bias_softmax_workspace_bytes(batch, heads, queries, keys, 128), dtype=torch.uint8, device=DEV)
+        lengths = torch.tensor([keys - 5, keys, keys // 2, 1], dtype=torch.int32, device=DEV)
+        out, part, lse = torch.empty_like(s), torch.empty_like(s[:1]), torch.empty(batch, heads, queries, device=DEV)
+        options = dict(scale=0.5, query_start=keys // 2, dropout=A.Dropout(0.2, 7, 8))
+        A.adacomp_bias_softmax_forward(s, bias, out, ws, lse=lse, key_lengths=lengths, **options)
+        A.adacomp_bias_softmax_forward(s[:1], bias, part, ws, key_lengths=lengths[:1], **options)
+        assert torch.equal(out[:1], part)
+        dtable, small = torch.empty(32, heads, device=DEV), torch.zeros(32, heads, device=DEV)
+        A.adacomp_bias_softmax_backward(s, bias, lse, up, out, dtable, ws, key_lengths=lengths, **options)
+        for b in range(batch):
+            drop = dict(options, dropout=None)
+            if b == 0:
+                A.adacomp_bias_softmax_backward(s[:1], bias, lse[:1], up[:1], part, None, ws, key_lengths=lengths[:1], **options)
+                assert torch.equal(out[:1], part)
+            A.adacomp_bias_softmax_backward(s[b:b + 1], bias, lse[b:b + 1], up[b:b + 1], part, small, ws, key_lengths=lengths[b:b + 1], accumulate=True, **drop)
+        whole = torch.empty_like(dtable)
+        A.adacomp_bias_softmax_backward(s, bias, lse, up, out, whole, ws, key_lengths=lengths, **drop)
+        # the same terms in another order: |e| is below 5 P, and a row's P add up to 1
+        assert (whole.double() - small.double()).abs().max() <= U * 400 * batch * queries * 10
+
+
 # ---- gradients against differences of the kernels' own results -----------------------------------------------------
 
 def test_norm_gradients_against_differences(A):
