@@ -1,8 +1,10 @@
 """Builds libadacomp.so (HIP, gfx950 only) in-tree with hipcc."""
 from __future__ import annotations
 
+import concurrent.futures
 import os
 import subprocess
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -21,15 +23,26 @@ HIPCC_FLAGS = [
 
 
 def build(verbose: bool = False) -> str:
+    """Compiles the sources side by side and links them."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = [hipcc, *HIPCC_FLAGS, "-I" + os.path.join(ROOT, "include"), "-I" + CSRC, "-o", LIB,
-           *[os.path.join(CSRC, s) for s in SOURCES]]
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if verbose or res.returncode != 0:
-        print(res.stdout)
-        print(res.stderr)
-    if res.returncode != 0:
-        raise RuntimeError("hipcc failed building libadacomp.so")
+    compile_flags = [f for f in HIPCC_FLAGS if f != "-shared"]
+    with tempfile.TemporaryDirectory(prefix="libadacomp_") as objects:
+        def compile_one(source):
+            out = os.path.join(objects, source + ".o")
+            return out, subprocess.run([hipcc, *compile_flags, "-I" + os.path.join(ROOT, "include"), "-I" + CSRC, "-c", "-o", out, os.path.join(CSRC, source)],
+                                       capture_output=True, text=True)
+        with concurrent.futures.ThreadPoolExecutor(max_workers=4) as pool:
+            done = list(pool.map(compile_one, SOURCES))
+        results = [res for _, res in done]
+        if all(res.returncode == 0 for res in results):
+            results.append(subprocess.run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *[out for out, _ in done]],
+                                          capture_output=True, text=True))
+    for res in results:
+        if verbose or res.returncode != 0:
+            print(res.stdout)
+            print(res.stderr)
+        if res.returncode != 0:
+            raise RuntimeError("hipcc failed building libadacomp.so")
     return LIB
 
 
