@@ -121,7 +121,7 @@ template <typename T, int TPR, int FLOW> __global__ __launch_bounds__(kBackThrea
 {
     constexpr uint32_t TEAMS = kBackThreads / TPR, COLS = TPR * 8;
     __shared__ float room[2][2][16];
-    __shared__ float sums[TEAMS > 1 ? TEAMS * COLS : 1];
+    __shared__ alignas(32) float sums[TEAMS > 1 ? TEAMS * COLS : 8];
     const uint32_t t = threadIdx.x % TPR, team = team_of<TPR>();
     const Drop d = drop_of(a.drop);
     const float per_col = 1.f / float(a.cols);
@@ -198,7 +198,7 @@ template <typename T, int TPR, int FLOW> __global__ __launch_bounds__(kBackThrea
                 out[which * a.pitch + c] = s;
             }
         } else if (t * 8u < a.pitch) {
-            *reinterpret_cast<f32x8 *>(out + which * a.pitch + t * 8u) = which ? dbeta : dgamma;
+            store8(out + which * a.pitch + t * 8u, which ? dbeta : dgamma);
         }
     }
 }
@@ -255,8 +255,8 @@ template <typename T, int V> __global__ __launch_bounds__(kBackThreads) void k_n
     for (int v = 0; v < V; ++v) {
         const uint32_t c = (t + v * TPR) * 8u;
         if (c >= a.pitch) continue;
-        *reinterpret_cast<f32x8 *>(out + c) = dgamma[v];
-        *reinterpret_cast<f32x8 *>(out + a.pitch + c) = dbeta[v];
+        store8(out + c, dgamma[v]);
+        store8(out + a.pitch + c, dbeta[v]);
     }
 }
 

@@ -86,10 +86,10 @@ struct Window {
     }
 };
 
-// The admitted ones of 8 keys, a bit each, of which n > 0 are below the row's limit; mask: their bytes of the mask.
+// The admitted ones of 8 keys, a bit each, of which n are below the row's limit; mask: their bytes of the mask.
 template <bool MASK> __device__ __forceinline__ uint32_t admitted8(uint64_t mask, int n)
 {
-    uint32_t bits = n >= 8 ? 0xFFu : (1u << n) - 1u;
+    uint32_t bits = n >= 8 ? 0xFFu : (1u << max(n, 0)) - 1u;
     if constexpr (MASK) {
         uint32_t keep = 0;
 #pragma unroll
@@ -184,8 +184,9 @@ template <typename T, int TPR, int V, int PHASE, int KIND> __global__ __launch_b
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const int j = int(groups.col(v)), n = r.limit - j;
+                // rounds of which a wave has nothing are left out; its other threads go along, and have nothing admitted
                 p[v] = -kInf;
-                if (n > 0) {
+                if (__any(n > 0)) {
                     const uint32_t here = admitted8<kMasked<KIND>>(kMasked<KIND> ? mask_of(groups, mask[v], v) : 0, n);
                     bits |= here << (8 * v);
                     p[v] = biased8(groups.values(raw[v], v), a, Unit<T>::scale(a), r, Window(r, j), bias, low, high, 0.f);
@@ -204,7 +205,7 @@ template <typename T, int TPR, int V, int PHASE, int KIND> __global__ __launch_b
             float l = 0.f;
 #pragma unroll
             for (int v = 0; v < V; ++v)
-                if (bits >> (8 * v) & 0xFFu) {
+                if (__any(bits >> (8 * v) & 0xFFu)) {
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
                         p[v][k] = Unit<T>::exp(p[v][k] - from);
@@ -248,7 +249,7 @@ template <typename T, int TPR, int V, int PHASE, int KIND> __global__ __launch_b
             groups.store(out + int64_t(i) * a.out.row, [&](int v) {
                 f32x8 y = {};
                 const uint32_t here = bits >> (8 * v) & 0xFFu;
-                if (here) {
+                if (__any(here != 0u)) {
                     y = p[v] * factor;
                     if (here != 0xFFu) {   // a row's NaN stays where it looks
 #pragma unroll
@@ -310,14 +311,16 @@ template <typename T, int TPR, int V, int PHASE, int KIND> __global__ __launch_b
         const bool coarse = !(fabsf(lse2) < 4194304.f);
         const float less = coarse || Unit<T>::kNatural ? 0.f : lse2;
         f32x8 p[V], dp[V];
+        uint32_t admitted = 0;   // 8 places to a group
         float inner = 0.f;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int j = int(groups.col(v)), n = r.limit - j;
             p[v] = 0.f;
             dp[v] = 0.f;
-            if (n > 0) {
+            if (__any(n > 0)) {   // rounds of which a wave has nothing are left out; its other threads go along, and have nothing admitted
                 const uint32_t bits = admitted8<kMasked<KIND>>(kMasked<KIND> ? mask_of(groups, mask[v], v) : 0, n);
+                admitted |= bits << (8 * v);
                 p[v] = biased8(groups.values(raw[v], v), a, Unit<T>::scale(a), r, Window(r, j), bias, bias_low, bias_high, less);
                 if (Unit<T>::kNatural && !coarse) {   // the difference as the formula has it: exact where it is small
 #pragma unroll
@@ -364,11 +367,16 @@ template <typename T, int TPR, int V, int PHASE, int KIND> __global__ __launch_b
         groups.store(o, [&](int v) {
             const int j = int(groups.col(v));
             f32x8 y = {};
-            if (j < r.limit) {
+            if (__any(j < r.limit)) {
+                const uint32_t bits = admitted >> (8 * v) & 0xFFu;
 #pragma unroll
                 for (int k = 0; k < 8; ++k) p[v][k] *= fmaf(dp[v][k], up_factor, -inner);
+                if (bits != 0xFFu) {   // a row's NaN stays where it looks
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) p[v][k] = bits >> k & 1u ? p[v][k] : 0.f;
+                }
                 y = p[v] * a.scale;
-                if (sums) {
+                if (sums && bits) {
                     const Window w(r, j);
                     if (w.above(last) || w.below()) {
                         float e = 0.f;

@@ -438,6 +438,23 @@ def test_softmax_of_infinities_and_lowest_values(A, keys):
         assert torch.all(out[1] == 0) and torch.all(out[2, keys // 2:] == 0) and torch.isfinite(out[[0, 1, 2, 3, 5]].double()).all()
 
 
+@pytest.mark.parametrize("keys", [30, 100, 700, 2000, 5000, 20000, 40000])
+def test_softmax_of_rows_with_nan_is_zero_where_it_does_not_look(A, keys):
+    """A NaN among the admitted scores or gradients of a row reaches the row's admitted places, no other place and no other row."""
+    for dtype in (torch.float32, torch.bfloat16):
+        c = Case(A, (1, 2, 5, keys, False, keys // 2, [keys - 3], "row", 32, 128), dtype, 0.1, wild=False)
+        first = int(c.ok[0, 0, 1].nonzero()[0])
+        c.g_scores[0, 0, 1, first] = float("nan")
+        c.g_dprobs[0, 1, 2, int(c.ok[0, 1, 2].nonzero()[0])] = float("nan") if not c.f.dim() or c.f[0, 1, 2, int(c.ok[0, 1, 2].nonzero()[0])] else 0.0
+        lse = torch.empty(1, 2, 5, device=DEV)
+        A.adacomp_bias_softmax_forward(c.g_scores, c.bias, c.out, c.ws, lse=lse, **c.options)
+        out, ok = c.out.cpu().double(), c.ok
+        assert torch.all(out[~ok] == 0) and torch.isnan(lse.cpu()).sum() == 1 and torch.isnan(out).any(-1).sum() == 1
+        A.adacomp_bias_softmax_backward(c.g_scores, c.bias, lse, c.g_dprobs, c.out, None, c.ws, **c.options)
+        out = c.out.cpu().double()
+        assert torch.all(out[~ok] == 0) and torch.isnan(out).any(-1).sum() <= 2 and torch.isnan(out[0, 0, 1][ok[0, 0, 1]]).all()
+
+
 def test_softmax_of_nothing(A):
     bias = A.RelativeBias(torch.zeros(8, 3, device=DEV), torch.zeros(9, dtype=torch.int32, device=DEV))
     ws = torch.empty(1024, dtype=torch.uint8, device=DEV)
@@ -532,6 +549,48 @@ def test_large_calls_agree_with_small_ones(A):
         A.adacomp_bias_softmax_backward(s, bias, lse, up, out, whole, ws, key_lengths=lengths, **drop)
         # the same terms in another order: |e| is below 5 P, and a row's P add up to 1
         assert (whole.double() - small.double()).abs().max() <= U * 400 * batch * queries * 10
+
+
+def test_more_rows_than_one_launch_takes(A):
+    """Dropout beyond 2^30 groups and norm beyond 2^22 rows, which go in several launches, and more (batch, head) pairs than a launch of the
+    forward softmax has workgroups: what lies behind the seams is what calls of those rows give."""
+    rows = (1 << 30) + 700
+    x = torch.ones(rows, 1, dtype=torch.bfloat16, device=DEV)
+    A.adacomp_dropout(x, x, A.Dropout(0.5, 12, 13))
+    for first in (0, (1 << 30) - 300, rows - 500):
+        assert torch.equal(x[first:first + 500, 0].cpu().double(), R.factors(500, 1, 0.5, 12, 13, first)[:, 0])
+    del x
+    rows, cols = (1 << 22) + 700, 9
+    g = torch.Generator(device=DEV).manual_seed(3)
+    x = torch.randn(rows, cols, generator=g, device=DEV)
+    y, mean, rstd = torch.empty_like(x), torch.empty(rows, device=DEV), torch.empty(rows, device=DEV)
+    A.adacomp_norm_forward(x, None, None, y, mean=mean, rstd=rstd)
+    part, part_mean, part_rstd = torch.empty(900, cols, device=DEV), torch.empty(900, device=DEV), torch.empty(900, device=DEV)
+    for first in (0, (1 << 22) - 300, rows - 900):
+        A.adacomp_norm_forward(x[first:first + 900], None, None, part, mean=part_mean, rstd=part_rstd)
+        assert torch.equal(y[first:first + 900], part) and torch.equal(mean[first:first + 900], part_mean) and torch.equal(rstd[first:first + 900], part_rstd)
+    A.adacomp_norm_forward(x, None, None, y, dropout=A.Dropout(0.5, 1, 2), z=y.new_empty(y.shape), mean=mean)
+    first = (1 << 22) - 300
+    kept = x[first:first + 900].cpu().double() * R.factors(900, cols, 0.5, 1, 2, first)
+    within(mean[first:first + 900], kept.mean(-1), U * DEEP * kept.abs().mean(-1), "mean of what dropout leaves")
+    batch, keys = (1 << 20) + 500, 11
+    s = torch.randn(batch, 1, 1, keys, generator=g, device=DEV)
+    bias = A.RelativeBias(torch.randn(8, 1, generator=g, device=DEV), torch.from_numpy(A.adacomp_relative_buckets(8, 6, True)).to(DEV))
+    ws = torch.empty(A.adacomp_bias_softmax_workspace_bytes(batch, 1, 1, keys, 6), dtype=torch.uint8, device=DEV)
+    probs, part = torch.empty_like(s), torch.empty_like(s[:900])
+    A.adacomp_bias_softmax_forward(s, bias, probs, ws, query_start=5)
+    for first in (0, batch - 900):
+        A.adacomp_bias_softmax_forward(s[first:first + 900], bias, part, ws, query_start=5)
+        assert torch.equal(probs[first:first + 900], part)
+    lse, ds, dtable = torch.empty(batch, 1, 1, device=DEV), torch.empty_like(s), torch.empty(8, 1, device=DEV)
+    A.adacomp_bias_softmax_forward(s, bias, probs, ws, query_start=5, lse=lse)
+    A.adacomp_bias_softmax_backward(s, bias, lse, s, ds, dtable, ws, query_start=5)
+    p = probs.double()
+    e = p * (s.double() - (p * s.double()).sum(-1, keepdim=True))
+    bucket = bias.map.long()[(torch.arange(keys, device=DEV) - 5).clamp(-6, 6) + 6]
+    want = torch.zeros(8, dtype=torch.float64, device=DEV).index_add_(0, bucket, e.sum((0, 1, 2)))
+    size = torch.zeros(8, dtype=torch.float64, device=DEV).index_add_(0, bucket, (p * (s.double().abs() + 5)).sum((0, 1, 2)))
+    assert torch.all((dtable[:, 0].double() - want).abs() <= U * 400 * size)   # a thread adds up to 25 of the rows
 
 
 # ---- gradients against differences of the kernels' own results -----------------------------------------------------
