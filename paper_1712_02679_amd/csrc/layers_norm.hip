@@ -1,11 +1,16 @@
 // layers_norm.hip -- kernels of dropout and layer norm (adacomp_layers.h).
+//
+// All of them read each input once and write each result once (rows of more than 8192 columns are read twice in the backward pass, the
+// second time from the caches), and are bound by memory in large calls, by one chain of load, reductions and store in small ones.
+// 16384 x 4096 bf16: residual sum with dropout 64 us (6.3 TB/s), norm with both and its z 93 us (5.8 TB/s), backward with both 118 us (5.7 TB/s,
+// of which k_norm_reduce 4); one row of 4096 3.4 us; 6007 x 577 f32 8.6 and 15 us.
 #include "layers_device.h"
 
 namespace adacomp {
 
 // ---- dropout ------------------------------------------------------------------------------------------------------
-// y = [residual +] D(x).  One group of 8 columns to a thread and round; rows are cut into groups of their own, so that a
-// group is one counter wherever it lies.
+// y = [residual +] D(x).  One group of 8 columns to a thread (2 and 4 were slower: 71.5, 76.4 us to 70.0 at 16384 x 4096 bf16, and 3.6, 5.2 to 2.6 at
+// 100 x 500 f32); rows are cut into groups of their own, so that a group is one counter wherever it lies.
 
 template <typename T, bool ONCE> __global__ __launch_bounds__(256) void k_dropout(DropoutLaunch a)
 {
@@ -41,7 +46,9 @@ template <typename T, bool ONCE> __global__ __launch_bounds__(256) void k_dropou
 }
 
 // ---- layer norm, forward ------------------------------------------------------------------------------------------
-// A row stays in the registers of its threads: mean first, then the squared distances from it.
+// A row stays in the registers of its threads: mean first, then the squared distances from it.  One row to a team of threads and no
+// loop: workgroups that walk over rows with the next one on its way were slower (4096 columns 108 us to 98), and so was fetching gamma and
+// beta ahead of the sums, which takes the registers of three waves in eight (bf16 59 / 61 us without residual).
 
 // Over the TPR threads of a row.  A row of several waves joins their sums in `room`, of which the next call takes another one.
 template <int TPR> __device__ __forceinline__ float over_row(float x, float *room, uint32_t team)
