@@ -11,7 +11,7 @@
  *   - dtype is the type of the tensors that have one value per row and column; parameters, their
  *     gradients, statistics and the arithmetic are float32.  A result is rounded once, to nearest even.
  *   - Every tensor's last dimension is contiguous; the other strides are in elements.  Addresses need
- *     the alignment of one element, parameters, statistics and workspaces that of 4 bytes.
+ *     the alignment of one element, parameters, statistics and index arrays that of 4 bytes, workspaces 16.
  *   - An output may be the same buffer as an input of the same strides; otherwise buffers must not overlap.
  *   - Calls only launch kernels on hip_stream: no allocation, no copy, no synchronisation; they can be
  *     captured in a graph.  The device is the one current in the calling thread.
@@ -94,7 +94,7 @@ size_t adacomp_norm_workspace_bytes(uint64_t rows, uint64_t cols);
  *        without dropout, when it would be dz
  *   dgamma = sum over rows of dy h, dbeta = sum over rows of dy; either may be NULL.  accumulate != 0 adds
  *        to what is there, 0 overwrites.
- * gamma NULL: ones.  The workspace is 16-byte aligned. */
+ * gamma NULL: ones. */
 int adacomp_norm_backward(const adacomp_norm_t *norm, const void *dy, const void *dz_add, const void *z, const float *mean,
                           const float *rstd, const float *gamma, const adacomp_dropout_t *dropout, void *dz, void *dx,
                           float *dgamma, float *dbeta, int accumulate, void *workspace, size_t workspace_bytes,
@@ -155,7 +155,8 @@ int adacomp_bias_softmax_forward(const adacomp_bias_softmax_t *op, const adacomp
  *   dP = D(dprobs);  e = P (dP - sum over the row of P dP);  dscores = scale e, zeros where not admitted;
  *   dtable[k, h] = sum of e over all places of head h whose distance has bucket k.
  * dtable [n_buckets, heads] may be NULL; accumulate != 0 adds to what is there, 0 overwrites.
- * The same op and dropout as in the forward pass. */
+ * The same op and dropout as in the forward pass.  lse is a float32, and P as exact as that allows: where it is beyond 2^22 in
+ * magnitude (rows of a type's lowest value, say) P is 1 at the places that are as near to it as its rounding. */
 int adacomp_bias_softmax_backward(const adacomp_bias_softmax_t *op, const adacomp_view_t *scores, const float *lse,
                                   const adacomp_view_t *dprobs, const adacomp_dropout_t *dropout,
                                   const adacomp_view_t *dscores, float *dtable, int accumulate, void *workspace,
