@@ -59,13 +59,27 @@ struct SoftmaxRoom {
     size_t all() const { return stats + sums; }
 };
 
-static SoftmaxRoom softmax_room(uint64_t batch, uint64_t heads, uint64_t queries, uint32_t keys, uint32_t distance, bool backward)
+static SoftmaxRoom softmax_room(const SoftmaxArgs &a, const SoftmaxForm &form, bool backward)
 {
-    const SoftmaxForm form = softmax_form(keys, distance, backward);
     SoftmaxRoom room = {0, 0};
-    if (form.parts > 1u) room.stats = pad256(size_t(batch * heads * queries) * form.parts * 8u);
-    if (backward && heads) room.sums = pad256(size_t(heads) * softmax_back_groups_most(batch * queries, uint32_t(heads), form) * (2u * distance + 1u) * 4u);
+    if (form.parts > 1u) room.stats = pad256(size_t(a.batch) * a.heads * a.queries * form.parts * 8u);
+    if (backward && a.heads) room.sums = pad256(size_t(a.heads) * softmax_back_groups_most(uint64_t(a.batch) * a.queries, a.heads, form) * a.places * 4u);
     return room;
+}
+
+// The distances key - query that a call can have, as far as the host knows, in the map's numbering.
+static void softmax_places(SoftmaxArgs &a)
+{
+    const int64_t far = a.distance, ends = 2 * far;
+    int64_t low = 0, high = ends;
+    if (!a.query_starts) {
+        low = std::min(std::max(far - (int64_t(a.query_start) + a.queries - 1), int64_t(0)), ends);
+        high = std::min(std::max(far + int64_t(a.keys) - 1 - a.query_start, low), ends);
+    }
+    if (a.causal) high = std::min(high, far);   // no key behind its query
+    low = std::min(low, high);
+    a.first_place = uint32_t(low);
+    a.places = uint32_t(high - low + 1);
 }
 
 // What the two softmax calls check alike.
@@ -94,6 +108,7 @@ static int softmax_args(const adacomp_bias_softmax_t *op, const adacomp_view_t *
     a.query_start = op->query_start;
     a.scale = op->scale;
     a.scale2 = float(double(op->scale) * 1.4426950408889634);
+    softmax_places(a);
     return ADACOMP_OK;
 }
 
@@ -221,8 +236,11 @@ int adacomp_relative_buckets(uint32_t n_buckets, uint32_t max_distance, int both
 size_t adacomp_bias_softmax_workspace_bytes(uint32_t batch, uint32_t heads, uint32_t queries, uint32_t keys, uint32_t max_distance)
 {
     if (!softmax_sizes(batch, heads, queries, keys, max_distance)) return 0;
-    return std::max<size_t>(256u, std::max(softmax_room(batch, heads, queries, keys, max_distance, false).all(),
-                                           softmax_room(batch, heads, queries, keys, max_distance, true).all()));
+    // in whatever form a call goes: parts of rows as the keys make them, sums of every distance for as many workgroups as there can be
+    const uint32_t parts = softmax_form(keys, 1, false).parts;
+    const size_t rows_of_head = size_t(batch) * queries * parts, rows = rows_of_head * heads;
+    const size_t groups = heads ? std::min<size_t>(rows_of_head, std::max(1u, kMostResident * kComputeUnits / heads)) : 0u;
+    return std::max<size_t>(256u, (parts > 1u ? pad256(rows * 8u) : 0u) + pad256(groups * heads * (2u * max_distance + 1u) * 4u));
 }
 
 int adacomp_bias_softmax_forward(const adacomp_bias_softmax_t *op, const adacomp_view_t *scores, const adacomp_view_t *probs, float *lse,
@@ -233,11 +251,12 @@ int adacomp_bias_softmax_forward(const adacomp_bias_softmax_t *op, const adacomp
     if (int rc = view_args(probs, op, element_bytes(op->dtype), true, a.out)) return rc;
     if (!aligned(lse, 4)) return ADACOMP_EALIGN;
     if (uint64_t(a.batch) * a.heads * a.queries == 0) return ADACOMP_OK;
-    const SoftmaxRoom room = softmax_room(a.batch, a.heads, a.queries, a.keys, a.distance, false);
+    const SoftmaxForm form = softmax_form(a.keys, a.places, false);
+    const SoftmaxRoom room = softmax_room(a, form, false);
     if (int rc = workspace_check(workspace, workspace_bytes, room.all())) return rc;
     a.lse = lse;
     a.part_stats = static_cast<float *>(workspace);
-    return launch_softmax_forward(a, op->dtype, softmax_form(a.keys, a.distance, false), hip_stream);
+    return launch_softmax_forward(a, op->dtype, form, hip_stream);
 }
 
 int adacomp_bias_softmax_backward(const adacomp_bias_softmax_t *op, const adacomp_view_t *scores, const float *lse,
@@ -252,8 +271,8 @@ int adacomp_bias_softmax_backward(const adacomp_bias_softmax_t *op, const adacom
     if (!aligned(lse, 4) || !aligned(dtable, 4)) return ADACOMP_EALIGN;
     if (a.heads == 0) return ADACOMP_OK;
     const uint64_t rows_of_head = uint64_t(a.batch) * a.queries;
-    const SoftmaxForm form = softmax_form(a.keys, a.distance, true);
-    SoftmaxRoom room = softmax_room(a.batch, a.heads, a.queries, a.keys, a.distance, true);
+    const SoftmaxForm form = softmax_form(a.keys, a.places, true);
+    SoftmaxRoom room = softmax_room(a, form, true);
     if (!dtable) room.sums = 0;
     char *base = static_cast<char *>(workspace);
     uint32_t groups = 0;
@@ -266,7 +285,7 @@ int adacomp_bias_softmax_backward(const adacomp_bias_softmax_t *op, const adacom
         if (int rc = launch_softmax_backward(a, op->dtype, form, groups, hip_stream)) return rc;
     }
     if (!dtable) return ADACOMP_OK;
-    const BiasReduce r = {reinterpret_cast<const float *>(base + room.stats), a.map, dtable, a.heads, groups, a.distance, a.n_buckets, accumulate != 0};
+    const BiasReduce r = {reinterpret_cast<const float *>(base + room.stats), a.map + a.first_place, dtable, a.heads, groups, a.places, a.n_buckets, accumulate != 0};
     return launch_bias_reduce(r, hip_stream);
 }
 

@@ -85,9 +85,10 @@ struct SoftmaxArgs {
     const float *table;
     float *lse;         // written by the forward pass, read by the backward pass
     float *part_stats;  // [rows][parts][2], of a row cut into parts: (maximum, sum) or (sum of P dP, -)
-    float *bias_sums;   // [heads][groups][2 D + 1]: sums of e by distance, of a workgroup's rows
+    float *bias_sums;   // [heads][groups][places]: sums of e by distance, of a workgroup's rows
     uint32_t batch, heads, queries, keys, causal;
     uint32_t n_buckets, distance;
+    uint32_t first_place, places;   // of the map's 2 D + 1 entries, those that the call can need
     int32_t query_start;
     float scale2, scale;        // scale log2(e), scale
     uint32_t rows_per_wg, wgs_per_head;   // forward: consecutive rows of a workgroup, workgroups to a (batch, head); backward: workgroups to a head
@@ -97,9 +98,9 @@ struct SoftmaxArgs {
 
 struct BiasReduce {
     const float *bias_sums;
-    const int32_t *map;
+    const int32_t *map;   // at the first place
     float *dtable;
-    uint32_t heads, groups, distance, n_buckets, accumulate;
+    uint32_t heads, groups, places, n_buckets, accumulate;
 };
 
 // How a call goes: whole rows, or rows cut into parts (two launches)
@@ -107,7 +108,9 @@ struct SoftmaxForm {
     RowForm row;
     uint32_t parts;   // 1: whole rows
 };
-SoftmaxForm softmax_form(uint32_t keys, uint32_t distance, bool backward);
+SoftmaxForm softmax_form(uint32_t keys, uint32_t places, bool backward);
+// Most workgroups to a head that the backward pass takes in a form; in any form, at most a row each and this many in all.
+constexpr uint32_t kMostResident = 6;   // workgroups on a compute unit; of kernels of which 7 should fit, 6 are faster (16 x 1000 x 1000 x 16 bf16 309 / 373 us)
 uint32_t softmax_back_groups_most(uint64_t rows_of_head, uint32_t heads, const SoftmaxForm &form);
 
 int launch_softmax_forward(const SoftmaxArgs &a, uint32_t dtype, const SoftmaxForm &form, void *stream);

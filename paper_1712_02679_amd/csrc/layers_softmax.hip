@@ -19,12 +19,12 @@ namespace adacomp {
 constexpr float kLog2e = 1.4426950408889634f, kLog2eRest = float(1.4426950408889634 - double(kLog2e)), kLn2 = 0.6931471805599453f;
 constexpr float kInf = __builtin_huge_valf();
 
-// The bias by distance index x = key - query + D, and the sums of its gradient, lie in LDS with 8 more places at either end, so that a
-// group of 8 keys that reaches over an end needs no clamp.  Place X = x + 8 is in cell X + X / 8: neighbouring lanes are 8 places
+// The bias by distance index x = key - query + D, as far as a call can have that distance (a.places of them from a.first_place on), and the sums of its
+// gradient, lie in LDS with 8 more places at either end, so that a group of 8 keys that reaches over an end needs no clamp.  Place X = x + 8 is in cell X + X / 8: neighbouring lanes are 8 places
 // and so 9 cells apart, in different banks.  Groups begin at multiples of 8 keys, so X % 8 is the same for a whole row.
 constexpr uint32_t kGuard = 8;
 __host__ __device__ constexpr uint32_t cell(uint32_t X) { return X + (X >> 3); }
-__host__ __device__ constexpr uint32_t cells(uint32_t distance) { return (cell(2u * distance + 2u * kGuard) + 3u) & ~3u; }
+__host__ __device__ constexpr uint32_t cells(uint32_t places) { return (cell(places - 1u + 2u * kGuard) + 3u) & ~3u; }
 
 // What exponents are made of.  16-bit tensors: everything in units of log2, one v_exp_f32 a value, whose argument has been rounded
 // where it is about 10: 5e-7 of the result at most, far below their own rounding.  32-bit ones: natural units, as in the formula, and the
@@ -47,9 +47,9 @@ template <typename T> struct Unit {
 // A workgroup's copy of its head's bias.
 template <typename T> __device__ __forceinline__ void stage_bias(float *bias, const SoftmaxArgs &a, uint32_t head)
 {
-    const int last = 2 * int(a.distance);
+    const int last = int(a.places) - 1;
     for (int X = threadIdx.x; X <= last + 2 * int(kGuard) - 1; X += blockDim.x) {
-        const int32_t b = min(max(a.map[min(max(X - int(kGuard), 0), last)], 0), int32_t(a.n_buckets) - 1);
+        const int32_t b = min(max(a.map[a.first_place + min(max(X - int(kGuard), 0), last)], 0), int32_t(a.n_buckets) - 1);
         bias[cell(X)] = Unit<T>::from_natural(a.table[uint64_t(b) * a.heads + head]);
     }
 }
@@ -70,7 +70,7 @@ __device__ __forceinline__ Row row_of(const SoftmaxArgs &a, uint32_t b, uint32_t
     if (a.causal) limit = min(limit, at + 1);
     r.limit = int(max(limit, int64_t(0)));
     // keys are below 2^30: a shift beyond these bounds is beyond D for every key either way
-    r.shift = int(min(max(int64_t(a.distance + kGuard) - at, -(int64_t(1) << 30) - 8192), int64_t(1) << 30));
+    r.shift = int(min(max(int64_t(a.distance + kGuard - a.first_place) - at, -(int64_t(1) << 30) - 8192), int64_t(1) << 30));
     r.mask = a.mask.data ? static_cast<const uint8_t *>(a.mask.data) + int64_t(b) * a.mask.batch + int64_t(h) * a.mask.head + int64_t(i) * a.mask.row : nullptr;
     return r;
 }
@@ -124,7 +124,7 @@ template <typename G> __device__ __forceinline__ uint64_t mask_of(const G &group
 __device__ __forceinline__ f32x8 biased8(f32x8 s, const SoftmaxArgs &a, float scale, const Row &r, const Window &w, const float *bias, float low, float high, float less)
 {
     f32x8 t;
-    const int last = 2 * int(a.distance);
+    const int last = int(a.places) - 1;
     if (w.above(last) || w.below()) {
         const float b = (w.below() ? low : high) - less;
 #pragma unroll
@@ -177,7 +177,7 @@ template <typename T, int TPR, int V, int PHASE, int KIND> __global__ __launch_b
         if (block != blockIdx.x) __syncthreads();   // the rows before are done with the bias
         stage_bias<T>(bias, a, h);
         __syncthreads();
-        const float low = bias[0], high = bias[cell(2u * a.distance + kGuard)];
+        const float low = bias[0], high = bias[cell(a.places - 1u + kGuard)];
         for (uint32_t i = first + team; i < end; i += TEAMS) {
             const Row r = next;
             const RowGroups<T, TPR, V, KIND == ONCE ? int(ALL_PAST) : kFlow<T>, TPR == 8 || KIND == SHORT> groups = {again(t), again_uniform(a.keys), base};
@@ -276,8 +276,8 @@ template <typename T, int TPR, int V, int PHASE, int KIND> __global__ __launch_b
     extern __shared__ float lds[];
     __shared__ float room[2][16];
     const uint32_t t = threadIdx.x % TPR, team = team_of<TPR>();
-    const uint32_t size = cells(a.distance);
-    const int last = 2 * int(a.distance);
+    const uint32_t size = cells(a.places);
+    const int last = int(a.places) - 1;
     float *bias = lds, *acc = lds + size * (1u + team);   // every team has sums of its own
     const bool sums = PHASE != STATS && a.bias_sums;
     const uint32_t h = blockIdx.x / a.wgs_per_head, group = blockIdx.x - h * a.wgs_per_head;
@@ -431,11 +431,11 @@ template <typename T, int TPR, int V, int PHASE, int KIND> __global__ __launch_b
 // workgroups have for them, always in the same order.
 __global__ __launch_bounds__(1024) void k_bias_reduce(BiasReduce a)
 {
-    extern __shared__ uint16_t mine[];   // [2 D + 1]
+    extern __shared__ uint16_t mine[];   // [places]
     __shared__ float room[16];
     __shared__ uint32_t found_room;
     constexpr uint32_t AHEAD = 8;        // loads on their way
-    const uint32_t n = 2u * a.distance + 1u, h = blockIdx.x, bucket = blockIdx.y;
+    const uint32_t n = a.places, h = blockIdx.x, bucket = blockIdx.y;
     if (threadIdx.x < 64u) {
         const uint32_t lane = threadIdx.x;
         uint32_t found = 0;
@@ -480,17 +480,16 @@ static int check_launch() { return hipGetLastError() == hipSuccess ? ADACOMP_OK 
 
 constexpr uint32_t kPartThreads = 256, kPartGroups = 4, kPartKeys = kPartThreads * kPartGroups * 8u;
 constexpr uint32_t kLdsMost = 40u << 10;      // of a workgroup: four of them fit a compute unit
-constexpr uint32_t kMostResident = 6;         // workgroups on a compute unit; of kernels of which 7 should fit, 6 are faster (16 x 1000 x 1000 x 16 bf16 309 / 373 us)
 constexpr uint32_t kMostWorkgroups = 1u << 20;   // of a launch, which has fewer than 2^32 threads; what is left is walked over
 
 // Threads to a row and groups of 8 keys to a thread.  The LDS that the sums take is one bound, registers are another.  Few threads with up to 4 groups, since what a row costs whatever its length is then
 // paid by few waves; in the backward pass, where a group takes twice the registers, 2 in short rows.  bf16, us, with 1 / 2 / 4 groups: forward
 // 512 x 100 x 100 x 16 151 / 101 / 111, 256 x 200 x 200 x 16 240 / 201 / 147, 64 x 512 x 512 x 16 298 / 209 / 195, 4 x 512 x 6000 x 16 395 / 187 / 158;
 // backward 202 / 154 / 305, 384 / 284 / 444, 509 / 376 / 400, 422 / 497 / 237.  Longer rows are cut into parts, and read twice.
-SoftmaxForm softmax_form(uint32_t keys, uint32_t distance, bool backward)
+SoftmaxForm softmax_form(uint32_t keys, uint32_t places, bool backward)
 {
     if (backward) {   // every row that a workgroup has in hand has its sums by distance in LDS, beside the bias
-        const uint32_t copies = kLdsMost / (4u * cells(distance)) - 1u;
+        const uint32_t copies = kLdsMost / (4u * cells(places)) - 1u;
         keys = std::max(keys, copies >= 32u ? 0u : copies >= 16u ? 129u : copies >= 8u ? 257u : copies >= 4u ? 513u : 2049u);
     }
     if (keys <= 64u) return {{8, 1}, 1};
@@ -515,7 +514,6 @@ static uint32_t back_groups(uint64_t rows_of_head, uint32_t heads, const Softmax
     return rounds ? uint32_t((all + rounds - 1u) / rounds) : 0u;   // all with as many rows, up to one
 }
 
-// Most of them that a call can have: what the workspace has room for.
 uint32_t softmax_back_groups_most(uint64_t rows_of_head, uint32_t heads, const SoftmaxForm &f) { return back_groups(rows_of_head, heads, f, kMostResident); }
 
 // Picks the kernel of a form and type and calls launch(kernel, phase) with it; twice where rows are cut into parts.
@@ -576,7 +574,7 @@ template <typename T, int TPR, int V, int PHASE, int KIND> struct KBackward { st
 // to lay out, and fewer where that leaves compute units without work.
 static uint32_t rows_of_team(const SoftmaxArgs &a, const SoftmaxForm &f)
 {
-    const uint32_t teams = f.row.teams(), wanted = std::max(24576u, 8u * (2u * a.distance + 1u));
+    const uint32_t teams = f.row.teams(), wanted = std::max(24576u, 8u * a.places);
     uint32_t rows = std::min(std::max(wanted / (teams * std::max(a.keys, 1u)), teams == 1u ? 4u : 2u), 16u);
     while (rows > 1u && uint64_t(a.batch) * a.heads * ((a.queries + rows * teams - 1u) / (rows * teams)) < 4u * kComputeUnits) --rows;
     return rows;
@@ -591,7 +589,7 @@ int launch_softmax_forward(const SoftmaxArgs &args, uint32_t dtype, const Softma
     const uint64_t blocks = uint64_t(a.batch) * a.heads * a.wgs_per_head * f.parts;
     const dim3 grid(uint32_t(std::min<uint64_t>(blocks, kMostWorkgroups))), wg(f.row.workgroup());
     return with_kernel<KForward>(a, dtype, f, [&](auto kernel) {
-        hipLaunchKernelGGL(kernel.value, grid, wg, 4u * cells(a.distance), static_cast<hipStream_t>(stream), a);
+        hipLaunchKernelGGL(kernel.value, grid, wg, 4u * cells(a.places), static_cast<hipStream_t>(stream), a);
     });
 }
 
@@ -599,7 +597,7 @@ int launch_softmax_backward(const SoftmaxArgs &args, uint32_t dtype, const Softm
 {
     SoftmaxArgs a = args;
     a.row_parts = f.parts;
-    const uint32_t lds = 4u * cells(a.distance) * (1u + (a.bias_sums ? f.row.teams() : 0u)), threads = f.row.workgroup();
+    const uint32_t lds = 4u * cells(a.places) * (1u + (a.bias_sums ? f.row.teams() : 0u)), threads = f.row.workgroup();
     return with_kernel<KBackward>(a, dtype, f, [&](auto kernel) {
         // how many of the kernel's workgroups a compute unit holds with so much LDS: asked once, and again if the LDS differs
         static std::atomic<uint64_t> known{0};
@@ -617,7 +615,7 @@ int launch_softmax_backward(const SoftmaxArgs &args, uint32_t dtype, const Softm
 
 int launch_bias_reduce(const BiasReduce &a, void *stream)
 {
-    const uint32_t lds = (2u * (2u * a.distance + 1u) + 15u) & ~15u;
+    const uint32_t lds = (2u * a.places + 15u) & ~15u;
     hipLaunchKernelGGL(k_bias_reduce, dim3(a.heads, a.n_buckets), dim3(1024), lds, static_cast<hipStream_t>(stream), a);
     return check_launch();
 }
