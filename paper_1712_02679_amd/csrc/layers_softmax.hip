@@ -1,7 +1,7 @@
 // layers_softmax.hip -- kernels of the masked softmax with a learned relative position bias (adacomp_layers.h).
 //
 // The bias of a place depends on its head and on clamp(key - query, -D, D) alone, so a workgroup, whose rows all belong to one
-// head, lays out the head's 2 D + 1 values in LDS once, and a place costs one LDS read; groups of 8 keys that lie
+// head, lays out the head's values in LDS once, for the distances that the call can have, and a place costs one LDS read; groups of 8 keys that lie
 // beyond D on one side cost none.  The gradient goes the same way back: sums by distance, added up in LDS (inside a row all
 // distances differ, so no two threads of a row meet, and rows follow each other), those beyond D in registers; k_bias_reduce
 // adds the workgroups' sums and only then turns distances into buckets.
@@ -489,7 +489,11 @@ constexpr uint32_t kMostWorkgroups = 1u << 20;   // of a launch, which has fewer
 SoftmaxForm softmax_form(uint32_t keys, uint32_t places, bool backward)
 {
     if (backward) {   // every row that a workgroup has in hand has its sums by distance in LDS, beside the bias
+        // and the rows get as many threads as leave room for that, with one group where it does: 64 x 16 x 600 x 250 with distances up to 800 takes
+        // 339 us in bf16 and 386 with two groups to a thread, 32 x 16 x 1500 x 400 691 and 730
         const uint32_t copies = kLdsMost / (4u * cells(places)) - 1u;
+        if (copies < 16u && copies >= 8u && keys <= 256u) return {{32, 1}, 1};
+        if (copies < 8u && copies >= 4u && keys <= 512u) return {{64, 1}, 1};
         keys = std::max(keys, copies >= 32u ? 0u : copies >= 16u ? 129u : copies >= 8u ? 257u : copies >= 4u ? 513u : 2049u);
     }
     if (keys <= 64u) return {{8, 1}, 1};
@@ -534,7 +538,7 @@ static int with_kernel(const SoftmaxArgs &a, uint32_t dtype, const SoftmaxForm &
             if (dtype == ADACOMP_DTYPE_BF16) launch(std::integral_constant<void (*)(SoftmaxArgs), K<bf16, TPR, V, PHASE, KIND>::kernel>());
             else launch(std::integral_constant<void (*)(SoftmaxArgs), K<f16, TPR, V, PHASE, KIND>::kernel>());
         };
-        if constexpr (BACK && TPR > 8 && V == 2 && PHASE == WHOLE)
+        if constexpr (BACK && TPR > 8 && V <= 2 && PHASE == WHOLE)
             if (a.keys < 8u) return of(std::integral_constant<int, SHORT>());
         if constexpr (BACK && V * TPR >= 256 && PHASE == WHOLE)
             if (once) return of(std::integral_constant<int, ONCE>());
@@ -554,6 +558,8 @@ static int with_kernel(const SoftmaxArgs &a, uint32_t dtype, const SoftmaxForm &
     case 8 * 8 + 4: if constexpr (!BACK) go(FormOf<8, 4>(), Whole()); break;
     case 16 * 8 + 2: if constexpr (BACK) go(FormOf<16, 2>(), Whole()); break;
     case 16 * 8 + 4: if constexpr (!BACK) go(FormOf<16, 4>(), Whole()); break;
+    case 32 * 8 + 1: if constexpr (BACK) go(FormOf<32, 1>(), Whole()); break;
+    case 64 * 8 + 1: if constexpr (BACK) go(FormOf<64, 1>(), Whole()); break;
     case 32 * 8 + 2: if constexpr (BACK) go(FormOf<32, 2>(), Whole()); break;
     case 32 * 8 + 4: if constexpr (!BACK) go(FormOf<32, 4>(), Whole()); break;
     case 64 * 8 + 2: if constexpr (BACK) go(FormOf<64, 2>(), Whole()); break;
