@@ -141,8 +141,10 @@ enum Phase { WHOLE, STATS, WRITE };
 // MASKED: with a mask.  SHORT: rows shorter than a group, with or without one, in forms of more than 8 threads to a row, which only the
 // backward pass gives to such rows, where the distances are many.
 // ONCE: large inputs without a mask, in whole lines, past the caches.
-enum Kind { PLAIN, MASKED, SHORT, ONCE };
-template <int KIND> constexpr bool kMasked = KIND == MASKED || KIND == SHORT;
+// MERGED, without a mask and with one: workgroups of the forward pass share out a head's rows of all sequences instead of one sequence's.
+enum Kind { PLAIN, MASKED, SHORT, ONCE, MERGED, MERGED_MASKED };
+template <int KIND> constexpr bool kMasked = KIND == MASKED || KIND == SHORT || KIND == MERGED_MASKED;
+template <int KIND> constexpr bool kMerged = KIND == MERGED || KIND == MERGED_MASKED;
 
 // ---- forward ------------------------------------------------------------------------------------------------------
 
@@ -155,22 +157,29 @@ template <typename T, int TPR, int V, int PHASE, int KIND> __global__ __launch_b
     const uint32_t t = threadIdx.x % TPR, team = team_of<TPR>();
     const Drop d = drop_of(a.drop);
     uint32_t turn = 0;
-    const uint64_t blocks = uint64_t(a.batch) * a.heads * a.wgs_per_head * a.row_parts;
+    const uint64_t blocks = uint64_t(kMerged<KIND> ? 1u : a.batch) * a.heads * a.wgs_per_head * a.row_parts;
     for (uint64_t block = blockIdx.x; block < blocks; block += gridDim.x) {
         uint32_t unit = uint32_t(block), part = 0;
         if constexpr (PHASE != WHOLE) { unit = uint32_t(block / a.row_parts); part = uint32_t(block - uint64_t(unit) * a.row_parts); }
         const uint32_t bh = unit / a.wgs_per_head, first = (unit - bh * a.wgs_per_head) * a.rows_per_wg;
-        const uint32_t b = bh / a.heads, h = bh - b * a.heads;
+        uint32_t b = kMerged<KIND> ? 0u : bh / a.heads;
+        const uint32_t h = bh - b * a.heads;
         const T *scores = static_cast<const T *>(a.scores.data) + int64_t(b) * a.scores.batch + int64_t(h) * a.scores.head;
         T *out = static_cast<T *>(const_cast<void *>(a.out.data)) + int64_t(b) * a.out.batch + int64_t(h) * a.out.head;
-        const uint32_t base = part * (TPR * V * 8u), end = min(first + a.rows_per_wg, a.queries);
+        const uint32_t base = part * (TPR * V * 8u), end = min(first + a.rows_per_wg, kMerged<KIND> ? a.batch * a.queries : a.queries);
         raw8<T> raw[V];
         raw8<uint8_t> mask[V];
         Row next = {};
         auto fetch = [&](uint32_t i) {   // a row's scores are on their way while the one before is worked on, the first one's while the bias is laid out
+            const T *s = scores;
+            if constexpr (kMerged<KIND>) {
+                b = i / a.queries;
+                i -= b * a.queries;
+                s += int64_t(b) * a.scores.batch;
+            }
             next = row_of(a, b, h, i);
             const RowGroups<T, TPR, V, KIND == ONCE ? int(ALL_PAST) : kFlow<T>, TPR == 8 || KIND == SHORT> groups = {again(t), again_uniform(a.keys), base};
-            groups.load_below(raw, scores + int64_t(i) * a.scores.row, uint32_t(next.limit));
+            groups.load_below(raw, s + int64_t(i) * a.scores.row, uint32_t(next.limit));
             if constexpr (kMasked<KIND>) load_mask(groups, mask, next);
         };
         if (first + team < end) fetch(first + team);
@@ -180,6 +189,13 @@ template <typename T, int TPR, int V, int PHASE, int KIND> __global__ __launch_b
         const float low = bias[0], high = bias[cell(a.places - 1u + kGuard)];
         for (uint32_t i = first + team; i < end; i += TEAMS) {
             const Row r = next;
+            uint64_t row = uint64_t(bh) * a.queries + i;
+            T *o = out + int64_t(i) * a.out.row;
+            if constexpr (kMerged<KIND>) {
+                const uint32_t q = i - b * a.queries;
+                row = (uint64_t(b) * a.heads + h) * a.queries + q;
+                o = out + int64_t(b) * a.out.batch + int64_t(q) * a.out.row;
+            }
             const RowGroups<T, TPR, V, KIND == ONCE ? int(ALL_PAST) : kFlow<T>, TPR == 8 || KIND == SHORT> groups = {again(t), again_uniform(a.keys), base};
             const Drop dr = again(d);
             f32x8 p[V];
@@ -230,7 +246,6 @@ template <typename T, int TPR, int V, int PHASE, int KIND> __global__ __launch_b
                 for (int w = 0; w < TPR / 64; ++w) total = fmaf(room[turn][1][w], Unit<T>::exp(room[turn][0][w] - from_top), total);
                 turn ^= 1u;
             }
-            const uint64_t row = uint64_t(bh) * a.queries + i;
             if constexpr (PHASE == STATS) {
                 if (threadIdx.x == 0u) {
                     float *to = a.part_stats + (row * a.row_parts + part) * 2u;
@@ -250,7 +265,7 @@ template <typename T, int TPR, int V, int PHASE, int KIND> __global__ __launch_b
             float factor = total == 0.f ? 0.f : Unit<T>::exp(from - (top == -kInf ? 0.f : top)) / total;
             if (a.drop.on) factor *= d.factor;
             if (a.lse && t == 0u && part == 0u) a.lse[row] = total == 0.f ? -kInf : Unit<T>::lse(top, total);
-            groups.store(out + int64_t(i) * a.out.row, [&](int v) {
+            groups.store(o, [&](int v) {
                 f32x8 y = {};
                 const uint32_t here = bits >> (8 * v) & 0xFFu;
                 if (__any(here != 0u)) {
@@ -542,6 +557,8 @@ static int with_kernel(const SoftmaxArgs &a, uint32_t dtype, const SoftmaxForm &
             if (a.keys < 8u) return of(std::integral_constant<int, SHORT>());
         if constexpr (BACK && V * TPR >= 256 && PHASE == WHOLE)
             if (once) return of(std::integral_constant<int, ONCE>());
+        if constexpr (!BACK && PHASE == WHOLE)
+            if (a.merged) return a.mask.data ? of(std::integral_constant<int, MERGED_MASKED>()) : of(std::integral_constant<int, MERGED>());
         if (a.mask.data) of(std::integral_constant<int, MASKED>());
         else of(std::integral_constant<int, PLAIN>());
     };
@@ -576,23 +593,31 @@ static int with_kernel(const SoftmaxArgs &a, uint32_t dtype, const SoftmaxForm &
 template <typename T, int TPR, int V, int PHASE, int KIND> struct KForward { static constexpr bool kBackward = false; static constexpr auto kernel = k_softmax_forward<T, TPR, V, PHASE, KIND>; };
 template <typename T, int TPR, int V, int PHASE, int KIND> struct KBackward { static constexpr bool kBackward = true; static constexpr auto kernel = k_softmax_backward<T, TPR, V, PHASE, KIND>; };
 
-// Rows of a team, one after the other, in a workgroup of the forward pass: about 24000 keys to a workgroup, or 8 times what its bias takes
-// to lay out, and fewer where that leaves compute units without work.
-static uint32_t rows_of_team(const SoftmaxArgs &a, const SoftmaxForm &f)
+// Shares the rows out to workgroups of the forward pass: to a team about 24000 keys, or 8 times what the bias takes to lay out, over the teams,
+// and fewer where that leaves compute units without work.  Sequences of at most a quarter of a workgroup's rows share workgroups, head by head:
+// 8000 x 16 x 17 x 17 in bf16 takes 160 us instead of 305, 4096 x 24 x 1 x 100 takes 18 instead of 148, 1024 x 16 x 60 x 60 takes 87 instead
+// of 89, while 512 x 16 x 100 x 100, whose rows are nearly half of a workgroup's, would take 104 instead of 97.
+static void share_rows(SoftmaxArgs &a, const SoftmaxForm &f)
 {
     const uint32_t teams = f.row.teams(), wanted = std::max(24576u, 8u * a.places);
     uint32_t rows = std::min(std::max(wanted / (teams * std::max(a.keys, 1u)), teams == 1u ? 4u : 2u), 16u);
-    while (rows > 1u && uint64_t(a.batch) * a.heads * ((a.queries + rows * teams - 1u) / (rows * teams)) < 4u * kComputeUnits) --rows;
-    return rows;
+    for (;; --rows) {
+        a.rows_per_wg = teams * rows;
+        a.merged = a.batch > 1u && uint64_t(a.queries) * 4u <= a.rows_per_wg;
+        const uint64_t together = a.merged ? uint64_t(a.batch) * a.queries : a.queries;
+        a.wgs_per_head = uint32_t((together + a.rows_per_wg - 1u) / a.rows_per_wg);
+        if (rows == 1u || uint64_t(a.merged ? 1u : a.batch) * a.heads * a.wgs_per_head >= 4u * kComputeUnits) return;
+    }
 }
 
 int launch_softmax_forward(const SoftmaxArgs &args, uint32_t dtype, const SoftmaxForm &f, void *stream)
 {
     SoftmaxArgs a = args;
-    a.rows_per_wg = f.parts > 1u ? 1u : f.row.teams() * rows_of_team(a, f);
-    a.wgs_per_head = (a.queries + a.rows_per_wg - 1u) / a.rows_per_wg;
     a.row_parts = f.parts;
-    const uint64_t blocks = uint64_t(a.batch) * a.heads * a.wgs_per_head * f.parts;
+    a.rows_per_wg = 1;
+    a.wgs_per_head = a.queries;
+    if (f.parts == 1u) share_rows(a, f);
+    const uint64_t blocks = uint64_t(a.merged ? 1u : a.batch) * a.heads * a.wgs_per_head * f.parts;
     const dim3 grid(uint32_t(std::min<uint64_t>(blocks, kMostWorkgroups))), wg(f.row.workgroup());
     return with_kernel<KForward>(a, dtype, f, [&](auto kernel) {
         hipLaunchKernelGGL(kernel.value, grid, wg, 4u * cells(a.places), static_cast<hipStream_t>(stream), a);

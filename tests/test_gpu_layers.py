@@ -397,6 +397,18 @@ def test_softmax_of_many_short_sequences(A):
         c.backward()
 
 
+@pytest.mark.parametrize("batch,heads,queries,keys", [(70, 3, 1, 17), (70, 3, 5, 60), (45, 5, 7, 100), (37, 2, 1, 300), (21, 3, 1, 1000), (4099, 1, 1, 700), (700, 6, 1, 2100),
+                                                      (9000, 4, 3, 9)])
+def test_softmax_of_sequences_that_share_workgroups(A, batch, heads, queries, keys):
+    """Sequences of so few rows that a workgroup takes rows of several, each with its own start, length and mask."""
+    starts, lengths = [(7 * b) % (keys + 3) - 1 for b in range(batch)], [(5 * b) % (keys + 1) for b in range(batch)]
+    for mask, dtype, order in ((None, torch.bfloat16, "bqhk"), ("single", torch.float32, "odd")):
+        c = Case(A, (batch, heads, queries, keys, True, starts, lengths, mask, 32, 128), dtype, 0.1, order)
+        c.forward()
+        if order == "odd":
+            untouched(c.out, 3, 1)
+
+
 def test_softmax_in_place_and_without_the_table_gradient(A):
     for shape in (SHAPES[4], SHAPES[12], SHAPES[18]):
         c = Case(A, shape, torch.bfloat16, 0.1)
@@ -591,6 +603,20 @@ def test_more_rows_than_one_launch_takes(A):
     want = torch.zeros(8, dtype=torch.float64, device=DEV).index_add_(0, bucket, e.sum((0, 1, 2)))
     size = torch.zeros(8, dtype=torch.float64, device=DEV).index_add_(0, bucket, (p * (s.double().abs() + 5)).sum((0, 1, 2)))
     assert torch.all((dtable[:, 0].double() - want).abs() <= U * 400 * size)   # a thread adds up to 25 of the rows
+
+
+def test_more_sequences_than_a_launch_of_the_softmax_has_workgroups(A):
+    """Sequences that have workgroups of their own, since they have too many rows to share them."""
+    g = torch.Generator(device=DEV).manual_seed(3)
+    batch, queries, keys = (1 << 20) + 500, 130, 2
+    s = torch.randn(batch, 1, queries, keys, generator=g, dtype=torch.bfloat16, device=DEV)
+    bias = A.RelativeBias(torch.randn(8, 1, generator=g, device=DEV), torch.from_numpy(A.adacomp_relative_buckets(8, 6, True)).to(DEV))
+    ws = torch.empty(A.adacomp_bias_softmax_workspace_bytes(batch, 1, queries, keys, 6), dtype=torch.uint8, device=DEV)
+    probs, part = torch.empty_like(s), torch.empty_like(s[:900])
+    A.adacomp_bias_softmax_forward(s, bias, probs, ws)
+    for first in (0, (1 << 20) - 450, batch - 900):
+        A.adacomp_bias_softmax_forward(s[first:first + 900], bias, part, ws)
+        assert torch.equal(probs[first:first + 900], part)
 
 
 # ---- gradients against differences of the kernels' own results -----------------------------------------------------
