@@ -262,7 +262,8 @@ template <typename T, int TPR, int V, int PHASE, int KIND> __global__ __launch_b
                 total = 0.f;
                 for (uint32_t q = 0; q < a.row_parts; ++q) total = fmaf(of[2u * q + 1u], Unit<T>::exp(of[2u * q] - from_top), total);
             }
-            float factor = total == 0.f ? 0.f : Unit<T>::exp(from - (top == -kInf ? 0.f : top)) / total;
+            // a wave of nothing but -infinity has zeros, whatever the row's maximum; a row's NaN is in its total
+            float factor = total == 0.f ? 0.f : (m == -kInf ? 1.f : Unit<T>::exp(from - top)) / total;
             if (a.drop.on) factor *= d.factor;
             if (a.lse && t == 0u && part == 0u) a.lse[row] = total == 0.f ? -kInf : Unit<T>::lse(top, total);
             groups.store(o, [&](int v) {
