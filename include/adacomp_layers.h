@@ -117,7 +117,8 @@ int adacomp_relative_buckets(uint32_t n_buckets, uint32_t max_distance, int both
  * (query_starts ? query_starts[b] : query_start) + i, key j at position j.
  * A place is admitted if j < key_lengths[b] (with key_lengths), j <= the query's position (with causal),
  * and mask[b, h, i, j] != 0 (with mask).  What stands in other places is never looked at.
- *   t = scale * score + table[map[clamp(j - position, -D, D) + D], head]
+ *   t = scale * score + table[map[clamp(j - position, -D, D) + D], head], a float32: only scores and products beyond its range
+ *       are infinities (a row of a type's lowest value is even at a scale of 1, not empty)
  *   P = exp(t - lse), lse = log(sum over the row's admitted places of exp(t)); a row without any (or with
  *       -infinity in all of them) has P = 0 and lse = -infinity
  * table      [n_buckets, heads] float32;  map  2 max_distance + 1 device int32, clamped to 0 .. n_buckets - 1

@@ -107,7 +107,6 @@ static int softmax_args(const adacomp_bias_softmax_t *op, const adacomp_view_t *
     a.distance = op->max_distance;
     a.query_start = op->query_start;
     a.scale = op->scale;
-    a.scale2 = float(double(op->scale) * 1.4426950408889634);
     softmax_places(a);
     return ADACOMP_OK;
 }

@@ -90,7 +90,7 @@ struct SoftmaxArgs {
     uint32_t n_buckets, distance;
     uint32_t first_place, places;   // of the map's 2 D + 1 entries, those that the call can need
     int32_t query_start;
-    float scale2, scale;        // scale log2(e), scale
+    float scale;
     uint32_t rows_per_wg, wgs_per_head;   // forward: consecutive rows of a workgroup, workgroups to a (batch, head), or merged to a head; backward: workgroups to a head
     uint32_t row_parts;                   // parts of a row
     uint32_t merged;                      // forward: workgroups share out a head's rows of all sequences, not of one

@@ -26,31 +26,25 @@ constexpr uint32_t kGuard = 8;
 __host__ __device__ constexpr uint32_t cell(uint32_t X) { return X + (X >> 3); }
 __host__ __device__ constexpr uint32_t cells(uint32_t places) { return (cell(places - 1u + 2u * kGuard) + 3u) & ~3u; }
 
-// What exponents are made of.  16-bit tensors: everything in units of log2, one v_exp_f32 a value, whose argument has been rounded
-// where it is about 10: 5e-7 of the result at most, far below their own rounding.  32-bit ones: natural units, as in the formula, and the
-// rounding of the product with log2(e) is made good to first order (6 x 5 x 333 x 777: dscores 3.1e-7 -> 2.3e-7 off).
-template <typename T> struct Unit {
-    static constexpr bool kNatural = sizeof(T) == 4;
-    static __device__ __forceinline__ float scale(const SoftmaxArgs &a) { return kNatural ? a.scale : a.scale2; }
-    static __device__ __forceinline__ float from_natural(float x) { return kNatural ? x : x * kLog2e; }
-    static __device__ __forceinline__ float exp(float x)
-    {
-        if constexpr (!kNatural) return __builtin_amdgcn_exp2f(x);
-        const float y = x * kLog2e;
-        const float off = fabsf(x) < 200.f ? fmaf(x, kLog2e, -y) + x * kLog2eRest : 0.f;   // infinities have none
-        const float p = __builtin_amdgcn_exp2f(y);
-        return fmaf(p, off * kLn2, p);
-    }
-    static __device__ __forceinline__ float lse(float top, float total) { return kNatural ? top + logf(total) : (top + log2f(total)) * kLn2; }
-};
+// Exponents are in natural units, as in the formula, so that they are finite wherever scale * score is: in units of log2 the lowest
+// bf16 value would be -infinity at a scale of 1.  16-bit tensors: the product with log2(e) is rounded, 5e-7 of the result at most where the
+// argument is about 10, far below their own rounding.  32-bit ones: that rounding is made good to first order (6 x 5 x 333 x 777: dscores
+// 3.1e-7 -> 2.3e-7 off).
+template <typename T> __device__ __forceinline__ float exp_of(float x)
+{
+    const float y = x * kLog2e, p = __builtin_amdgcn_exp2f(y);
+    if constexpr (sizeof(T) == 2) return p;
+    const float off = fabsf(x) < 200.f ? fmaf(x, kLog2e, -y) + x * kLog2eRest : 0.f;   // infinities have none
+    return fmaf(p, off * kLn2, p);
+}
 
 // A workgroup's copy of its head's bias.
-template <typename T> __device__ __forceinline__ void stage_bias(float *bias, const SoftmaxArgs &a, uint32_t head)
+__device__ __forceinline__ void stage_bias(float *bias, const SoftmaxArgs &a, uint32_t head)
 {
     const int last = int(a.places) - 1;
     for (int X = threadIdx.x; X <= last + 2 * int(kGuard) - 1; X += blockDim.x) {
         const int32_t b = min(max(a.map[a.first_place + min(max(X - int(kGuard), 0), last)], 0), int32_t(a.n_buckets) - 1);
-        bias[cell(X)] = Unit<T>::from_natural(a.table[uint64_t(b) * a.heads + head]);
+        bias[cell(X)] = a.table[uint64_t(b) * a.heads + head];
     }
 }
 
@@ -184,7 +178,7 @@ template <typename T, int TPR, int V, int PHASE, int KIND> __global__ __launch_b
         };
         if (first + team < end) fetch(first + team);
         if (block != blockIdx.x) __syncthreads();   // the rows before are done with the bias
-        stage_bias<T>(bias, a, h);
+        stage_bias(bias, a, h);
         __syncthreads();
         const float low = bias[0], high = bias[cell(a.places - 1u + kGuard)];
         for (uint32_t i = first + team; i < end; i += TEAMS) {
@@ -209,7 +203,7 @@ template <typename T, int TPR, int V, int PHASE, int KIND> __global__ __launch_b
                 if (__any(n > 0)) {
                     const uint32_t here = admitted8<kMasked<KIND>>(kMasked<KIND> ? mask_of(groups, mask[v], v) : 0, n);
                     bits |= here << (8 * v);
-                    p[v] = biased8(groups.values(raw[v], v), a, Unit<T>::scale(a), r, Window(r, j), bias, low, high, 0.f);
+                    p[v] = biased8(groups.values(raw[v], v), a, a.scale, r, Window(r, j), bias, low, high, 0.f);
                     if (here != 0xFFu) {
 #pragma unroll
                         for (int k = 0; k < 8; ++k) p[v][k] = here >> k & 1u ? p[v][k] : -kInf;
@@ -222,13 +216,17 @@ template <typename T, int TPR, int V, int PHASE, int KIND> __global__ __launch_b
             // exponentials from the maximum of a wave's lanes; the waves' sums are joined behind them
             m = over_lanes<Max, LANES>(m);
             const float from = m == -kInf ? 0.f : m;
+            // 16 bits: units of log2 in the same operation as the difference (a product of its own costs 2 %).  The rounding of from * unit is common to the
+            // wave's values, and no larger than that of its maximum; beyond 2^24 scores that differ at all differ by thousands, in any unit, and the
+            // product could overflow.
+            const float unit = fabsf(from) < 0x1p24f ? kLog2e : 1.f, from_units = from * unit;
             float l = 0.f;
 #pragma unroll
             for (int v = 0; v < V; ++v)
                 if (__any(bits >> (8 * v) & 0xFFu)) {
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
-                        p[v][k] = Unit<T>::exp(p[v][k] - from);
+                        p[v][k] = sizeof(T) == 2 ? __builtin_amdgcn_exp2f(fmaf(p[v][k], unit, -from_units)) : exp_of<T>(p[v][k] - from);
                         l += p[v][k];
                     }
                 }
@@ -243,7 +241,7 @@ template <typename T, int TPR, int V, int PHASE, int KIND> __global__ __launch_b
                 const float from_top = top == -kInf ? 0.f : top;
                 total = 0.f;
 #pragma unroll
-                for (int w = 0; w < TPR / 64; ++w) total = fmaf(room[turn][1][w], Unit<T>::exp(room[turn][0][w] - from_top), total);
+                for (int w = 0; w < TPR / 64; ++w) total = fmaf(room[turn][1][w], exp_of<T>(room[turn][0][w] - from_top), total);
                 turn ^= 1u;
             }
             if constexpr (PHASE == STATS) {
@@ -260,12 +258,12 @@ template <typename T, int TPR, int V, int PHASE, int KIND> __global__ __launch_b
                 for (uint32_t q = 0; q < a.row_parts; ++q) top = fmaxf(top, of[2u * q]);
                 const float from_top = top == -kInf ? 0.f : top;
                 total = 0.f;
-                for (uint32_t q = 0; q < a.row_parts; ++q) total = fmaf(of[2u * q + 1u], Unit<T>::exp(of[2u * q] - from_top), total);
+                for (uint32_t q = 0; q < a.row_parts; ++q) total = fmaf(of[2u * q + 1u], exp_of<T>(of[2u * q] - from_top), total);
             }
             // a wave of nothing but -infinity has zeros, whatever the row's maximum; a row's NaN is in its total
-            float factor = total == 0.f ? 0.f : (m == -kInf ? 1.f : Unit<T>::exp(from - top)) / total;
+            float factor = total == 0.f ? 0.f : (m == -kInf ? 1.f : exp_of<T>(from - top)) / total;
             if (a.drop.on) factor *= d.factor;
-            if (a.lse && t == 0u && part == 0u) a.lse[row] = total == 0.f ? -kInf : Unit<T>::lse(top, total);
+            if (a.lse && t == 0u && part == 0u) a.lse[row] = total == 0.f ? -kInf : sizeof(T) == 2 ? fmaf(log2f(total), kLn2, top) : top + logf(total);
             groups.store(o, [&](int v) {
                 f32x8 y = {};
                 const uint32_t here = bits >> (8 * v) & 0xFFu;
@@ -299,7 +297,7 @@ template <typename T, int TPR, int V, int PHASE, int KIND> __global__ __launch_b
     const uint32_t h = blockIdx.x / a.wgs_per_head, group = blockIdx.x - h * a.wgs_per_head;
     const Drop d = drop_of(a.drop);
     const float up_factor = a.drop.on ? d.factor : 1.f;
-    stage_bias<T>(bias, a, h);
+    stage_bias(bias, a, h);
     if (sums)
         for (uint32_t x = threadIdx.x; x < size * TEAMS; x += WG) lds[size + x] = 0.f;
     __syncthreads();
@@ -325,11 +323,11 @@ template <typename T, int TPR, int V, int PHASE, int KIND> __global__ __launch_b
         groups.load_below(raw_up, up, uint32_t(r.limit));
         raw8<uint8_t> mask[V];
         if constexpr (kMasked<KIND>) load_mask(groups, mask, r);
-        const float lse = a.lse[row], lse2 = lse == -kInf ? kInf : Unit<T>::from_natural(lse);
+        const float lse = a.lse[row], from = lse == -kInf ? kInf : lse;
         // Beyond 2^22 an lse has no fraction left, and its roundings alone would make exponents of any size: there, places that are as
         // near to it as that have P = 1 (rows of the type's lowest value, say; their number is lost in lse).
-        const bool coarse = !(fabsf(lse2) < 4194304.f);
-        const float less = coarse || Unit<T>::kNatural ? 0.f : lse2;
+        const bool coarse = !(fabsf(from) < 4194304.f);
+        const float less = coarse || sizeof(T) == 4 ? 0.f : from;
         f32x8 p[V], dp[V];
         uint32_t admitted = 0;   // 8 places to a group
         float inner = 0.f;
@@ -341,22 +339,22 @@ template <typename T, int TPR, int V, int PHASE, int KIND> __global__ __launch_b
             if (__any(n > 0)) {   // rounds of which a wave has nothing are left out; its other threads go along, and have nothing admitted
                 const uint32_t bits = admitted8<kMasked<KIND>>(kMasked<KIND> ? mask_of(groups, mask[v], v) : 0, n);
                 admitted |= bits << (8 * v);
-                p[v] = biased8(groups.values(raw[v], v), a, Unit<T>::scale(a), r, Window(r, j), bias, bias_low, bias_high, less);
-                if (Unit<T>::kNatural && !coarse) {   // the difference as the formula has it: exact where it is small
+                p[v] = biased8(groups.values(raw[v], v), a, a.scale, r, Window(r, j), bias, bias_low, bias_high, less);
+                if (sizeof(T) == 4 && !coarse) {   // the difference as the formula has it: exact where it is small
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) p[v][k] -= lse2;
+                    for (int k = 0; k < 8; ++k) p[v][k] -= from;
                 }
                 if (coarse) {
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
-                        const float x = p[v][k] - lse2;
-                        p[v][k] = x > fabsf(lse2) * -0x1p-21f ? 0.f : x;
+                        const float x = p[v][k] - from;
+                        p[v][k] = x > fabsf(from) * -0x1p-21f ? 0.f : x;
                     }
                 }
                 dp[v] = groups.values(raw_up[v], v);
                 if (a.drop.on) dp[v] = kept8(dp[v], dr, uint32_t(j) / 8u, uint32_t(row));
 #pragma unroll
-                for (int k = 0; k < 8; ++k) p[v][k] = Unit<T>::exp(p[v][k]);
+                for (int k = 0; k < 8; ++k) p[v][k] = exp_of<T>(p[v][k]);
                 if (bits != 0xFFu) {
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {

@@ -72,3 +72,33 @@ def test_stretches_of_minus_infinity_beside_low_scores(A, keys, dtype):
         assert torch.all(probs[i][torch.isinf(s[i])] == 0)
     check_gradient(ds, s, up, lse, scale, dtype, [0, 2, 4, 6], False)
     assert torch.all(ds[3] == 0) and torch.all(ds[1, :-8] == 0)
+
+
+@pytest.mark.parametrize("keys", KEYS)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_finite_scores_at_the_ends_of_their_type_count(A, keys, dtype):
+    """At scale 1 every finite score is a finite exponent: a row of the type's lowest value is even, not empty, its largest value takes all."""
+    inf, low, high = float("inf"), torch.finfo(dtype).min, torch.finfo(dtype).max
+    g = torch.Generator().manual_seed(keys)
+    rows = torch.randn(6, keys, generator=g)
+    rows[0] = low
+    rows[1, keys // 2] = high
+    rows[2] = high
+    rows[3], rows[3, :keys // 2] = -inf, low
+    rows[5, ::2] = low
+    s, up, probs, lse, ds = call(A, rows, dtype, 1.0)
+    for i, n in ((0, keys), (2, keys), (3, keys // 2)):   # differences of equal numbers are zeros, a sum of ones is exact
+        want = torch.where(torch.isinf(s[i]), 0.0, 1.0 / n)
+        within(probs[i], want, want * (HALF_STEP[dtype] * 1.01 + 2 * U) + TINY[dtype], ("probs", i))
+        within(lse[i], s[i, 0] + torch.tensor(float(n)).double().log(), 4 * U * (abs(s[i, 0]) + 20), ("lse", i))
+    only = torch.zeros(keys, dtype=dtype)
+    only[keys // 2] = 1.0
+    assert torch.equal(probs[1], only) and abs(lse[1].double() - s[1, keys // 2]) <= 4 * U * high
+    for i in (4, 5):
+        p, exact_lse = R.softmax_forward(s[i])
+        rho = U * (8 * (s[4].abs().max() + exact_lse.abs()) + DEEP)
+        within(probs[i], p, p * (HALF_STEP[dtype] * 1.01 + 2 * rho) + TINY[dtype], ("probs", i))
+        within(lse[i], exact_lse, rho, ("lse", i))
+    check_gradient(ds, s, up, lse, 1.0, dtype, [4], False)
+    check_gradient(ds, s, up, lse, 1.0, dtype, [0, 1, 2, 3], dtype is not torch.float16)   # float16's ends have fractions of an exponent left
+    assert torch.isfinite(ds[5].double()).all()
