@@ -317,15 +317,7 @@ int launch_dropout(const DropoutLaunch &a, void *stream)
     });
 }
 
-// Forward: 16 values to a thread, or up to 32 in the widest rows (16 and not 8: twice the bytes on their way for a wave, at no more
-// than 64 registers).  Backward: 8, of columns whose sums a thread keeps.
-static uint32_t forward_threads(uint32_t cols)
-{
-    uint32_t threads = 8;
-    while (threads < 1024u && threads * (cols <= 64u ? 8u : 16u) < cols) threads *= 2u;
-    return threads;
-}
-
+// 8 values to a thread, of columns whose sums it keeps.
 static uint32_t backward_threads(uint32_t cols)
 {
     uint32_t threads = 8;
@@ -375,8 +367,10 @@ static uint32_t idle_lds(const NormForward &a, uint32_t size, uint32_t wg)
 
 int launch_norm_forward(const NormForward &args, uint32_t dtype, void *stream)
 {
-    const uint32_t threads = forward_threads(args.cols), wg = std::max(threads, 256u), teams = wg / threads;
-    const uint64_t step = uint64_t(1) << 22;   // rows of a launch: it has fewer than 2^32 threads
+    const uint32_t threads = norm_forward_threads(args.cols);
+    const RowForm form = {threads, 0};
+    const uint32_t wg = form.workgroup(), teams = form.teams();
+    const uint64_t step = norm_forward_rows(form);
     const uint64_t size = dtype == ADACOMP_DTYPE_F32 ? 4u : 2u;
     for (uint64_t first = 0; first < args.all_rows; first += step) {
         NormForward a = args;

@@ -65,6 +65,17 @@ struct NormReduce {
     uint32_t parts, pitch, cols, accumulate;
 };
 
+// Threads to a row of the forward pass: 16 values to a thread, or up to 32 in the widest rows (16 and not 8: twice the bytes on their way for a
+// wave, at no more than 64 registers).
+inline uint32_t norm_forward_threads(uint32_t cols)
+{
+    uint32_t threads = 8;
+    while (threads < 1024u && threads * (cols <= 64u ? 8u : 16u) < cols) threads *= 2u;
+    return threads;
+}
+// Rows of one of its launches, which has at most 2^31 threads: the grid is counted in threads, in 32 bits.
+inline uint64_t norm_forward_rows(const RowForm &row) { return std::min(uint64_t(1) << 22, row.teams() * ((uint64_t(1) << 31) / row.workgroup())); }
+
 uint32_t norm_parts(uint64_t rows, uint32_t cols);   // workgroups of the backward pass
 inline uint32_t norm_pitch(uint32_t cols) { return (cols + 7u) & ~7u; }
 
