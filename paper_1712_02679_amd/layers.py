@@ -74,6 +74,13 @@ _current_device = torch._C._cuda_getDevice          # torch.cuda.current_device(
 _current_stream = torch._C._cuda_getCurrentRawStream   # and a look at the module's state around them: 1 us less, of 8 in all
 
 
+def _in_32_bits(x, what):
+    """x, a size or number that the library takes as an unsigned 32-bit one: ctypes would cut off what is above."""
+    if not 0 <= x < 2 ** 32:
+        _refuse(f"{what}: {x} is not a number of 32 bits")
+    return x
+
+
 def _device_of(x):
     """The GPU that x and every other tensor of the call have to be on."""
     device = x.get_device()
@@ -180,7 +187,7 @@ def adacomp_norm_forward(x, gamma, beta, y, residual=None, dropout=None, z=None,
     py, sy = _rows(y, shape, dtype, dev, "y")
     pr, sr = _rows(residual, shape, dtype, dev, "residual")
     pz, sz = _rows(z, shape, dtype, dev, "z")
-    norm = _Norm(rows, cols, number, sx, sr, sz, sy)
+    norm = _Norm(rows, _in_32_bits(cols, "columns"), number, sx, sr, sz, sy)
     rc = L.adacomp_norm_forward(norm, px, pr, _vector(gamma, cols, dev, "gamma"), _vector(beta, cols, dev, "beta"), eps, _drop(dropout, dev), pz, py,
                                 _vector(mean, rows, dev, "mean"), _vector(rstd, rows, dev, "rstd"), _current_stream(dev))
     if rc:
@@ -188,7 +195,8 @@ def adacomp_norm_forward(x, gamma, beta, y, residual=None, dropout=None, z=None,
 
 
 def adacomp_norm_workspace_bytes(rows, cols) -> int:
-    return int(_lib().adacomp_norm_workspace_bytes(int(rows), int(cols)))
+    rows, cols = int(rows), int(cols)
+    return int(_lib().adacomp_norm_workspace_bytes(rows, cols)) if 0 <= rows < 2 ** 32 and 0 <= cols < 2 ** 32 else 0
 
 
 def adacomp_norm_backward(dy, z, mean, rstd, gamma, dz, dgamma, dbeta, workspace, dz_add=None, dropout=None, dx=None, accumulate=False):
@@ -203,7 +211,7 @@ def adacomp_norm_backward(dy, z, mean, rstd, gamma, dz, dgamma, dbeta, workspace
     pdz, sdz = _rows(dz, shape, dtype, dev, "dz")
     pdx, sdx = _rows(dx, shape, dtype, dev, "dx")
     pw, nw = _room(workspace, dev)
-    norm = _Norm(rows, cols, number, 0, 0, sz, 0, sdy, sa, sdz, sdx)
+    norm = _Norm(rows, _in_32_bits(cols, "columns"), number, 0, 0, sz, 0, sdy, sa, sdz, sdx)
     rc = L.adacomp_norm_backward(norm, pdy, pa, pz, _vector(mean, rows, dev, "mean"), _vector(rstd, rows, dev, "rstd"), _vector(gamma, cols, dev, "gamma"),
                                  _drop(dropout, dev), pdz, pdx, _vector(dgamma, cols, dev, "dgamma"), _vector(dbeta, cols, dev, "dbeta"),
                                  1 if accumulate else 0, pw, nw, _current_stream(dev))
@@ -213,8 +221,11 @@ def adacomp_norm_backward(dy, z, mean, rstd, gamma, dz, dgamma, dbeta, workspace
 
 def adacomp_relative_buckets(n_buckets, max_distance, both_directions):
     """The usual logarithmic map of distances key - query in -max_distance .. max_distance to buckets, as an int32 numpy array."""
-    out = np.zeros(2 * int(max_distance) + 1, np.int32)
-    _check(_lib().adacomp_relative_buckets(int(n_buckets), int(max_distance), 1 if both_directions else 0, out.ctypes.data))
+    n_buckets, max_distance = _in_32_bits(int(n_buckets), "n_buckets"), int(max_distance)
+    if not 1 <= max_distance <= BIAS_DISTANCE_MAX:
+        _refuse(f"max_distance: {max_distance} is not one of 1 .. {BIAS_DISTANCE_MAX}")
+    out = np.zeros(2 * max_distance + 1, np.int32)
+    _check(_lib().adacomp_relative_buckets(n_buckets, max_distance, 1 if both_directions else 0, out.ctypes.data))
     return out
 
 
@@ -259,6 +270,8 @@ def _bias_softmax(scores, bias, scale, causal, query_start, query_starts, key_le
     b, h, q, k = shape
     if bias.heads != h or bias.table.get_device() != dev:
         _refuse(f"the bias is one of {bias.heads} heads on {bias.table.device}, the scores have {h} on {scores.device}")
+    if (b | h | q | k | bias.n_buckets | bias.max_distance) >> 32 or not -2 ** 31 <= query_start < 2 ** 31:
+        _refuse(f"sizes {tuple(shape)}, {bias.n_buckets} buckets, distances up to {bias.max_distance}, query_start {query_start}: not all are numbers of 32 bits")
     view = _NO_VIEW
     if mask is not None:
         if mask.dtype not in (torch.uint8, torch.bool) or mask.dim() != 4 or mask.get_device() != dev:
@@ -280,7 +293,8 @@ _NO_VIEW = _View()
 
 
 def adacomp_bias_softmax_workspace_bytes(batch, heads, queries, keys, max_distance) -> int:
-    return int(_lib().adacomp_bias_softmax_workspace_bytes(int(batch), int(heads), int(queries), int(keys), int(max_distance)))
+    sizes = [int(n) for n in (batch, heads, queries, keys, max_distance)]
+    return int(_lib().adacomp_bias_softmax_workspace_bytes(*sizes)) if all(0 <= n < 2 ** 32 for n in sizes) else 0
 
 
 def adacomp_bias_softmax_forward(scores, bias, probs, workspace, lse=None, scale=1.0, causal=False, query_start=0, query_starts=None,
