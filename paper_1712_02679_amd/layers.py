@@ -145,20 +145,56 @@ def _room(workspace, device):
 
 class Dropout:
     """What decides which values a call keeps: rate, seed and the number of the call (`stream`, one per layer and training step).
-    `step`, an int64 tensor of one value on the GPU, is added to `stream` when the kernel runs, for captured graphs."""
+    `step`, an int64 tensor of one value on the GPU, is added to `stream` when the kernel runs, for captured graphs.
+    The attributes can be set; calls from then on use what they are."""
 
     def __init__(self, p, seed, stream=0, step=None):
+        self._c = _Dropout()
+        self._ref = ctypes.byref(self._c)
+        self.p, self.seed, self.stream, self.step = p, seed, stream, step
+
+    @property
+    def p(self):
+        return self._p
+
+    @p.setter
+    def p(self, p):
+        self._p = self._c.p = float(p)
+
+    @property
+    def seed(self):
+        return self._seed
+
+    @seed.setter
+    def seed(self, seed):
+        self._seed = int(seed)
+        self._c.seed = self._seed & (2 ** 64 - 1)
+
+    @property
+    def stream(self):
+        return self._stream
+
+    @stream.setter
+    def stream(self, stream):
+        self._stream = int(stream)
+        self._c.stream = self._stream & (2 ** 64 - 1)
+
+    @property
+    def step(self):
+        return self._step
+
+    @step.setter
+    def step(self, step):
         if step is not None and (step.dtype != torch.int64 or step.numel() != 1 or not step.is_cuda):
             _refuse("step: one int64 value on the GPU is wanted")
-        self.p, self.seed, self.stream, self.step = float(p), int(seed), int(stream), step
-        self._c = _Dropout(self.p, 0, self.seed & (2 ** 64 - 1), self.stream & (2 ** 64 - 1), None if step is None else step.data_ptr())
-        self._ref = ctypes.byref(self._c)
+        self._step = step
+        self._c.step = None if step is None else step.data_ptr()
 
 
 def _drop(dropout, device):
     if dropout is None:
         return None
-    if dropout.step is not None and dropout.step.get_device() != device:
+    if dropout._step is not None and dropout._step.get_device() != device:
         _refuse("step is on another device")
     return dropout._ref
 

@@ -1,0 +1,53 @@
+"""The attributes of a Dropout are what its next call uses."""
+import pytest
+import torch
+
+from paper_1712_02679_amd import binding, layers
+
+
+def fields(drop):
+    """What the library is given."""
+    return drop._c.p, drop._c.seed, drop._c.stream, drop._c.step
+
+
+def test_setting_an_attribute_changes_the_next_call():
+    drop = layers.Dropout(0.25, 1, 2)
+    assert fields(drop) == (0.25, 1, 2, None)
+    drop.stream = 7
+    drop.seed = 2 ** 64 + 9
+    drop.p = 0.5
+    assert fields(drop) == (0.5, 9, 7, None) and (drop.p, drop.seed, drop.stream, drop.step) == (0.5, 2 ** 64 + 9, 7, None)
+    drop.stream += 1
+    assert fields(drop)[2] == 8
+
+
+def test_a_step_is_one_number_on_the_gpu():
+    drop = layers.Dropout(0.25, 1, 2)
+    for step in (torch.zeros(1, dtype=torch.int64), torch.zeros(2, dtype=torch.int64), torch.zeros(1)):
+        with pytest.raises(binding.AdacompError):
+            drop.step = step
+        with pytest.raises(binding.AdacompError):
+            layers.Dropout(0.25, 1, 2, step)
+    assert drop.step is None and fields(drop)[3] is None
+
+
+@pytest.mark.gpu
+def test_calls_follow_the_attributes():
+    dev = "cuda:0"
+    x = torch.ones(64, 500, device=dev)
+
+    def of(drop):
+        y = torch.empty_like(x)
+        layers.adacomp_dropout(x, y, drop)
+        return y
+
+    drop = layers.Dropout(0.25, 1, 2)
+    first = of(drop)
+    drop.stream = 3
+    assert torch.equal(of(drop), of(layers.Dropout(0.25, 1, 3))) and not torch.equal(of(drop), first)
+    drop.step = torch.full((1,), 5, dtype=torch.int64, device=dev)
+    assert torch.equal(of(drop), of(layers.Dropout(0.25, 1, 8)))
+    drop.step = torch.full((1,), 6, dtype=torch.int64, device=dev)
+    assert torch.equal(of(drop), of(layers.Dropout(0.25, 1, 9)))
+    drop.step, drop.stream = None, 2
+    assert torch.equal(of(drop), first)
