@@ -267,16 +267,36 @@ def adacomp_relative_buckets(n_buckets, max_distance, both_directions):
 
 class RelativeBias:
     """A learned bias by buckets of distance: `table` [n_buckets, heads] float32 (it may be a part of the flat weights) and `map`, an int32
-    tensor of 2 * max_distance + 1 buckets on the GPU."""
+    tensor of 2 * max_distance + 1 buckets on the GPU.  Both can be set; the sizes are theirs."""
 
     def __init__(self, table, map):
+        self.table, self.map = table, map
+
+    n_buckets = property(lambda self: self._n_buckets)
+    heads = property(lambda self: self._heads)
+    max_distance = property(lambda self: self._max_distance)
+
+    @property
+    def table(self):
+        return self._table
+
+    @table.setter
+    def table(self, table):
         if table.dim() != 2 or table.dtype != torch.float32 or not table.is_contiguous():
             _refuse("table: a contiguous float32 tensor [n_buckets, heads] is wanted")
-        if map.dim() != 1 or map.dtype != torch.int32 or not map.is_contiguous() or map.numel() % 2 == 0 or map.get_device() != table.get_device():
+        self._n_buckets, self._heads = table.shape
+        self._table = table
+
+    @property
+    def map(self):
+        return self._map
+
+    @map.setter
+    def map(self, map):
+        if map.dim() != 1 or map.dtype != torch.int32 or not map.is_contiguous() or map.numel() % 2 == 0 or map.get_device() != self._table.get_device():
             _refuse("map: an int32 tensor of 2 * max_distance + 1 values beside the table is wanted")
-        self.table, self.map = table, map
-        self.n_buckets, self.heads = table.shape
-        self.max_distance = map.numel() // 2
+        self._max_distance = map.numel() // 2
+        self._map = map
 
 
 def _view(t, shape, dtype, device, what):
@@ -304,10 +324,10 @@ def _bias_softmax(scores, bias, scale, causal, query_start, query_starts, key_le
         _refuse("scores: [batch, heads, queries, keys] of float32, bfloat16 or float16 is wanted")
     dev = _device_of(scores)
     b, h, q, k = shape
-    if bias.heads != h or bias.table.get_device() != dev:
-        _refuse(f"the bias is one of {bias.heads} heads on {bias.table.device}, the scores have {h} on {scores.device}")
-    if (b | h | q | k | bias.n_buckets | bias.max_distance) >> 32 or not -2 ** 31 <= query_start < 2 ** 31:
-        _refuse(f"sizes {tuple(shape)}, {bias.n_buckets} buckets, distances up to {bias.max_distance}, query_start {query_start}: not all are numbers of 32 bits")
+    if bias._heads != h or bias._table.get_device() != dev or bias._map.get_device() != dev:
+        _refuse(f"the bias is one of {bias._heads} heads on {bias._table.device} (its map on {bias._map.device}), the scores have {h} on {scores.device}")
+    if (b | h | q | k | bias._n_buckets | bias._max_distance) >> 32 or not -2 ** 31 <= query_start < 2 ** 31:
+        _refuse(f"sizes {tuple(shape)}, {bias._n_buckets} buckets, distances up to {bias._max_distance}, query_start {query_start}: not all are numbers of 32 bits")
     view = _NO_VIEW
     if mask is not None:
         if mask.dtype not in (torch.uint8, torch.bool) or mask.dim() != 4 or mask.get_device() != dev:
@@ -319,9 +339,9 @@ def _bias_softmax(scores, bias, scale, causal, query_start, query_starts, key_le
         if s[3] != 1 and k > 1:
             _refuse("mask: its last dimension is contiguous and as long as the scores'")
         view = _View(mask.data_ptr(), s[0], s[1], s[2])
-    op = _BiasSoftmax(b, h, q, k, number, 1 if causal else 0, bias.n_buckets, bias.max_distance, scale, query_start,
+    op = _BiasSoftmax(b, h, q, k, number, 1 if causal else 0, bias._n_buckets, bias._max_distance, scale, query_start,
                       _per_sequence(query_starts, b, dev, "query_starts"), _per_sequence(key_lengths, b, dev, "key_lengths"),
-                      bias.table.data_ptr(), bias.map.data_ptr(), view)
+                      bias._table.data_ptr(), bias._map.data_ptr(), view)
     return op, shape, dtype, dev, b * h * q
 
 
@@ -354,6 +374,6 @@ def adacomp_bias_softmax_backward(scores, bias, lse, dprobs, dscores, dtable, wo
     pw, nw = _room(workspace, dev)
     rc = L.adacomp_bias_softmax_backward(op, _view(scores, shape, dtype, dev, "scores"), _vector(lse, rows, dev, "lse"),
                                          _view(dprobs, shape, dtype, dev, "dprobs"), _drop(dropout, dev), _view(dscores, shape, dtype, dev, "dscores"),
-                                         _vector(dtable, bias.n_buckets * bias.heads, dev, "dtable"), 1 if accumulate else 0, pw, nw, _current_stream(dev))
+                                         _vector(dtable, bias._n_buckets * bias._heads, dev, "dtable"), 1 if accumulate else 0, pw, nw, _current_stream(dev))
     if rc:
         _check(rc)

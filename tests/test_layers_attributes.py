@@ -1,4 +1,4 @@
-"""The attributes of a Dropout are what its next call uses."""
+"""The attributes of a Dropout and a RelativeBias are what their next call uses, and have been checked."""
 import pytest
 import torch
 
@@ -51,3 +51,22 @@ def test_calls_follow_the_attributes():
     assert torch.equal(of(drop), of(layers.Dropout(0.25, 1, 9)))
     drop.step, drop.stream = None, 2
     assert torch.equal(of(drop), first)
+
+
+def test_a_bias_has_the_sizes_of_its_table_and_map():
+    bias = layers.RelativeBias(torch.zeros(32, 4), torch.zeros(257, dtype=torch.int32))
+    assert (bias.n_buckets, bias.heads, bias.max_distance) == (32, 4, 128)
+    small, short = torch.zeros(8, 3), torch.zeros(9, dtype=torch.int32)
+    bias.table, bias.map = small, short      # a call with the old sizes would read behind their ends
+    assert bias.table is small and bias.map is short
+    assert (bias.n_buckets, bias.heads, bias.max_distance) == (8, 3, 4)
+    for table in (torch.zeros(8, 3).t(), torch.zeros(8), torch.zeros(8, 3).double()):
+        with pytest.raises(binding.AdacompError):
+            bias.table = table
+    for index in (torch.zeros(8, dtype=torch.int32), torch.zeros(9), torch.zeros(18, dtype=torch.int32)[::2], torch.zeros(3, 3, dtype=torch.int32)):
+        with pytest.raises(binding.AdacompError):
+            bias.map = index
+    assert bias.table is small and bias.map is short
+    for name in ("n_buckets", "heads", "max_distance"):
+        with pytest.raises(AttributeError):
+            setattr(bias, name, 5)
