@@ -312,8 +312,9 @@ int launch_dropout(const DropoutLaunch &a, void *stream)
                       uint64_t(a.rows) * a.cols * size * (a.residual ? 2u : 1u) >= kInputsPast;
     return with_type(a.dtype, [&](auto of) {
         using T = decltype(of);
-        if (once) hipLaunchKernelGGL((k_dropout<T, true>), grid, wg, 0, s, a);
-        else hipLaunchKernelGGL((k_dropout<T, false>), grid, wg, 0, s, a);
+        if constexpr (sizeof(T) == 2)
+            if (once) { hipLaunchKernelGGL((k_dropout<T, true>), grid, wg, 0, s, a); return; }
+        hipLaunchKernelGGL((k_dropout<T, false>), grid, wg, 0, s, a);
     });
 }
 

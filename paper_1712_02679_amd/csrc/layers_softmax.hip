@@ -552,7 +552,7 @@ static int with_kernel(const SoftmaxArgs &a, uint32_t dtype, const SoftmaxForm &
             if (dtype == ADACOMP_DTYPE_BF16) launch(std::integral_constant<void (*)(SoftmaxArgs), K<bf16, TPR, V, PHASE, KIND>::kernel>());
             else launch(std::integral_constant<void (*)(SoftmaxArgs), K<f16, TPR, V, PHASE, KIND>::kernel>());
         };
-        if constexpr (BACK && TPR > 8 && V <= 2 && PHASE == WHOLE)
+        if constexpr (BACK && PHASE == WHOLE && TPR > 8 && (V == 1 || (V == 2 && (TPR == 16 || TPR == 256))))   // what softmax_form gives to rows of fewer than 8 keys
             if (a.keys < 8u) return of(std::integral_constant<int, SHORT>());
         if constexpr (BACK && V * TPR >= 256 && PHASE == WHOLE)
             if (once) return of(std::integral_constant<int, ONCE>());
