@@ -223,7 +223,9 @@ def adacomp_norm_forward(x, gamma, beta, y, residual=None, dropout=None, z=None,
     py, sy = _rows(y, shape, dtype, dev, "y")
     pr, sr = _rows(residual, shape, dtype, dev, "residual")
     pz, sz = _rows(z, shape, dtype, dev, "z")
-    norm = _Norm(rows, _in_32_bits(cols, "columns"), number, sx, sr, sz, sy)
+    if cols >> 32:
+        _in_32_bits(cols, "columns")
+    norm = _Norm(rows, cols, number, sx, sr, sz, sy)
     rc = L.adacomp_norm_forward(norm, px, pr, _vector(gamma, cols, dev, "gamma"), _vector(beta, cols, dev, "beta"), eps, _drop(dropout, dev), pz, py,
                                 _vector(mean, rows, dev, "mean"), _vector(rstd, rows, dev, "rstd"), _current_stream(dev))
     if rc:
@@ -247,7 +249,9 @@ def adacomp_norm_backward(dy, z, mean, rstd, gamma, dz, dgamma, dbeta, workspace
     pdz, sdz = _rows(dz, shape, dtype, dev, "dz")
     pdx, sdx = _rows(dx, shape, dtype, dev, "dx")
     pw, nw = _room(workspace, dev)
-    norm = _Norm(rows, _in_32_bits(cols, "columns"), number, 0, 0, sz, 0, sdy, sa, sdz, sdx)
+    if cols >> 32:
+        _in_32_bits(cols, "columns")
+    norm = _Norm(rows, cols, number, 0, 0, sz, 0, sdy, sa, sdz, sdx)
     rc = L.adacomp_norm_backward(norm, pdy, pa, pz, _vector(mean, rows, dev, "mean"), _vector(rstd, rows, dev, "rstd"), _vector(gamma, cols, dev, "gamma"),
                                  _drop(dropout, dev), pdz, pdx, _vector(dgamma, cols, dev, "dgamma"), _vector(dbeta, cols, dev, "dbeta"),
                                  1 if accumulate else 0, pw, nw, _current_stream(dev))
@@ -284,7 +288,7 @@ class RelativeBias:
     def table(self, table):
         if table.dim() != 2 or table.dtype != torch.float32 or not table.is_contiguous():
             _refuse("table: a contiguous float32 tensor [n_buckets, heads] is wanted")
-        self._n_buckets, self._heads = table.shape
+        self._n_buckets, self._heads = _in_32_bits(table.shape[0], "buckets"), table.shape[1]
         self._table = table
 
     @property
@@ -295,7 +299,7 @@ class RelativeBias:
     def map(self, map):
         if map.dim() != 1 or map.dtype != torch.int32 or not map.is_contiguous() or map.numel() % 2 == 0 or map.get_device() != self._table.get_device():
             _refuse("map: an int32 tensor of 2 * max_distance + 1 values beside the table is wanted")
-        self._max_distance = map.numel() // 2
+        self._max_distance = _in_32_bits(map.numel() // 2, "max_distance")
         self._map = map
 
 
@@ -326,8 +330,8 @@ def _bias_softmax(scores, bias, scale, causal, query_start, query_starts, key_le
     b, h, q, k = shape
     if bias._heads != h or bias._table.get_device() != dev or bias._map.get_device() != dev:
         _refuse(f"the bias is one of {bias._heads} heads on {bias._table.device} (its map on {bias._map.device}), the scores have {h} on {scores.device}")
-    if (b | h | q | k | bias._n_buckets | bias._max_distance) >> 32 or not -2 ** 31 <= query_start < 2 ** 31:
-        _refuse(f"sizes {tuple(shape)}, {bias._n_buckets} buckets, distances up to {bias._max_distance}, query_start {query_start}: not all are numbers of 32 bits")
+    if (b | h | q | k) >> 32 or query_start and not -2 ** 31 <= query_start < 2 ** 31:   # ctypes would cut off what is above
+        _refuse(f"sizes {tuple(shape)}, query_start {query_start}: not all are numbers of 32 bits")
     view = _NO_VIEW
     if mask is not None:
         if mask.dtype not in (torch.uint8, torch.bool) or mask.dim() != 4 or mask.get_device() != dev:
