@@ -162,7 +162,8 @@ template <typename T, int TPR, int V, int FLOW = kFlow<T>, bool SHORT = TPR == 8
 
 // A value that the compiler takes for a new one: what is made from it inside a loop is made there.  Otherwise everything about
 // a row that its threads and length decide moves in front of the loop over rows, and costs it its registers: scalar ones
-// spilled to lanes of a vector register and read back every time.
+// spilled to lanes of a vector register and read back every time.  The norm kernels spill none; the softmax kernels, whose arguments alone
+// are 72 words for 106 registers, still do, fewer.
 __device__ __forceinline__ uint32_t again_uniform(uint32_t x) { asm volatile("" : "+s"(x)); return x; }
 __device__ __forceinline__ uint32_t again(uint32_t x) { asm volatile("" : "+v"(x)); return x; }
 

@@ -3,7 +3,9 @@
 // All of them read each input once and write each result once (rows of more than 8192 columns are read twice in the backward pass, the
 // second time from the caches), and are bound by memory in large calls, by one chain of load, reductions and store in small ones.
 // 16384 x 4096 bf16: residual sum with dropout 64 us (6.3 TB/s), norm with both and its z 93 us (5.8 TB/s), backward with both 118 us (5.7 TB/s,
-// of which k_norm_reduce 4); one row of 4096 3.4 us; 6007 x 577 f32 8.6 and 15 us.
+// of which k_norm_reduce 5); one row of 4096 3.1 us; 6007 x 577 f32 8.1 and 14.7 us.
+// The backward pass that reads twice is further off: 8192 x 8200 bf16 166 us (2.4 TB/s), 8192 x 16384 238 us (3.4), 4096 x 32768 615 us (1.3); the last
+// is the form for more than 16384 columns, which spills 94 to 98 vector registers to memory.
 #include "layers_device.h"
 
 namespace adacomp {
@@ -211,7 +213,7 @@ template <typename T, int TPR, int FLOW> __global__ __launch_bounds__(kBackThrea
 }
 
 // Rows of more than 8192 columns: the sums of V groups of columns leave no registers for the row, which is read a second time, from
-// the caches, for dz.
+// the caches, for dz.  With 4 groups the sums alone take 64 of a thread's 128 registers, and what does not fit beside them is spilled.
 template <typename T, int V> __global__ __launch_bounds__(kBackThreads) void k_norm_backward_wide(NormBackward a)
 {
     constexpr int TPR = kBackThreads;

@@ -7,9 +7,13 @@
 // adds the workgroups' sums and only then turns distances into buckets.
 //
 // Forward reads the admitted scores and writes all probabilities, backward reads scores and dprobs and writes dscores, once each;
-// a row stays in registers between its reductions.  Measured, bf16, 4 x 16 x 2048 x 2048 with dropout: forward 196 us (5.5 TB/s), causal 164 us
-// (4.9 TB/s of what it needs), backward 320 us (5.0 TB/s), with padding 293.  What bounds the large calls is memory, and in the backward
-// pass also the vector units: 340 instructions for 8 values of a wave's threads, 55 of them the generator's (without dropout 275 us).
+// a row of up to 32768 keys stays in registers between its reductions.  Measured, bf16, 4 x 16 x 2048 x 2048 with dropout: forward 197 us (5.5 TB/s),
+// causal 163 us (4.9 TB/s of what it needs), backward 319 us (5.1 TB/s), with padding 293.  What bounds the large calls is memory, and in the backward
+// pass also the vector units: 340 instructions for 8 values of a wave's threads, 55 of them the generator's (padded, without dropout 273 us).
+// Short rows are far from that, bound by what a row costs whatever its length (with dropout: forward 8000 x 16 x 17 x 17 162 us, 1.0 TB/s, 512 x 16 x
+// 100 x 100 107 us, 3.1; backward 2048 x 16 x 30 x 30 117 us, 1.6), and so is the backward pass where many distances leave few rows to a
+// workgroup (32 x 16 x 1500 x 400 with distances up to 800 643 us, 2.9 TB/s).  The kernels use all of their scalar registers, and keep 9 to 92 more values in lanes
+// of vector registers; none has vector registers in memory.
 #include <atomic>
 
 #include "layers_device.h"
@@ -503,8 +507,8 @@ constexpr uint32_t kMostWorkgroups = 1u << 20;   // of a launch, which has fewer
 SoftmaxForm softmax_form(uint32_t keys, uint32_t places, bool backward)
 {
     if (backward) {   // every row that a workgroup has in hand has its sums by distance in LDS, beside the bias
-        // and the rows get as many threads as leave room for that, with one group where it does: 64 x 16 x 600 x 250 with distances up to 800 takes
-        // 339 us in bf16 and 386 with two groups to a thread, 32 x 16 x 1500 x 400 691 and 730
+        // and the rows get as many threads as leave room for that, with one group where it does: 64 x 16 x 600 x 250 with distances up to 800 and dropout
+        // took 339 us in bf16 and 386 with two groups to a thread, 32 x 16 x 1500 x 400 691 and 730
         const uint32_t copies = kLdsMost / (4u * cells(places)) - 1u;
         if (copies < 16u && copies >= 8u && keys <= 256u) return {{32, 1}, 1};
         if (copies < 8u && copies >= 4u && keys <= 512u) return {{64, 1}, 1};
@@ -594,7 +598,7 @@ template <typename T, int TPR, int V, int PHASE, int KIND> struct KBackward { st
 
 // Shares the rows out to workgroups of the forward pass: to a team about 24000 keys, or 8 times what the bias takes to lay out, over the teams,
 // and fewer where that leaves compute units without work.  Sequences of at most a quarter of a workgroup's rows share workgroups, head by head:
-// 8000 x 16 x 17 x 17 in bf16 takes 160 us instead of 305, 4096 x 24 x 1 x 100 takes 18 instead of 148, 1024 x 16 x 60 x 60 takes 87 instead
+// 8000 x 16 x 17 x 17 in bf16 with dropout takes 160 us instead of 305, 4096 x 24 x 1 x 100 takes 18 instead of 148, 1024 x 16 x 60 x 60 takes 87 instead
 // of 89, while 512 x 16 x 100 x 100, whose rows are nearly half of a workgroup's, would take 104 instead of 97.
 static void share_rows(SoftmaxArgs &a, const SoftmaxForm &f)
 {
