@@ -11,3 +11,6 @@ from .binding import (AdacompError, adacomp_compress, adacomp_compress_static, a
 from .layers import (LAYER_EXPORTS, Dropout, RelativeBias, adacomp_bias_softmax_backward, adacomp_bias_softmax_forward,  # noqa: F401
                      adacomp_bias_softmax_workspace_bytes, adacomp_dropout, adacomp_norm_backward, adacomp_norm_forward,
                      adacomp_norm_workspace_bytes, adacomp_relative_buckets)
+from .sequence import (RECURRENCE_KEEP, SEQUENCE_EXPORTS, TEACHER_TOP_MAX, adacomp_distill_backward, adacomp_distill_forward,  # noqa: F401
+                       adacomp_embed_backward, adacomp_embed_forward, adacomp_embed_workspace_bytes, adacomp_recurrence_backward, adacomp_recurrence_forward,
+                       adacomp_recurrence_kept, adacomp_recurrence_workspace_bytes)

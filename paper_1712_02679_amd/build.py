@@ -10,7 +10,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libadacomp.so")
-SOURCES = ["adacomp_api.hip", "adacomp_kernels.hip", "layers_api.hip", "layers_norm.hip", "layers_softmax.hip"]
+SOURCES = ["adacomp_api.hip", "adacomp_kernels.hip", "layers_api.hip", "layers_norm.hip", "layers_softmax.hip",
+           "sequence_api.hip", "sequence_embed.hip", "sequence_recurrence.hip", "sequence_distill.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
@@ -31,7 +32,7 @@ def build(verbose: bool = False) -> str:
             out = os.path.join(objects, source + ".o")
             return out, subprocess.run([hipcc, *compile_flags, "-I" + os.path.join(ROOT, "include"), "-I" + CSRC, "-c", "-o", out, os.path.join(CSRC, source)],
                                        capture_output=True, text=True)
-        with concurrent.futures.ThreadPoolExecutor(max_workers=4) as pool:
+        with concurrent.futures.ThreadPoolExecutor(max_workers=8) as pool:
             done = list(pool.map(compile_one, SOURCES))
         results = [res for _, res in done]
         if all(res.returncode == 0 for res in results):

@@ -12,6 +12,9 @@ using bf16 = __bf16;
 using f16 = _Float16;
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 
+constexpr float kLog2e = 1.4426950408889634f, kLog2eRest = float(1.4426950408889634 - double(kLog2e)), kLn2 = 0.6931471805599453f;
+constexpr float kInf = __builtin_huge_valf();
+
 // 8 neighbouring values in memory.  The type's alignment is that of one value: rows of odd lengths begin anywhere, and the
 // memory pipeline takes 16-byte accesses at any address of a value.
 template <typename T> struct Raw;
@@ -270,12 +273,37 @@ template <typename OP, int WAVES> __device__ __forceinline__ float over_waves(fl
     return all;
 }
 
+// exp(x).  Exponents are in natural units, as in the formulas, so that they are finite wherever scale * score is: in units of log2 the lowest
+// bf16 value would be -infinity at a scale of 1.  16-bit tensors: the product with log2(e) is rounded, 5e-7 of the result at most where the
+// argument is about 10, far below their own rounding.  32-bit ones: that rounding is made good to first order (6 x 5 x 333 x 777: dscores
+// 3.1e-7 -> 2.3e-7 off).
+template <typename T> __device__ __forceinline__ float exp_of(float x)
+{
+    const float y = x * kLog2e, p = __builtin_amdgcn_exp2f(y);
+    if constexpr (sizeof(T) == 2) return p;
+    const float off = fabsf(x) < 200.f ? fmaf(x, kLog2e, -y) + x * kLog2eRest : 0.f;   // infinities have none
+    return fmaf(p, off * kLn2, p);
+}
+
 // Which of a workgroup's rows a thread belongs to.
 template <int TPR> __device__ __forceinline__ uint32_t team_of()
 {
     const uint32_t team = threadIdx.x / TPR;
     if constexpr (TPR >= 64) return __builtin_amdgcn_readfirstlane(team);
     return team;
+}
+
+// ---- launches -----------------------------------------------------------------------------------------------------
+
+inline int check_launch() { return hipGetLastError() == hipSuccess ? ADACOMP_OK : ADACOMP_EHIP; }
+
+// Calls f with a type.
+template <typename F> inline int with_type(uint32_t dtype, F &&f)
+{
+    if (dtype == ADACOMP_DTYPE_F32) f(float());
+    else if (dtype == ADACOMP_DTYPE_BF16) f(bf16());
+    else f(f16());
+    return check_launch();
 }
 
 }  // namespace adacomp

@@ -291,17 +291,6 @@ __global__ __launch_bounds__(1024) void k_norm_reduce(NormReduce a)
 
 // ---- launches -----------------------------------------------------------------------------------------------------
 
-static int check_launch() { return hipGetLastError() == hipSuccess ? ADACOMP_OK : ADACOMP_EHIP; }
-
-// Calls f with a type.
-template <typename F> static int with_type(uint32_t dtype, F &&f)
-{
-    if (dtype == ADACOMP_DTYPE_F32) f(float());
-    else if (dtype == ADACOMP_DTYPE_BF16) f(bf16());
-    else f(f16());
-    return check_launch();
-}
-
 // Whether all of a tensor's rows begin with a line of memory.
 static bool lines(const void *p, uint64_t stride, uint64_t size) { return !p || (reinterpret_cast<uintptr_t>(p) | stride * size) % 64u == 0u; }
 

@@ -20,27 +20,12 @@
 
 namespace adacomp {
 
-constexpr float kLog2e = 1.4426950408889634f, kLog2eRest = float(1.4426950408889634 - double(kLog2e)), kLn2 = 0.6931471805599453f;
-constexpr float kInf = __builtin_huge_valf();
-
 // The bias by distance index x = key - query + D, as far as a call can have that distance (a.places of them from a.first_place on), and the sums of its
 // gradient, lie in LDS with 8 more places at either end, so that a group of 8 keys that reaches over an end needs no clamp.  Place X = x + 8 is in cell X + X / 8: neighbouring lanes are 8 places
 // and so 9 cells apart, in different banks.  Groups begin at multiples of 8 keys, so X % 8 is the same for a whole row.
 constexpr uint32_t kGuard = 8;
 __host__ __device__ constexpr uint32_t cell(uint32_t X) { return X + (X >> 3); }
 __host__ __device__ constexpr uint32_t cells(uint32_t places) { return (cell(places - 1u + 2u * kGuard) + 3u) & ~3u; }
-
-// Exponents are in natural units, as in the formula, so that they are finite wherever scale * score is: in units of log2 the lowest
-// bf16 value would be -infinity at a scale of 1.  16-bit tensors: the product with log2(e) is rounded, 5e-7 of the result at most where the
-// argument is about 10, far below their own rounding.  32-bit ones: that rounding is made good to first order (6 x 5 x 333 x 777: dscores
-// 3.1e-7 -> 2.3e-7 off).
-template <typename T> __device__ __forceinline__ float exp_of(float x)
-{
-    const float y = x * kLog2e, p = __builtin_amdgcn_exp2f(y);
-    if constexpr (sizeof(T) == 2) return p;
-    const float off = fabsf(x) < 200.f ? fmaf(x, kLog2e, -y) + x * kLog2eRest : 0.f;   // infinities have none
-    return fmaf(p, off * kLn2, p);
-}
 
 // A workgroup's copy of its head's bias.
 __device__ __forceinline__ void stage_bias(float *bias, const SoftmaxArgs &a, uint32_t head)
@@ -493,8 +478,6 @@ __global__ __launch_bounds__(1024) void k_bias_reduce(BiasReduce a)
 }
 
 // ---- launches -----------------------------------------------------------------------------------------------------
-
-static int check_launch() { return hipGetLastError() == hipSuccess ? ADACOMP_OK : ADACOMP_EHIP; }
 
 constexpr uint32_t kPartThreads = 256, kPartGroups = 4, kPartKeys = kPartThreads * kPartGroups * 8u;
 constexpr uint32_t kLdsMost = 40u << 10;      // of a workgroup: four of them fit a compute unit

@@ -1,0 +1,88 @@
+// sequence_plan.h -- what the checks (sequence_api.hip) and the kernels (sequence_embed.hip, sequence_recurrence.hip,
+// sequence_distill.hip) of the calls in adacomp_sequence.h share: kernel arguments and the rules that choose a kernel's form.
+#pragma once
+
+#include "adacomp_sequence.h"
+#include "layers_plan.h"
+
+namespace adacomp {
+
+// ---- embedding ----------------------------------------------------------------------------------------------------
+
+struct EmbedArgs {
+    const void *tokens;
+    const float *table;   // forward
+    void *rows_of;        // y, or dy
+    float *dtable;        // backward
+    uint32_t *first;      // [vocab + 1]: where a token's places begin in order
+    uint32_t *order;      // [rows]: places, sorted by token and then by place
+    uint64_t stride, first_row;
+    uint32_t rows, vocab, cols, groups;   // groups of 8 to a row
+    uint32_t index64, accumulate;
+    uint32_t range;       // tokens that a sorting workgroup has
+    float scale;
+    DropArgs drop;
+};
+
+constexpr uint32_t kSortThreads = 1024, kSortWaves = kSortThreads / 64;
+constexpr uint32_t kSortRange = 512;   // most tokens of a sorting workgroup, which has a count of each for every wave in LDS
+inline uint32_t embed_range(uint32_t vocab) { return std::min(kSortRange, (vocab + kComputeUnits - 1u) / kComputeUnits); }
+
+int launch_embed_forward(const EmbedArgs &a, uint32_t dtype, void *stream);
+int launch_embed_backward(const EmbedArgs &a, uint32_t dtype, void *stream);
+
+// ---- gated linear recurrence --------------------------------------------------------------------------------------
+
+struct StepsArgs {
+    const void *data;
+    int64_t batch, row;
+};
+
+struct RecurrenceArgs {
+    StepsArgs x, forget, out;
+    StepsArgs y;                        // forward: y, backward: dy
+    StepsArgs dx, dforget, dout;
+    const float *bias, *first;          // first: forward: h[-1], backward: dlast
+    float *last;                        // forward: the last state, backward: dfirst
+    float *states;
+    float *dbias_parts;                 // [batch][channels]
+    const int32_t *lengths;
+    const uint8_t *resets;
+    int64_t resets_stride;
+    uint32_t batch, length, channels, slabs;   // slabs of kSlab channels
+    uint32_t kept;                             // states of a sequence
+    uint32_t first_sequence;                   // of a launch
+};
+
+constexpr uint32_t kSlab = 64;   // channels of a workgroup: a line of memory in 16 bits
+
+struct BiasSumArgs {
+    const float *parts;
+    float *dbias;
+    uint32_t count, channels, accumulate;
+};
+
+int launch_recurrence_forward(const RecurrenceArgs &a, uint32_t dtype, void *stream);
+int launch_recurrence_backward(const RecurrenceArgs &a, uint32_t dtype, void *stream);
+int launch_bias_sum(const BiasSumArgs &a, void *stream);
+
+// ---- distillation -------------------------------------------------------------------------------------------------
+
+struct DistillArgs {
+    const void *logits;
+    void *dlogits;
+    const void *teacher_tokens, *teacher_logits, *targets;
+    float *loss, *lse;          // lse: written by the forward pass, read by the backward pass
+    const float *dloss;
+    uint64_t logits_stride, dlogits_stride, tokens_stride, teacher_stride;
+    uint64_t rows;
+    uint32_t vocab, top;
+    uint32_t tokens64, targets64, teacher_dtype;
+    float per_temperature, soft, hard;   // 1 / temperature; soft temperature^2 of a loss, soft temperature of a gradient:
+    float soft_loss, soft_grad, scale;
+};
+
+enum DistillPass { LOSS, LOSS_GRAD, GRAD };
+int launch_distill(const DistillArgs &a, uint32_t dtype, DistillPass pass, void *stream);
+
+}  // namespace adacomp
