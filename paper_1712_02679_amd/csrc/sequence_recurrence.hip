@@ -58,6 +58,14 @@ template <typename T> __device__ __forceinline__ Gate gate_of(float f)
     return {on, e * on};
 }
 
+// The gate of the state, whose error is multiplied over as many places as the state lasts: the exponential that float32 tensors have, and near 1,
+// where it lasts long, the sigmoid from the exact difference.
+__device__ __forceinline__ Gate state_gate_of(float f)
+{
+    const Gate g = gate_of<float>(f);
+    return {f > 0.f ? 1.f - g.off : g.on, g.off};
+}
+
 // What comes through a place: nothing through one that begins a document, whatever it is.
 template <bool RESETS> __device__ __forceinline__ float through(float m, float h)
 {
@@ -152,7 +160,7 @@ template <typename T, int WAVES, int L> struct Place {
         const bool reset = RESETS && inside && a.resets[int64_t(b) * a.resets_stride + t] != 0;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const Gate g = gate_of<T>(f[k]);
+            const Gate g = state_gate_of(f[k]);
             on[k] = g.on;
             m[k] = !inside ? 1.f : reset ? 0.f : g.on;
             rest[k] = inside ? g.off : 0.f;
