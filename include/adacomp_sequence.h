@@ -19,7 +19,7 @@ extern "C" {
 
 /* ---- embedding ------------------------------------------------------------------------------------ */
 
-/* rows below 2^31; vocab 1 .. 2^30; cols below 2^30; tokens [rows] contiguous; stride: of y or dy, in elements.
+/* rows below 2^31; vocab 1 .. 2^30; cols up to 2^20; rows * cols up to 2^38; tokens [rows] contiguous; stride: of y or dy, in elements.
  * dropout may be NULL. */
 typedef struct {
     uint64_t rows, stride;

@@ -7,13 +7,18 @@
 
 namespace adacomp {
 
-constexpr uint64_t kMost = uint64_t(1) << 31, kMostVocab = uint64_t(1) << 30;
+constexpr uint64_t kMost = uint64_t(1) << 31, kMostVocab = uint64_t(1) << 30, kMostCols = uint64_t(1) << 20, kMostValues = uint64_t(1) << 38;
+
+static bool embed_sizes(uint64_t rows, uint64_t vocab, uint64_t cols)
+{
+    return rows < kMost && vocab != 0 && vocab <= kMostVocab && cols <= kMostCols && rows * cols <= kMostValues;
+}
 
 static int embed_args(const adacomp_embed_t *op, const adacomp_dropout_t *dropout, EmbedArgs &a)
 {
     a = EmbedArgs();
     if (!op || op->dtype > ADACOMP_DTYPE_F16 || op->reserved != 0) return ADACOMP_EINVAL;
-    if (op->rows >= kMost || op->vocab == 0 || op->vocab > kMostVocab || op->cols >= kMostVocab) return ADACOMP_EINVAL;
+    if (!embed_sizes(op->rows, op->vocab, op->cols)) return ADACOMP_EINVAL;
     if (op->index_bytes != 4 && op->index_bytes != 8) return ADACOMP_EINVAL;
     if (int rc = drop_args(dropout, a.drop)) return rc;
     if (op->rows != 0 && op->cols != 0 && !op->tokens) return ADACOMP_EINVAL;
@@ -45,7 +50,7 @@ static int steps_args(const adacomp_steps_t *steps, const adacomp_recurrence_t *
 
 static bool recurrence_sizes(uint64_t batch, uint64_t length, uint64_t channels)
 {
-    return batch < kMost && length < kMost && channels <= (uint64_t(1) << 20) && batch * length < kMost;
+    return batch < kMost && length < kMost && channels <= kMostCols && batch * length < kMost;
 }
 
 static int recurrence_args(const adacomp_recurrence_t *op, RecurrenceArgs &a)
@@ -135,8 +140,9 @@ int adacomp_embed_forward(const adacomp_embed_t *op, const float *table, void *y
 
 size_t adacomp_embed_workspace_bytes(uint64_t rows, uint32_t vocab, uint32_t cols)
 {
-    if (rows >= kMost || vocab == 0 || vocab > kMostVocab || cols >= kMostVocab) return 0;
-    return pad256((size_t(vocab) + 1u) * 4u) + pad256(size_t(rows) * 4u);
+    if (!embed_sizes(rows, vocab, cols)) return 0;
+    const EmbedForm f = embed_form(uint32_t(rows), vocab, cols);
+    return pad256((size_t(vocab) + 1u) * 4u) + pad256(size_t(rows) * sizeof(EmbedPlace)) + pad256(size_t(f.pieces) * 2u * f.pitch * 4u);
 }
 
 int adacomp_embed_backward(const adacomp_embed_t *op, const void *dy, float *dtable, const adacomp_dropout_t *dropout, int accumulate,
@@ -152,7 +158,9 @@ int adacomp_embed_backward(const adacomp_embed_t *op, const void *dy, float *dta
     a.dtable = dtable;
     a.accumulate = accumulate != 0;
     a.first = static_cast<uint32_t *>(workspace);
-    a.order = a.first + pad256((size_t(a.vocab) + 1u) * 4u) / 4u;
+    char *behind = static_cast<char *>(workspace) + pad256((size_t(a.vocab) + 1u) * 4u);
+    a.order = reinterpret_cast<EmbedPlace *>(behind);
+    a.parts = reinterpret_cast<float *>(behind + pad256(size_t(a.rows) * sizeof(EmbedPlace)));
     return launch_embed_backward(a, op->dtype, hip_stream);
 }
 

@@ -46,6 +46,8 @@ template <typename T> __global__ __launch_bounds__(256) void k_embed_forward(Emb
 // wave's places of each token go, and the waves look at their run again and put them there in order.  No workgroup waits for
 // another, and the order does not depend on which of them comes first.
 
+constexpr uint32_t kChunks = 16;   // of 64 tokens, that a wave has on their way at once
+
 __global__ __launch_bounds__(kSortThreads) void k_embed_sort(EmbedArgs a)
 {
     extern __shared__ uint32_t counts[];   // [range][waves]
@@ -53,14 +55,23 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_sort(EmbedArgs a)
     const uint32_t lane = threadIdx.x % 64u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64u);
     const uint32_t low = blockIdx.x * a.range, n = min(a.range, a.vocab - low);
     for (uint32_t i = threadIdx.x; i < n * kSortWaves; i += kSortThreads) counts[i] = 0;
-    __syncthreads();
     const uint32_t run = ((a.rows + kSortThreads - 1u) / kSortThreads) * 64u;   // places of a wave: whole chunks of 64
     const uint32_t begin = min(wave * run, a.rows), end = min(begin + run, a.rows);
+    uint32_t tokens[kChunks];
+    auto fetch = [&](uint32_t from) {
+#pragma unroll
+        for (uint32_t k = 0; k < kChunks; ++k) tokens[k] = from + k * 64u + lane < end ? token_at(a, from + k * 64u + lane) : a.vocab;
+    };
+    fetch(begin);
+    __syncthreads();
     uint32_t below = 0;
-    for (uint32_t i = begin + lane; i < end; i += 64u) {
-        const uint32_t token = token_at(a, i);
-        below += token < low ? 1u : 0u;
-        if (token - low < n) atomicAdd(&counts[(token - low) * kSortWaves + wave], 1u);
+    for (uint32_t from = begin; from < end; from += kChunks * 64u) {
+        if (from != begin) fetch(from);
+#pragma unroll
+        for (uint32_t k = 0; k < kChunks; ++k) {
+            below += tokens[k] < low ? 1u : 0u;
+            if (tokens[k] - low < n) atomicAdd(&counts[(tokens[k] - low) * kSortWaves + wave], 1u);
+        }
     }
     for (uint32_t s = 32; s > 0; s /= 2u) below += __shfl_xor(below, s);
     if (lane == 0u) room[wave] = below;
@@ -92,47 +103,139 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_sort(EmbedArgs a)
         if (lane == 0u && low + n == a.vocab) a.first[a.vocab] = base;
     }
     __syncthreads();
-    for (uint32_t i = begin; i < end; i += 64u) {
-        const bool here = i + lane < end;
-        const uint32_t t = here ? token_at(a, i + lane) - low : n;
-        uint64_t left = __ballot(t < n);
-        while (left) {   // every token among the 64, lanes in order
-            const uint32_t which = __builtin_amdgcn_readlane(t, __builtin_ctzll(left));
-            const uint64_t same = __ballot(t == which);
-            uint32_t *count = &counts[which * kSortWaves + wave];
-            if (t == which) {
-                const uint32_t before = __builtin_popcountll(same & ((uint64_t(1) << lane) - 1u));
-                const uint32_t at = *count;
-                a.order[at + before] = i + lane;
-                if (before == 0u) *count = at + __builtin_popcountll(same);
+    for (uint32_t from = begin; from < end; from += kChunks * 64u) {
+        if (run > kChunks * 64u) fetch(from);
+#pragma unroll
+        for (uint32_t k = 0; k < kChunks; ++k) {
+            const uint32_t t = tokens[k] - low;
+            uint64_t left = __ballot(t < n);
+            while (left) {   // every token among the 64, lanes in order
+                const uint32_t which = __builtin_amdgcn_readlane(t, __builtin_ctzll(left));
+                const uint64_t same = __ballot(t == which);
+                volatile uint32_t *count = &counts[which * kSortWaves + wave];
+                if (t == which) {
+                    const uint32_t before = __builtin_popcountll(same & ((uint64_t(1) << lane) - 1u));
+                    const uint32_t at = *count;
+                    a.order[at + before] = {low + t, from + k * 64u + lane};
+                    if (before == 0u) *count = at + __builtin_popcountll(same);
+                }
+                left &= ~same;
             }
-            left &= ~same;
         }
     }
 }
 
 // ---- backward: sums -----------------------------------------------------------------------------------------------
+// The order is cut into pieces of as many places, whatever their tokens are, so that a frequent token's are shared out like all others.  A team of
+// threads has a piece and a slab of columns, 8 to a thread, and adds up the rows of a token while it lasts.  A token whose places lie in
+// one piece is done then.  Of one that goes on in another piece every piece leaves its part, and k_embed_join adds the parts up in order.
+// The other workgroups of the launch write the zeros of tokens that do not occur.
 
-template <typename T> __global__ __launch_bounds__(256) void k_embed_sum(EmbedArgs a, uint64_t work, uint32_t slabs)
+constexpr uint32_t kSumThreads = 256;
+
+template <typename T, bool DROP> __global__ __launch_bounds__(kSumThreads) void k_embed_sum(EmbedArgs a)
 {
-    const Drop d = drop_of(a.drop);
-    for (uint64_t i = blockIdx.x; i < work; i += gridDim.x) {
-        const uint32_t token = uint32_t(i / slabs), c = (uint32_t(i % slabs) * 256u + threadIdx.x) * 8u;
-        if (c >= a.cols) continue;
-        const uint32_t begin = a.first[token], end = a.first[token + 1u];
-        if (begin == end && a.accumulate) continue;
-        f32x8 sum = 0.f;
-        for (uint32_t k = begin; k < end; ++k) {
-            const uint32_t row = a.order[k];
-            f32x8 v = group8(static_cast<const T *>(a.rows_of) + uint64_t(row) * a.stride, c, a.cols);
-            if (a.drop.on) v = drop8(v, d, c / 8u, row);
-            sum += v;
+    extern __shared__ EmbedPlace staged[];   // [teams][piece + 2]: the places of a piece, one before and one behind
+    constexpr uint32_t BATCH = 16u / sizeof(T);   // rows on their way at once
+    const uint32_t t = threadIdx.x & (a.team - 1u), team = threadIdx.x / a.team, teams = kSumThreads / a.team;
+    if (blockIdx.x >= a.sum_blocks) {
+        for (uint64_t v = (blockIdx.x - a.sum_blocks) * uint64_t(teams) + team; v < a.vocab; v += uint64_t(gridDim.x - a.sum_blocks) * teams) {
+            if (a.first[v] != a.first[v + 1u]) continue;
+            float *out = a.dtable + v * a.cols;
+            for (uint32_t c = t * 8u; c < a.cols; c += a.team * 8u) {
+                if (c + 8u <= a.cols) store8(out + c, f32x8(0.f));
+                else store_some(out + c, a.cols - c, f32x8(0.f));
+            }
         }
-        sum *= a.scale;
-        float *out = a.dtable + uint64_t(token) * a.cols;
-        if (a.accumulate) sum += group8(out, c, a.cols);
-        if (c + 8u <= a.cols) store8(out + c, sum);
-        else store_some(out + c, a.cols - c, sum);
+        return;
+    }
+    const Drop d = drop_of(a.drop);
+    const uint32_t job = blockIdx.x * teams + team, piece = job / a.slabs, slab = job - piece * a.slabs;
+    const uint32_t count_all = a.first[a.vocab], begin = min(piece, a.pieces) * a.piece;
+    const uint32_t count = begin < count_all && piece < a.pieces ? min(a.piece, count_all - begin) : 0u;
+    EmbedPlace *mine = staged + team * (a.piece + 2u);
+    for (uint32_t k = t; k < count + 2u; k += a.team) {   // places that there are not hold no token
+        const uint32_t at = begin + k;
+        mine[k] = at >= 1u && at <= count_all ? a.order[at - 1u] : EmbedPlace{a.vocab, 0u};
+    }
+    __syncthreads();
+    const uint32_t c = (slab * a.team + t) * 8u;
+    if (c >= a.cols) return;
+    const uint32_t cut = a.cols >= 8u && c + 8u > a.cols ? 8u - a.cols % 8u : 0u;   // an incomplete group reads the row's last 8 values
+    const T *dy = static_cast<const T *>(a.rows_of) + (c - cut);
+    const uint32_t whole_row = a.cols >= 8u;
+    f32x8 sum = 0.f;
+    uint32_t run = 0;   // where the token's run begins
+    for (uint32_t from = 0; from < count; from += BATCH) {
+        raw8<T> raw[BATCH];
+#pragma unroll
+        for (uint32_t k = 0; k < BATCH; ++k) {
+            const T *row = dy + uint64_t(mine[min(from + k, count - 1u) + 1u].row) * a.stride;
+            raw[k] = whole_row ? load8(row) : load_some(row, a.cols);
+        }
+#pragma unroll
+        for (uint32_t k = 0; k < BATCH; ++k) {
+            const uint32_t at = from + k;
+            if (at >= count) break;
+            const EmbedPlace place = mine[at + 1u];
+            f32x8 v = widen<T>(raw[k]);
+            if constexpr (DROP) {
+                if (cut) v = shifted(v, cut);
+                v = drop8(v, d, c / 8u, place.row);
+            }
+            sum += v;
+            const uint32_t next = mine[at + 2u].token;
+            if (next == place.token && at + 1u < count) continue;
+            if (!DROP && cut) sum = shifted(sum, cut);
+            const bool goes_on = next == place.token, came = run == 0u && mine[0].token == place.token;
+            const uint32_t n = a.cols - c;
+            if (came || goes_on) {   // a part: behind others, or the first of them
+                float *out = a.parts + (uint64_t(piece) * 2u + (came ? 0u : 1u)) * a.pitch + c;
+                store8(out, sum);
+            } else {
+                float *out = a.dtable + uint64_t(place.token) * a.cols + c;
+                sum *= a.scale;
+                if (a.accumulate) sum += n >= 8u ? widen<float>(load8(out)) : widen<float>(load_some(out, n));
+                if (n >= 8u) store8(out, sum);
+                else store_some(out, n, sum);
+            }
+            sum = 0.f;
+            run = at + 1u;
+        }
+    }
+}
+
+// The token that begins in a piece and goes on behind it: its parts, in order, 8 columns to each of 32 threads, 16 slices of the parts.
+constexpr uint32_t kJoinSlices = 16;
+
+__global__ __launch_bounds__(32 * kJoinSlices) void k_embed_join(EmbedArgs a)
+{
+    __shared__ f32x8 sums[kJoinSlices][32];
+    const uint32_t lane = threadIdx.x % 32u, slice = threadIdx.x / 32u, c = (blockIdx.y * 32u + lane) * 8u, n = a.cols - c;
+    for (uint32_t piece = blockIdx.x; piece + 1u < a.pieces; piece += gridDim.x) {
+        const uint32_t last = (piece + 1u) * a.piece;   // the first place behind it
+        if (last >= a.first[a.vocab]) return;
+        const uint32_t token = a.order[last].token;
+        if (a.order[last - 1u].token != token) continue;
+        const uint32_t begin = a.first[token], end = a.first[token + 1u];
+        if (begin < last - a.piece) continue;   // an earlier piece's
+        const uint32_t to = (end - 1u) / a.piece;
+        f32x8 s = 0.f;
+        if (c < a.cols) {
+            if (slice == 0u) s = widen<float>(load8(a.parts + (uint64_t(piece) * 2u + 1u) * a.pitch + c));
+#pragma unroll 4
+            for (uint32_t p = piece + 1u + slice; p <= to; p += kJoinSlices) s += widen<float>(load8(a.parts + uint64_t(p) * 2u * a.pitch + c));
+        }
+        __syncthreads();   // the token before has been added up
+        sums[slice][lane] = s;
+        __syncthreads();
+        if (slice != 0u || c >= a.cols) continue;
+        for (uint32_t k = 1; k < kJoinSlices; ++k) s += sums[k][lane];
+        s *= a.scale;
+        float *out = a.dtable + uint64_t(token) * a.cols + c;
+        if (a.accumulate) s += n >= 8u ? widen<float>(load8(out)) : widen<float>(load_some(out, n));
+        if (n >= 8u) store8(out, s);
+        else store_some(out, n, s);
     }
 }
 
@@ -156,13 +259,31 @@ int launch_embed_backward(const EmbedArgs &args, uint32_t dtype, void *stream)
 {
     EmbedArgs a = args;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    a.range = embed_range(a.vocab);
+    const EmbedForm form = embed_form(a.rows, a.vocab, a.cols);
+    a.range = form.range;
+    a.team = form.team;
+    a.slabs = form.slabs;
+    a.piece = form.piece;
+    a.pieces = form.pieces;
+    a.pitch = form.pitch;
     hipLaunchKernelGGL(k_embed_sort, dim3((a.vocab + a.range - 1u) / a.range), dim3(kSortThreads), a.range * kSortWaves * 4u, s, a);
     if (int rc = check_launch()) return rc;
-    const uint32_t slabs = (a.groups + 255u) / 256u;
-    const uint64_t work = uint64_t(a.vocab) * slabs;
-    const dim3 grid(uint32_t(std::min<uint64_t>(work, 1u << 20)));
-    return with_type(dtype, [&](auto of) { hipLaunchKernelGGL((k_embed_sum<decltype(of)>), grid, dim3(256), 0, s, a, work, slabs); });
+    const uint32_t teams = kSumThreads / a.team;
+    a.sum_blocks = uint32_t((uint64_t(a.pieces) * a.slabs + teams - 1u) / teams);
+    const uint32_t zero_blocks = a.accumulate ? 0u : std::min((a.vocab + teams - 1u) / teams, 8u * kComputeUnits);
+    if (a.sum_blocks + zero_blocks != 0u) {
+        const dim3 grid(a.sum_blocks + zero_blocks), wg(kSumThreads);
+        const uint32_t lds = teams * (a.piece + 2u) * 8u;
+        const int rc = with_type(dtype, [&](auto of) {
+            using T = decltype(of);
+            if (a.drop.on) hipLaunchKernelGGL((k_embed_sum<T, true>), grid, wg, lds, s, a);
+            else hipLaunchKernelGGL((k_embed_sum<T, false>), grid, wg, lds, s, a);
+        });
+        if (rc) return rc;
+    }
+    if (a.pieces < 2u) return ADACOMP_OK;
+    hipLaunchKernelGGL(k_embed_join, dim3(std::min(a.pieces - 1u, 1u << 20), (a.groups + 31u) / 32u), dim3(32u * kJoinSlices), 0, s, a);
+    return check_launch();
 }
 
 }  // namespace adacomp

@@ -9,24 +9,51 @@ namespace adacomp {
 
 // ---- embedding ----------------------------------------------------------------------------------------------------
 
+struct EmbedPlace { uint32_t token, row; };   // a row of the call, in the order of the tokens
+
 struct EmbedArgs {
     const void *tokens;
     const float *table;   // forward
     void *rows_of;        // y, or dy
     float *dtable;        // backward
     uint32_t *first;      // [vocab + 1]: where a token's places begin in order
-    uint32_t *order;      // [rows]: places, sorted by token and then by place
+    EmbedPlace *order;    // [rows]: places, sorted by token and then by row
+    float *parts;         // [pieces][2][pitch]
     uint64_t stride, first_row;
     uint32_t rows, vocab, cols, groups;   // groups of 8 to a row
     uint32_t index64, accumulate;
-    uint32_t range;       // tokens that a sorting workgroup has
+    uint32_t range, team, slabs, piece, pieces, pitch;   // see EmbedForm
+    uint32_t sum_blocks;  // workgroups that add up; those behind them write zeros
     float scale;
     DropArgs drop;
 };
 
 constexpr uint32_t kSortThreads = 1024, kSortWaves = kSortThreads / 64;
 constexpr uint32_t kSortRange = 512;   // most tokens of a sorting workgroup, which has a count of each for every wave in LDS
-inline uint32_t embed_range(uint32_t vocab) { return std::min(kSortRange, (vocab + kComputeUnits - 1u) / kComputeUnits); }
+
+// How a backward pass goes.
+struct EmbedForm {
+    uint32_t range;    // tokens of a sorting workgroup
+    uint32_t team;     // threads to a row, 8 columns each
+    uint32_t slabs;    // of a row, if it has more columns than a team takes
+    uint32_t piece;    // places that are added up together
+    uint32_t pieces, pitch;
+};
+
+inline EmbedForm embed_form(uint32_t rows, uint32_t vocab, uint32_t cols)
+{
+    EmbedForm f = {};
+    f.range = std::min(kSortRange, (vocab + kComputeUnits - 1u) / kComputeUnits);
+    f.team = 8;
+    while (f.team < 256u && f.team * 8u < cols) f.team *= 2u;
+    f.slabs = (cols + f.team * 8u - 1u) / (f.team * 8u);
+    // as long as there are waves for all compute units
+    f.piece = 64;
+    while (f.piece > 8u && uint64_t(rows) * f.slabs * f.team / (uint64_t(f.piece) * 64u) < 8u * kComputeUnits) f.piece /= 2u;
+    f.pieces = (rows + f.piece - 1u) / f.piece;
+    f.pitch = (cols + 7u) & ~7u;
+    return f;
+}
 
 int launch_embed_forward(const EmbedArgs &a, uint32_t dtype, void *stream);
 int launch_embed_backward(const EmbedArgs &a, uint32_t dtype, void *stream);

@@ -41,7 +41,7 @@ def test_struct_sizes():
 def test_sizes(L):
     beyond = 2 ** 32
     assert sequence.adacomp_embed_workspace_bytes(1000, 50, 8) > 0
-    for bad in ((2 ** 31, 50, 8), (1000, 0, 8), (1000, 2 ** 30 + 1, 8), (1000, 50, 2 ** 30), (beyond + 5, 50, 8), (1000, beyond + 5, 8), (1000, 50, beyond + 8), (-1, 50, 8)):
+    for bad in ((2 ** 31, 50, 8), (1000, 0, 8), (1000, 2 ** 30 + 1, 8), (1000, 50, 2 ** 20 + 1), (2 ** 30, 50, 2 ** 9), (beyond + 5, 50, 8), (1000, beyond + 5, 8), (1000, 50, beyond + 8), (-1, 50, 8)):
         assert sequence.adacomp_embed_workspace_bytes(*bad) == 0, bad
     assert 0 < sequence.adacomp_embed_workspace_bytes(0, 1, 0) <= 1024
     assert sequence.adacomp_recurrence_workspace_bytes(8, 100, 64) > 0
@@ -62,7 +62,7 @@ def test_refusals_by_code(L):
     forward = lambda op=None, table=base, y=out, d=None: L.adacomp_embed_forward(op or embed(), table, y, d, None)
     backward = lambda op=None, dy=base, dtable=out, d=None, w=ws, n=1 << 14: L.adacomp_embed_backward(op or embed(), dy, dtable, d, 0, w, n, None)
     for call in (forward, backward):
-        for op in (embed(rows=2 ** 31), embed(vocab=0), embed(vocab=2 ** 30 + 1), embed(cols=2 ** 30), embed(dtype=3), embed(index=2), embed(tokens=None), embed(reserved=1)):
+        for op in (embed(rows=2 ** 31), embed(vocab=0), embed(vocab=2 ** 30 + 1), embed(cols=2 ** 20 + 1), embed(rows=2 ** 30, cols=2 ** 9), embed(dtype=3), embed(index=2), embed(tokens=None), embed(reserved=1)):
             assert call(op) == binding.EINVAL
         assert call(embed(tokens=base + 4)) == binding.EALIGN and call(embed(index=4, tokens=base + 2)) == binding.EALIGN
         assert call(d=drop(1.0)) == binding.EINVAL
