@@ -50,19 +50,32 @@ constexpr uint32_t kChunks = 16;   // of 64 tokens, that a wave has on their way
 
 __global__ __launch_bounds__(kSortThreads) void k_embed_sort(EmbedArgs a)
 {
-    extern __shared__ uint32_t counts[];   // [range][waves]
+    extern __shared__ uint32_t counts[];   // [waves][range]
     __shared__ uint32_t room[kSortWaves];
     const uint32_t lane = threadIdx.x % 64u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64u);
     const uint32_t low = blockIdx.x * a.range, n = min(a.range, a.vocab - low);
     for (uint32_t i = threadIdx.x; i < n * kSortWaves; i += kSortThreads) counts[i] = 0;
     const uint32_t run = ((a.rows + kSortThreads - 1u) / kSortThreads) * 64u;   // places of a wave: whole chunks of 64
     const uint32_t begin = min(wave * run, a.rows), end = min(begin + run, a.rows);
-    uint32_t tokens[kChunks];
+    uint32_t tokens[kChunks], *mine = counts + wave * n;
+    const uint32_t hits_of_run = (run / 64u + 31u) / 32u;   // chunks to a bit of `hits`
+    uint32_t hits = 0;
+    // no branch around a load: they are on their way together
     auto fetch = [&](uint32_t from) {
+        if (a.index64) {
+            int64_t raw[kChunks];
 #pragma unroll
-        for (uint32_t k = 0; k < kChunks; ++k) tokens[k] = from + k * 64u + lane < end ? token_at(a, from + k * 64u + lane) : a.vocab;
+            for (uint32_t k = 0; k < kChunks; ++k) raw[k] = static_cast<const int64_t *>(a.tokens)[min(from + k * 64u + lane, a.rows - 1u)];
+#pragma unroll
+            for (uint32_t k = 0; k < kChunks; ++k) tokens[k] = uint64_t(raw[k]) < a.vocab ? uint32_t(raw[k]) : a.vocab;
+        } else {
+#pragma unroll
+            for (uint32_t k = 0; k < kChunks; ++k) tokens[k] = static_cast<const uint32_t *>(a.tokens)[min(from + k * 64u + lane, a.rows - 1u)];
+        }
+#pragma unroll
+        for (uint32_t k = 0; k < kChunks; ++k) tokens[k] = from + k * 64u + lane < end ? min(tokens[k], a.vocab) : a.vocab;
     };
-    fetch(begin);
+    if (begin < end) fetch(begin);
     __syncthreads();
     uint32_t below = 0;
     for (uint32_t from = begin; from < end; from += kChunks * 64u) {
@@ -70,7 +83,9 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_sort(EmbedArgs a)
 #pragma unroll
         for (uint32_t k = 0; k < kChunks; ++k) {
             below += tokens[k] < low ? 1u : 0u;
-            if (tokens[k] - low < n) atomicAdd(&counts[(tokens[k] - low) * kSortWaves + wave], 1u);
+            const bool here = tokens[k] - low < n;
+            if (__ballot(here)) hits |= 1u << ((from - begin) / 64u + k) / hits_of_run;
+            if (here) atomicAdd(&mine[tokens[k] - low], 1u);
         }
     }
     for (uint32_t s = 32; s > 0; s /= 2u) below += __shfl_xor(below, s);
@@ -81,21 +96,22 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_sort(EmbedArgs a)
     // counts, token by token and in each wave by wave, become where they begin: the first wave adds them up, 64 tokens at a time
     if (wave == 0u) {
         for (uint32_t t = 0; t < n; t += 64u) {
-            uint32_t mine = 0;
+            uint32_t all = 0;
             if (t + lane < n)
-                for (uint32_t w = 0; w < kSortWaves; ++w) mine += counts[(t + lane) * kSortWaves + w];
-            uint32_t upto = mine;
+#pragma unroll
+                for (uint32_t w = 0; w < kSortWaves; ++w) all += counts[w * n + t + lane];
+            uint32_t upto = all;
             for (uint32_t s = 1; s < 64u; s *= 2u) {
                 const uint32_t other = __shfl_up(upto, s);
                 if (lane >= s) upto += other;
             }
-            uint32_t at = base + upto - mine;
+            uint32_t at = base + upto - all;
             base += __shfl(upto, 63);
             if (t + lane < n) {
                 a.first[low + t + lane] = at;
                 for (uint32_t w = 0; w < kSortWaves; ++w) {
-                    const uint32_t c = counts[(t + lane) * kSortWaves + w];
-                    counts[(t + lane) * kSortWaves + w] = at;
+                    const uint32_t c = counts[w * n + t + lane];
+                    counts[w * n + t + lane] = at;
                     at += c;
                 }
             }
@@ -104,6 +120,8 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_sort(EmbedArgs a)
     }
     __syncthreads();
     for (uint32_t from = begin; from < end; from += kChunks * 64u) {
+        const uint32_t chunk = (from - begin) / 64u;
+        if (!(hits >> chunk / hits_of_run & (2u << (chunk + kChunks - 1u) / hits_of_run - chunk / hits_of_run) - 1u)) continue;   // none of these is here
         if (run > kChunks * 64u) fetch(from);
 #pragma unroll
         for (uint32_t k = 0; k < kChunks; ++k) {
@@ -112,7 +130,7 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_sort(EmbedArgs a)
             while (left) {   // every token among the 64, lanes in order
                 const uint32_t which = __builtin_amdgcn_readlane(t, __builtin_ctzll(left));
                 const uint64_t same = __ballot(t == which);
-                volatile uint32_t *count = &counts[which * kSortWaves + wave];
+                volatile uint32_t *count = &mine[which];
                 if (t == which) {
                     const uint32_t before = __builtin_popcountll(same & ((uint64_t(1) << lane) - 1u));
                     const uint32_t at = *count;
@@ -214,16 +232,16 @@ __global__ __launch_bounds__(32 * kJoinSlices) void k_embed_join(EmbedArgs a)
     const uint32_t lane = threadIdx.x % 32u, slice = threadIdx.x / 32u, c = (blockIdx.y * 32u + lane) * 8u, n = a.cols - c;
     for (uint32_t piece = blockIdx.x; piece + 1u < a.pieces; piece += gridDim.x) {
         const uint32_t last = (piece + 1u) * a.piece;   // the first place behind it
-        if (last >= a.first[a.vocab]) return;
-        const uint32_t token = a.order[last].token;
-        if (a.order[last - 1u].token != token) continue;
+        const uint32_t all = a.first[a.vocab], token = a.order[last].token, before = a.order[last - 1u].token;   // on their way together
+        if (last >= all) return;
+        if (before != token) continue;
         const uint32_t begin = a.first[token], end = a.first[token + 1u];
         if (begin < last - a.piece) continue;   // an earlier piece's
         const uint32_t to = (end - 1u) / a.piece;
         f32x8 s = 0.f;
         if (c < a.cols) {
             if (slice == 0u) s = widen<float>(load8(a.parts + (uint64_t(piece) * 2u + 1u) * a.pitch + c));
-#pragma unroll 4
+#pragma unroll 8
             for (uint32_t p = piece + 1u + slice; p <= to; p += kJoinSlices) s += widen<float>(load8(a.parts + uint64_t(p) * 2u * a.pitch + c));
         }
         __syncthreads();   // the token before has been added up
