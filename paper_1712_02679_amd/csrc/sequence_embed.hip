@@ -109,10 +109,13 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_sort(EmbedArgs a)
             base += __shfl(upto, 63);
             if (t + lane < n) {
                 a.first[low + t + lane] = at;
+                uint32_t of_wave[kSortWaves];
+#pragma unroll
+                for (uint32_t w = 0; w < kSortWaves; ++w) of_wave[w] = counts[w * n + t + lane];
+#pragma unroll
                 for (uint32_t w = 0; w < kSortWaves; ++w) {
-                    const uint32_t c = counts[w * n + t + lane];
                     counts[w * n + t + lane] = at;
-                    at += c;
+                    at += of_wave[w];
                 }
             }
         }
@@ -146,7 +149,7 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_sort(EmbedArgs a)
 // ---- backward: sums -----------------------------------------------------------------------------------------------
 // The order is cut into pieces of as many places, whatever their tokens are, so that a frequent token's are shared out like all others.  A team of
 // threads has a piece and a slab of columns, 8 to a thread, and adds up the rows of a token while it lasts.  A token whose places lie in
-// one piece is done then.  Of one that goes on in another piece every piece leaves its part, and k_embed_join adds the parts up in order.
+// one piece is done then.  Of one that goes on in another piece every piece leaves its part, and k_embed_join adds them up in order.
 // The other workgroups of the launch write the zeros of tokens that do not occur.
 
 constexpr uint32_t kSumThreads = 256;
@@ -223,37 +226,57 @@ template <typename T, bool DROP> __global__ __launch_bounds__(kSumThreads) void 
     }
 }
 
-// The token that begins in a piece and goes on behind it: its parts, in order, 8 columns to each of 32 threads, 16 slices of the parts.
-constexpr uint32_t kJoinSlices = 16;
+// Tokens whose places lie in several pieces: their parts, in order.  A workgroup has the tokens of a sorting workgroup and 256 columns, 8 to each of
+// 32 threads; of a token with many parts each of its 16 slices of threads takes every 16th, tokens of few parts are the slices' own.
+constexpr uint32_t kJoinSlices = 16, kFewParts = 8;
 
 __global__ __launch_bounds__(32 * kJoinSlices) void k_embed_join(EmbedArgs a)
 {
     __shared__ f32x8 sums[kJoinSlices][32];
+    __shared__ uint32_t list[2][kSortRange], count[2];   // tokens of few parts, of many
     const uint32_t lane = threadIdx.x % 32u, slice = threadIdx.x / 32u, c = (blockIdx.y * 32u + lane) * 8u, n = a.cols - c;
-    for (uint32_t piece = blockIdx.x; piece + 1u < a.pieces; piece += gridDim.x) {
-        const uint32_t last = (piece + 1u) * a.piece;   // the first place behind it
-        const uint32_t all = a.first[a.vocab], token = a.order[last].token, before = a.order[last - 1u].token;   // on their way together
-        if (last >= all) return;
-        if (before != token) continue;
-        const uint32_t begin = a.first[token], end = a.first[token + 1u];
-        if (begin < last - a.piece) continue;   // an earlier piece's
-        const uint32_t to = (end - 1u) / a.piece;
-        f32x8 s = 0.f;
-        if (c < a.cols) {
-            if (slice == 0u) s = widen<float>(load8(a.parts + (uint64_t(piece) * 2u + 1u) * a.pitch + c));
-#pragma unroll 8
-            for (uint32_t p = piece + 1u + slice; p <= to; p += kJoinSlices) s += widen<float>(load8(a.parts + uint64_t(p) * 2u * a.pitch + c));
-        }
-        __syncthreads();   // the token before has been added up
-        sums[slice][lane] = s;
-        __syncthreads();
-        if (slice != 0u || c >= a.cols) continue;
-        for (uint32_t k = 1; k < kJoinSlices; ++k) s += sums[k][lane];
+    const uint32_t low = blockIdx.x * a.range, tokens = min(a.range, a.vocab - low);
+    if (threadIdx.x < 2u) count[threadIdx.x] = 0;
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < tokens; i += 32u * kJoinSlices) {
+        const uint32_t begin = a.first[low + i], end = a.first[low + i + 1u];
+        if (begin == end || begin / a.piece == (end - 1u) / a.piece) continue;
+        const uint32_t many = (end - 1u) / a.piece - begin / a.piece >= kFewParts;
+        list[many][atomicAdd(&count[many], 1u)] = low + i;   // in any order: tokens have nothing to do with each other
+    }
+    __syncthreads();
+    const bool live = c < a.cols;
+    auto part = [&](uint32_t p, uint32_t begin) {   // the first part of a token lies behind its piece's others
+        return widen<float>(load8(a.parts + (uint64_t(p) * 2u + (p == begin ? 1u : 0u)) * a.pitch + c));
+    };
+    auto put = [&](uint32_t token, f32x8 s) {
         s *= a.scale;
         float *out = a.dtable + uint64_t(token) * a.cols + c;
         if (a.accumulate) s += n >= 8u ? widen<float>(load8(out)) : widen<float>(load_some(out, n));
         if (n >= 8u) store8(out, s);
         else store_some(out, n, s);
+    };
+    if (live)
+        for (uint32_t i = slice; i < count[0]; i += kJoinSlices) {
+            const uint32_t token = list[0][i], begin = a.first[token] / a.piece, last = (a.first[token + 1u] - 1u) / a.piece;
+            f32x8 s = part(begin, begin);
+#pragma unroll 4
+            for (uint32_t p = begin + 1u; p <= last; ++p) s += part(p, begin);
+            put(token, s);
+        }
+    for (uint32_t i = 0; i < count[1]; ++i) {
+        const uint32_t token = list[1][i], begin = a.first[token] / a.piece, last = (a.first[token + 1u] - 1u) / a.piece;
+        f32x8 s = 0.f;
+        if (live)
+#pragma unroll 8
+            for (uint32_t p = begin + slice; p <= last; p += kJoinSlices) s += part(p, begin);
+        sums[slice][lane] = s;
+        __syncthreads();
+        if (slice == 0u && live) {
+            for (uint32_t k = 1; k < kJoinSlices; ++k) s += sums[k][lane];
+            put(token, s);
+        }
+        __syncthreads();   // the sums have been read
     }
 }
 
@@ -300,7 +323,7 @@ int launch_embed_backward(const EmbedArgs &args, uint32_t dtype, void *stream)
         if (rc) return rc;
     }
     if (a.pieces < 2u) return ADACOMP_OK;
-    hipLaunchKernelGGL(k_embed_join, dim3(std::min(a.pieces - 1u, 1u << 20), (a.groups + 31u) / 32u), dim3(32u * kJoinSlices), 0, s, a);
+    hipLaunchKernelGGL(k_embed_join, dim3((a.vocab + a.range - 1u) / a.range, (a.groups + 31u) / 32u), dim3(32u * kJoinSlices), 0, s, a);
     return check_launch();
 }
 
