@@ -46,7 +46,6 @@ int adacomp_embed_backward(const adacomp_embed_t *op, const void *dy, float *dta
  *   a[t] = sigmoid(forget[t] + bias),  m[t] = a[t], or 0 where resets[t] != 0 (a document begins there)
  *   h[t] = m[t] h[t - 1] + (1 - a[t]) x[t],  y[t] = sigmoid(out[t]) h[t], or h[t] without out
  * Places from lengths[b] on are padding: not looked at, the state stays what it is, y and gradients are zeros there.
- * Arguments of a sigmoid count as at least -80.
  * Backward, with G[t] = sigmoid(out[t]) dy[t] + m[t + 1] G[t + 1], at the sequence's last place dlast added:
  *   dx = (1 - a) G,  dforget = a (1 - a) (p - x) G with p[t] = h[t - 1], or 0 where resets[t] != 0,
  *   dout = sigmoid(out) sigmoid(-out) h dy,  dbias = sum of dforget over all places,  dfirst = m[0] G[0]

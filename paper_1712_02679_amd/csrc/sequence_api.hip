@@ -48,6 +48,9 @@ static int steps_args(const adacomp_steps_t *steps, const adacomp_recurrence_t *
     return ADACOMP_OK;
 }
 
+// Whether 64 rows lie within 32 bits of the first one.
+static bool near_rows(const StepsArgs &s) { return s.row >= 0 && s.row < int64_t(1) << 23; }
+
 static bool recurrence_sizes(uint64_t batch, uint64_t length, uint64_t channels)
 {
     return batch < kMost && length < kMost && channels <= kMostCols && batch * length < kMost;
@@ -67,8 +70,14 @@ static int recurrence_args(const adacomp_recurrence_t *op, RecurrenceArgs &a)
     a.channels = op->channels;
     a.slabs = (op->channels + kSlab - 1u) / kSlab;
     a.kept = (op->length + ADACOMP_RECURRENCE_KEEP - 1u) / ADACOMP_RECURRENCE_KEEP;
+    const RecurrenceForm form = recurrence_form(op->batch, op->length, op->channels);
+    a.segments = form.segments;
+    a.segment = form.segment;
     return ADACOMP_OK;
 }
+
+// Bytes of the sums of the bias gradient; changes of the parts follow them.
+static size_t recurrence_sums(const RecurrenceForm &form, uint64_t batch, uint64_t channels) { return pad256(size_t(batch) * form.segments * channels * 4u); }
 
 static bool finite_at_least(float x, float least) { return std::isfinite(x) && x >= least; }
 
@@ -167,7 +176,9 @@ int adacomp_embed_backward(const adacomp_embed_t *op, const void *dy, float *dta
 size_t adacomp_recurrence_workspace_bytes(uint32_t batch, uint32_t length, uint32_t channels)
 {
     if (!recurrence_sizes(batch, length, channels)) return 0;
-    return std::max<size_t>(256u, pad256(size_t(batch) * channels * 4u));
+    const RecurrenceForm form = recurrence_form(batch, length, channels);
+    const size_t sums = recurrence_sums(form, batch, channels);
+    return std::max<size_t>(256u, sums + (form.segments > 1u ? 2u * sums : 0u));
 }
 
 int adacomp_recurrence_forward(const adacomp_recurrence_t *op, const adacomp_steps_t *x, const adacomp_steps_t *forget, const adacomp_steps_t *out,
@@ -187,6 +198,8 @@ int adacomp_recurrence_forward(const adacomp_recurrence_t *op, const adacomp_ste
     a.first = first;
     a.last = last;
     a.states = states;
+    a.near_rows = near_rows(a.x) && near_rows(a.forget) && near_rows(a.out) && near_rows(a.y);
+    a.changes = reinterpret_cast<float *>(static_cast<char *>(workspace) + recurrence_sums({a.segments, a.segment}, a.batch, a.channels));
     return launch_recurrence_forward(a, op->dtype, hip_stream);
 }
 
@@ -212,14 +225,16 @@ int adacomp_recurrence_backward(const adacomp_recurrence_t *op, const adacomp_st
     if (a.batch != 0) {
         if (a.length != 0 && !states) return ADACOMP_EINVAL;
         if (int rc = workspace_check(workspace, workspace_bytes, adacomp_recurrence_workspace_bytes(op->batch, op->length, op->channels))) return rc;
+        a.near_rows = near_rows(a.x) && near_rows(a.forget) && near_rows(a.out) && near_rows(a.y) && near_rows(a.dx) && near_rows(a.dforget) && near_rows(a.dout);
         a.first = dlast;
         a.last = dfirst;
         a.states = const_cast<float *>(states);
         a.dbias_parts = dbias ? static_cast<float *>(workspace) : nullptr;
+        a.changes = reinterpret_cast<float *>(static_cast<char *>(workspace) + recurrence_sums({a.segments, a.segment}, a.batch, a.channels));
         if (int rc = launch_recurrence_backward(a, op->dtype, hip_stream)) return rc;
     }
     if (!dbias) return ADACOMP_OK;
-    return launch_bias_sum({a.dbias_parts, dbias, a.batch, a.channels, accumulate != 0}, hip_stream);
+    return launch_bias_sum({a.dbias_parts, dbias, a.batch * a.segments, a.channels, accumulate != 0}, hip_stream);
 }
 
 int adacomp_distill_forward(const adacomp_distill_t *op, const void *logits, float *loss, float *lse, const float *dloss, void *dlogits,

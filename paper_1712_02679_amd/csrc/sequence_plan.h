@@ -72,16 +72,33 @@ struct RecurrenceArgs {
     const float *bias, *first;          // first: forward: h[-1], backward: dlast
     float *last;                        // forward: the last state, backward: dfirst
     float *states;
-    float *dbias_parts;                 // [batch][channels]
+    float *dbias_parts;                 // [batch][segments][channels]
+    float *changes;                     // [batch][segments][2][channels]: what a part does to the state
     const int32_t *lengths;
     const uint8_t *resets;
     int64_t resets_stride;
     uint32_t batch, length, channels, slabs;   // slabs of kSlab channels
     uint32_t kept;                             // states of a sequence
+    uint32_t segments, segment;                // parts of a sequence, places of a part
     uint32_t first_sequence;                   // of a launch
+    uint32_t near_rows;                        // rows of all tensors are so near that a wave's lie within 32 bits
 };
 
 constexpr uint32_t kSlab = 64;   // channels of a workgroup: a line of memory in 16 bits
+
+// Into how many parts a sequence is cut, and how many places a part has: one where every compute unit has a workgroup anyway, as parts are read
+// twice; otherwise as many as give two (8 x 2048 x 2048 bf16, 256 workgroups, in one / two parts: 53 / 76 us, backward 133 / 144; 4 x 2048 x 2048 in two /
+// four / eight: 53 / 41 / 43 us, backward 101 / 75 / 77).
+struct RecurrenceForm { uint32_t segments, segment; };
+inline RecurrenceForm recurrence_form(uint32_t batch, uint32_t length, uint32_t channels)
+{
+    constexpr uint32_t kLeast = 256;   // places of a part, whole blocks of a workgroup
+    const uint64_t workgroups = uint64_t(batch) * ((channels + kSlab - 1u) / kSlab);
+    if (workgroups == 0 || workgroups >= kComputeUnits || length == 0) return {1u, std::max(length, 1u)};
+    const uint64_t wanted = std::min<uint64_t>((2u * kComputeUnits + workgroups - 1u) / workgroups, (length + kLeast - 1u) / kLeast);
+    const uint32_t segment = uint32_t((length + wanted - 1u) / wanted + kLeast - 1u) / kLeast * kLeast;
+    return {(length + segment - 1u) / segment, segment};
+}
 
 struct BiasSumArgs {
     const float *parts;

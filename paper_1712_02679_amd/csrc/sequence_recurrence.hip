@@ -17,16 +17,14 @@ template <typename T> using raw4 = typename Raw4<T>::vec;
 using f32x4 = raw4<float>;
 
 // The 4 channels that a thread has, of which the last thread of a row may share some with its neighbour: it reads the row's last 4
-// and writes those from `own` on.
+// and writes those from `own` on.  Threads behind the row's end read its last 4 as well, and write none.
 struct Channels {
     uint32_t first, own, count;   // count: channels read, 4 but in rows of fewer
-    bool live;
     __device__ __forceinline__ Channels(uint32_t c, uint32_t channels)
     {
-        live = c < channels;
         count = min(channels, 4u);
         first = min(c, channels - count);
-        own = live ? c - first : 4u;
+        own = c < channels ? c - first : 4u;
     }
     template <typename T> __device__ __forceinline__ raw4<T> load(const T *p) const   // p: at the row's channel `first`
     {
@@ -49,21 +47,33 @@ struct Channels {
 
 template <typename T> __device__ __forceinline__ f32x4 widen4(raw4<T> v) { return __builtin_convertvector(v, f32x4); }
 
-struct Gate { float on, off; };   // sigmoid(f), sigmoid(-f)
-
-// 1 - sigmoid as a value of its own: near 1 the difference would have lost its digits.  Below -80 exp(-f) would leave the range.
-template <typename T> __device__ __forceinline__ Gate gate_of(float f)
+// Values that the compiler takes for new ones: it would keep them widened across the scan otherwise, in twice the registers.
+template <typename T, int L> __device__ __forceinline__ void renew(raw4<T> (&v)[L])
 {
-    const float e = exp_of<T>(-(f < -80.f ? -80.f : f)), on = __builtin_amdgcn_rcpf(1.f + e);
-    return {on, e * on};
+    typedef uint32_t words __attribute__((ext_vector_type(sizeof(T))));
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+        words w = __builtin_bit_cast(words, v[i]);
+#pragma unroll
+        for (uint32_t k = 0; k < sizeof(T); ++k) w[k] = again(w[k]);
+        v[i] = __builtin_bit_cast(raw4<T>, w);
+    }
 }
 
-// The gate of the state, whose error is multiplied over as many places as the state lasts: the exponential that float32 tensors have, and near 1,
-// where it lasts long, the sigmoid from the exact difference.
-__device__ __forceinline__ Gate state_gate_of(float f)
+// sigmoid(f) and sigmoid(-f), from e = exp(-|f|), which cannot leave the range: the smaller one is e / (1 + e), the larger one what is missing to 1.
+// That difference is exact to half a step of the last place, where the reciprocal is not; a state that lasts for thousands of places
+// has been multiplied by it as often.
+struct Gate { float on, off; };
+template <typename T> __device__ __forceinline__ Gate gate_of(float f)
 {
-    const Gate g = gate_of<float>(f);
-    return {f > 0.f ? 1.f - g.off : g.on, g.off};
+    const float e = exp_of<T>(-fabsf(f)), small = e * __builtin_amdgcn_rcpf(1.f + e), big = 1.f - small;
+    return {f > 0.f ? big : small, f > 0.f ? small : big};
+}
+// Where sigmoid(f) alone is wanted and only rounded.  exp(-f) may be an infinity: 1 / (1 + it) is 0.
+template <typename T> __device__ __forceinline__ float sigmoid_of(float f)
+{
+    if constexpr (sizeof(T) == 2) return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(f * -kLog2e));
+    return gate_of<T>(f).on;
 }
 
 // What comes through a place: nothing through one that begins a document, whatever it is.
@@ -83,29 +93,46 @@ template <bool RESETS> __device__ __forceinline__ f32x4 applied(const Change &c,
     for (int k = 0; k < 4; ++k) r[k] = RESETS ? through<RESETS>(c.m[k], h[k]) + c.v[k] : fmaf(c.m[k], h[k], c.v[k]);
     return r;
 }
+// One change and then another.
+template <bool RESETS> __device__ __forceinline__ Change then(const Change &one, const Change &other) { return {one.m * other.m, applied<RESETS>(other, one.v)}; }
 
-// Over the 4 groups of 16 lanes of a wave, in their order or (BACK) from the last: what lies before each group, and `all`, valid in the
-// last one (BACK: the first).
+// x of the even and the odd one of each two neighbouring groups of 16 lanes; of the lower and the upper half of the wave.
+struct Two { float first, second; };
+__device__ __forceinline__ Two groups_of(float x)
+{
+    const uint32_t b = __builtin_bit_cast(uint32_t, x);
+    const auto r = __builtin_amdgcn_permlane16_swap(b, b, false, false);
+    return {__builtin_bit_cast(float, uint32_t(r[0])), __builtin_bit_cast(float, uint32_t(r[1]))};
+}
+__device__ __forceinline__ Two halves_of(float x)
+{
+    const uint32_t b = __builtin_bit_cast(uint32_t, x);
+    const auto r = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+    return {__builtin_bit_cast(float, uint32_t(r[0])), __builtin_bit_cast(float, uint32_t(r[1]))};
+}
+
+// Over the 4 groups of 16 lanes of a wave, in their order or (BACK) from the last: what lies before each group, and `all` of them.
 template <bool RESETS, bool BACK> __device__ __forceinline__ Change before_groups(const Change &own, Change &all)
 {
-    const uint32_t group = threadIdx.x % 64u / 16u, order = BACK ? 3u - group : group;
-    auto from = [](float x, uint32_t by) { return BACK ? __shfl_down(x, by) : __shfl_up(x, by); };
-    Change c = own;
+    const uint32_t group = threadIdx.x % 64u / 16u;
+    Change even, odd, lower, upper;
 #pragma unroll
-    for (uint32_t step = 1; step < 4u; step *= 2u) {
-        Change other;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) { other.m[k] = from(c.m[k], 16u * step); other.v[k] = from(c.v[k], 16u * step); }
-        if (order >= step) {
-            c.v = applied<RESETS>(c, other.v);
-            c.m *= other.m;
-        }
+    for (int k = 0; k < 4; ++k) {
+        const Two m = groups_of(own.m[k]), v = groups_of(own.v[k]);
+        even.m[k] = m.first; odd.m[k] = m.second;
+        even.v[k] = v.first; odd.v[k] = v.second;
     }
-    all = c;
-    Change before;
+    const Change pair = BACK ? then<RESETS>(odd, even) : then<RESETS>(even, odd);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) { before.m[k] = from(c.m[k], 16u); before.v[k] = from(c.v[k], 16u); }
-    if (order == 0u) { before.m = 1.f; before.v = 0.f; }
+    for (int k = 0; k < 4; ++k) {
+        const Two m = halves_of(pair.m[k]), v = halves_of(pair.v[k]);
+        lower.m[k] = m.first; upper.m[k] = m.second;
+        lower.v[k] = v.first; upper.v[k] = v.second;
+    }
+    all = BACK ? then<RESETS>(upper, lower) : then<RESETS>(lower, upper);
+    Change before = {1.f, 0.f};
+    if (BACK ? group < 2u : group >= 2u) before = BACK ? upper : lower;   // the other pair
+    if (BACK ? group % 2u == 0u : group % 2u == 1u) before = then<RESETS>(before, BACK ? odd : even);   // the other one of the pair
     return before;
 }
 
@@ -114,10 +141,10 @@ template <bool RESETS, bool BACK> __device__ __forceinline__ Change before_group
 template <int WAVES, bool RESETS, bool BACK>
 __device__ __forceinline__ f32x4 begin_of(const Change &own, f32x4 &carry, Change (&room)[WAVES][16])
 {
-    const uint32_t lane = threadIdx.x % 64u, wave = threadIdx.x / 64u;
+    const uint32_t lane = threadIdx.x % 64u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64u);
     Change all;
     const Change before = before_groups<RESETS, BACK>(own, all);
-    if (lane / 16u == (BACK ? 0u : 3u)) room[wave][lane % 16u] = all;
+    if (lane < 16u) room[wave][lane] = all;
     __syncthreads();
     f32x4 mine = carry;
 #pragma unroll
@@ -129,174 +156,413 @@ __device__ __forceinline__ f32x4 begin_of(const Change &own, f32x4 &carry, Chang
     return applied<RESETS>(before, mine);
 }
 
-// What a thread has to do with.
+// Which part of which sequence a workgroup has: slabs of a part are neighbours.
+struct Job {
+    uint32_t slab, segment, sequence, begin, end;   // places of the part
+    __device__ __forceinline__ explicit Job(const RecurrenceArgs &a) : slab(blockIdx.x % a.slabs)
+    {
+        const uint32_t i = blockIdx.x / a.slabs;
+        segment = i % a.segments;
+        sequence = a.first_sequence + i / a.segments;
+        begin = segment * a.segment;
+        end = uint32_t(min(uint64_t(a.length), (segment + 1ull) * a.segment));
+    }
+};
+
+// A tensor as a thread sees it.
+struct Steps {
+    const char *base;    // of the sequence; the same for a workgroup
+    int64_t row;         // bytes
+    uint32_t offset;     // of the thread from its wave's first place, where that is near
+    template <typename T> __device__ __forceinline__ void set(const StepsArgs &s, uint32_t sequence, uint32_t places, uint32_t first)
+    {
+        base = static_cast<const char *>(s.data) + int64_t(sequence) * s.batch * int64_t(sizeof(T));
+        row = s.row * int64_t(sizeof(T));
+        offset = places * uint32_t(row) + first * uint32_t(sizeof(T));
+    }
+};
+
+// What a thread has to do with: 4 channels and runs of L places.
 template <typename T, int WAVES, int L> struct Place {
     static constexpr uint32_t kSteps = WAVES * 4u * L;   // places of a block
     Channels ch;
-    uint32_t b, run, length, end;   // run: first place inside a block; end: of the sequence
+    uint32_t b, wave, run, length, end;   // run: first place inside a block; end: of the sequence
+    bool whole;                           // all of the workgroup's channels are there, and its rows near each other
     f32x4 bias;
-    __device__ __forceinline__ Place(const RecurrenceArgs &a, uint32_t slab, uint32_t sequence)
-        : ch(slab * kSlab + threadIdx.x % 16u * 4u, a.channels), b(sequence), run(threadIdx.x / 16u * L), length(a.length), end(a.length)
+    __device__ __forceinline__ Place(const RecurrenceArgs &a, const Job &job)
+        : ch(job.slab * kSlab + threadIdx.x % 16u * 4u, a.channels), b(job.sequence), wave(__builtin_amdgcn_readfirstlane(threadIdx.x / 64u)),
+          run(threadIdx.x / 16u * L), length(a.length), end(a.length), whole(a.near_rows && (job.slab + 1u) * kSlab <= a.channels)
     {
         if (a.lengths) end = uint32_t(min(max(a.lengths[b], 0), int32_t(a.length)));
         bias = 0.f;
         if (a.bias) bias = ch.load(a.bias + ch.first);
     }
-    template <typename S> __device__ __forceinline__ S *row(const StepsArgs &s, uint32_t t) const
+    __device__ __forceinline__ Steps steps(const StepsArgs &s) const
     {
-        return static_cast<S *>(const_cast<void *>(s.data)) + (int64_t(b) * s.batch + int64_t(t) * s.row + ch.first);
+        Steps r = {};
+        if (s.data) r.template set<T>(s, b, threadIdx.x % 64u / 16u * L, ch.first);
+        return r;
     }
-    // the thread's places from t on; zeros behind the sequence's end
-    __device__ __forceinline__ void load(raw4<T> (&to)[L], const StepsArgs &s, uint32_t t) const
+    // Where the part's blocks without an exception end: every thread has L places and 4 channels there.
+    __device__ __forceinline__ uint32_t full_end(const Job &job) const
+    {
+        const uint32_t upto = min(job.end, end);
+        return whole && upto > job.begin ? job.begin + (upto - job.begin) / kSteps * kSteps : job.begin;
+    }
+    // Address of place i of the thread's run in a block.  FULL: an address that the wave shares, and a 32-bit offset.
+    template <bool FULL> __device__ __forceinline__ T *at(const Steps &s, uint32_t block, int i) const
+    {
+        if constexpr (FULL) {
+            const uintptr_t shared = reinterpret_cast<uintptr_t>(s.base) + uint64_t(int64_t(block + wave * 4u * L + i) * s.row);
+            return reinterpret_cast<T *>(shared + s.offset);
+        } else {
+            const uint32_t t = min(block + run + i, length - 1u);
+            return reinterpret_cast<T *>(reinterpret_cast<uintptr_t>(s.base) + uint64_t(int64_t(t) * s.row) + ch.first * sizeof(T));
+        }
+    }
+    // The thread's places; where there is none anything.
+    template <bool FULL> __device__ __forceinline__ void load(raw4<T> (&to)[L], const Steps &s, uint32_t block) const
     {
 #pragma unroll
-        for (int i = 0; i < L; ++i) to[i] = t + i < end && ch.live ? ch.load(row<const T>(s, t + i)) : raw4<T>{};
+        for (int i = 0; i < L; ++i) {
+            if constexpr (FULL) to[i] = *reinterpret_cast<const typename Raw4<T>::at *>(at<FULL>(s, block, i));
+            else to[i] = ch.load(static_cast<const T *>(at<FULL>(s, block, i)));
+        }
     }
-    // m and 1 - a of place t
-    template <bool RESETS> __device__ __forceinline__ void gates(const RecurrenceArgs &a, raw4<T> forget, uint32_t t, f32x4 &m, f32x4 &rest, f32x4 &on) const
+    template <bool FULL> __device__ __forceinline__ void load_resets(uint8_t (&to)[L], const RecurrenceArgs &a, uint32_t block) const
+    {
+        const uint8_t *row = a.resets + int64_t(b) * a.resets_stride;
+#pragma unroll
+        for (int i = 0; i < L; ++i) to[i] = row[FULL ? block + run + i : min(block + run + i, length - 1u)];
+    }
+    template <bool FULL> __device__ __forceinline__ bool inside(uint32_t block, int i) const { return FULL || block + run + i < end; }
+    // A value that counts only inside the sequence, whatever it is.
+    template <bool FULL> __device__ __forceinline__ f32x4 value(raw4<T> raw, uint32_t block, int i) const { return inside<FULL>(block, i) ? widen4<T>(raw) : f32x4(0.f); }
+    // m and 1 - a of a place
+    template <bool FULL, bool RESETS> __device__ __forceinline__ void gates(raw4<T> forget, uint8_t reset, uint32_t block, int i, f32x4 &m, f32x4 &rest, f32x4 &on) const
     {
         const f32x4 f = widen4<T>(forget) + bias;
-        const bool inside = t < end;
-        const bool reset = RESETS && inside && a.resets[int64_t(b) * a.resets_stride + t] != 0;
+        const bool in = inside<FULL>(block, i);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const Gate g = state_gate_of(f[k]);
+            const Gate g = gate_of<T>(f[k]);
             on[k] = g.on;
-            m[k] = !inside ? 1.f : reset ? 0.f : g.on;
-            rest[k] = inside ? g.off : 0.f;
+            m[k] = !in ? 1.f : RESETS && reset ? 0.f : g.on;
+            rest[k] = in ? g.off : 0.f;
         }
+    }
+    template <bool FULL> __device__ __forceinline__ void store(const Steps &s, uint32_t block, int i, f32x4 x) const
+    {
+        if constexpr (FULL) __builtin_nontemporal_store(__builtin_convertvector(x, raw4<T>), reinterpret_cast<typename Raw4<T>::at *>(at<FULL>(s, block, i)));
+        else if (block + run + i < length) ch.store(at<FULL>(s, block, i), inside<FULL>(block, i) ? x : f32x4(0.f));
     }
     __device__ __forceinline__ uint64_t state(uint32_t channels, uint64_t i) const { return i * channels + ch.first; }
 };
 
-template <typename T, int WAVES, int L, bool RESETS> __global__ __launch_bounds__(WAVES * 64) void k_recurrence_forward(RecurrenceArgs a)
+// ---- sequences in several parts -----------------------------------------------------------------------------------
+// Few sequences of few channels are cut into parts.  One launch says what each part does to the state (BACK: to the gradient that comes from
+// behind), as one change; the next one's workgroups put the changes before their part together and walk along it.  Here nothing
+// but the end of a part is wanted, so each group of 16 threads goes along a run of its own, without a scan until the last place.
+
+template <typename T, int WAVES, int L, bool RESETS, bool BACK, bool GATE> __global__ __launch_bounds__(WAVES * 64) void k_recurrence_changes(RecurrenceArgs a)
+{
+    __shared__ Change room[WAVES][16];
+    const Job job(a);
+    if (job.segment == (BACK ? 0u : a.segments - 1u)) return;   // nobody comes behind
+    const Place<T, WAVES, L> p(a, job);
+    const uint32_t each = (job.end - job.begin + WAVES * 4u - 1u) / (WAVES * 4u), group = threadIdx.x / 16u;
+    const uint32_t begin = min(job.begin + group * each, job.end), count = min(each, job.end - begin);
+    const Steps forget_of = p.steps(a.forget), other_of = p.steps(BACK ? a.y : a.x), out_of = p.steps(a.out);
+    const uint8_t *resets = RESETS ? a.resets + int64_t(p.b) * a.resets_stride : nullptr;
+    Change all = {1.f, 0.f};
+    for (uint32_t n = 0; n < count; n += L) {
+        raw4<T> forget[L], other[L], out[L];
+        uint8_t reset[L];
+        // place i, or the nearest one that is there
+        auto place = [&](int i) { const uint32_t k = min(n + i, count - 1u); return BACK ? begin + count - 1u - k : begin + k; };
+        auto inside = [&](int i) { return n + i < count && place(i) < p.end; };
+        auto load = [&](raw4<T> (&to)[L], const Steps &s) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < L; ++i) to[i] = p.ch.load(reinterpret_cast<const T *>(s.base + int64_t(place(i)) * s.row + p.ch.first * sizeof(T)));
+        };
+        load(forget, forget_of);
+        load(other, other_of);
+        if constexpr (BACK && GATE) load(out, out_of);
+        if constexpr (RESETS)
+#pragma unroll
+            for (int i = 0; i < L; ++i) reset[i] = resets[place(i)];
+#pragma unroll
+        for (int i = 0; i < L; ++i) {
+            const bool in = inside(i);
+            const f32x4 f = widen4<T>(forget[i]) + p.bias;
+            f32x4 v = widen4<T>(other[i]);
+            if constexpr (BACK && GATE) {
+                const f32x4 o = widen4<T>(out[i]);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v[k] *= sigmoid_of<T>(o[k]);
+            }
+            Change c;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const Gate g = gate_of<T>(f[k]);
+                c.m[k] = !in ? 1.f : RESETS && reset[i] ? 0.f : g.on;
+                c.v[k] = !in ? 0.f : BACK ? v[k] : g.off * v[k];
+            }
+            if constexpr (BACK) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) all.v[k] = through<RESETS>(c.m[k], c.v[k] + all.v[k]);
+                all.m *= c.m;
+            } else {
+                all = then<RESETS>(all, c);
+            }
+        }
+    }
+    // the change of the whole part: what the groups do one after the other
+    Change of_wave;
+    before_groups<RESETS, BACK>(all, of_wave);
+    const uint32_t lane = threadIdx.x % 64u;
+    if (lane < 16u) room[threadIdx.x / 64u][lane] = of_wave;
+    __syncthreads();
+    if (threadIdx.x >= 16u) return;
+    Change total = {1.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) total = then<RESETS>(total, room[BACK ? WAVES - 1 - i : i][lane]);
+    float *to = a.changes + (uint64_t(job.sequence) * a.segments + job.segment) * 2u * a.channels + p.ch.first;
+    p.ch.store(to, total.m);
+    p.ch.store(to + a.channels, total.v);
+}
+
+// The state that a part begins with (BACK: the gradient from behind it), from that of the sequence: groups of 16 threads put runs of the
+// changes before it together.
+template <int WAVES, bool RESETS, bool BACK, typename P>
+__device__ __forceinline__ f32x4 begin_of_part(const RecurrenceArgs &a, const P &p, const Job &job, Change (&room)[WAVES][16])
+{
+    f32x4 carry = 0.f;
+    if (a.first) carry = p.ch.load(a.first + p.state(a.channels, p.b));
+    if (a.segments == 1u) return carry;
+    const uint32_t before = BACK ? a.segments - 1u - job.segment : job.segment, each = (before + WAVES * 4u - 1u) / (WAVES * 4u), group = threadIdx.x / 16u;
+    const uint32_t order = BACK ? WAVES * 4u - 1u - group : group;
+    Change all = {1.f, 0.f};
+    for (uint32_t i = order * each; i < min((order + 1u) * each, before); ++i) {
+        const uint32_t segment = BACK ? a.segments - 1u - i : i;
+        const float *from = a.changes + (uint64_t(job.sequence) * a.segments + segment) * 2u * a.channels + p.ch.first;
+        all = then<RESETS>(all, {p.ch.load(from), p.ch.load(from + a.channels)});
+    }
+    begin_of<WAVES, RESETS, BACK>(all, carry, room);
+    return carry;
+}
+
+// ---- the walk along a sequence or a part of it --------------------------------------------------------------------
+// Blocks without an exception have a loop of their own, in which the next block's values are on their way while a block is worked on: no branch
+// stands between its loads and stores, or the wait for the loads would be one for the stores behind them too.
+
+template <typename T, int WAVES, int L, bool RESETS, bool GATE> __global__ __launch_bounds__(WAVES * 64, 2) void k_recurrence_forward(RecurrenceArgs a)
 {
     using P = Place<T, WAVES, L>;
-    __shared__ Change room[2][WAVES][16];
-    const P p(a, blockIdx.x % a.slabs, a.first_sequence + blockIdx.x / a.slabs);
-    f32x4 carry = 0.f;
-    if (a.first && p.ch.live) carry = p.ch.load(a.first + p.state(a.channels, p.b));
+    __shared__ Change room[3][WAVES][16];
+    const Job job(a);
+    const P p(a, job);
+    const Steps x_of = p.steps(a.x), forget_of = p.steps(a.forget), out_of = p.steps(a.out), y_of = p.steps(a.y);
+    raw4<T> x[L], forget[L], out[L] = {};
+    uint8_t reset[L] = {};
+    auto fetch = [&](uint32_t block, auto full) __attribute__((always_inline)) {
+        constexpr bool FULL = decltype(full)::value;
+        p.template load<FULL>(x, x_of, block);
+        p.template load<FULL>(forget, forget_of, block);
+        if constexpr (GATE) p.template load<FULL>(out, out_of, block);
+        if constexpr (RESETS) p.template load_resets<FULL>(reset, a, block);
+    };
+    const uint32_t full_end = p.full_end(job);   // blocks before it are full
+    if (job.begin < full_end) fetch(job.begin, std::true_type());
+    f32x4 carry = begin_of_part<WAVES, RESETS, false>(a, p, job, room[2]);
     uint32_t turn = 0;
-    for (uint32_t block = 0; block < a.length; block += P::kSteps) {
-        const uint32_t t0 = block + p.run;
-        raw4<T> x[L], forget[L], out[L];
-        p.load(x, a.x, t0);
-        p.load(forget, a.forget, t0);
-        if (a.out.data) p.load(out, a.out, t0);
+    auto work = [&](uint32_t block, auto full) __attribute__((always_inline)) {
+        constexpr bool FULL = decltype(full)::value;
+        raw4<T> out_now[L];
         Change step[L], all = {1.f, 0.f};
+        if constexpr (!FULL) fetch(block, full);
 #pragma unroll
         for (int i = 0; i < L; ++i) {
             f32x4 rest, on;
-            p.template gates<RESETS>(a, forget[i], t0 + i, step[i].m, rest, on);
-            step[i].v = rest * widen4<T>(x[i]);
-            all.v = applied<RESETS>(step[i], all.v);
-            all.m *= step[i].m;
+            p.template gates<FULL, RESETS>(forget[i], reset[i], block, i, step[i].m, rest, on);
+            step[i].v = rest * p.template value<FULL>(x[i], block, i);
+            all = then<RESETS>(all, step[i]);
+            out_now[i] = out[i];
         }
+        if constexpr (FULL) fetch(min(block + P::kSteps, full_end - P::kSteps), full);
         f32x4 h = begin_of<WAVES, RESETS, false>(all, carry, room[turn]);
         turn ^= 1u;
-        if (!p.ch.live) continue;
+        renew<T>(out_now);
+        const uint32_t t0 = block + p.run;
         if (a.states && t0 % ADACOMP_RECURRENCE_KEEP == 0u && t0 < a.length) p.ch.store(a.states + p.state(a.channels, uint64_t(p.b) * a.kept + t0 / ADACOMP_RECURRENCE_KEEP), h);
 #pragma unroll
         for (int i = 0; i < L; ++i) {
-            if (t0 + i >= a.length) break;
             h = applied<RESETS>(step[i], h);
             f32x4 y = h;
-            if (a.out.data) {
-                const f32x4 o = widen4<T>(out[i]);
+            if constexpr (GATE) {
+                const f32x4 o = widen4<T>(out_now[i]);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) y[k] *= gate_of<T>(o[k]).on;
+                for (int k = 0; k < 4; ++k) y[k] *= sigmoid_of<T>(o[k]);
             }
-            if (t0 + i >= p.end) y = 0.f;
-            p.ch.store(p.template row<T>(a.y, t0 + i), y);
+            p.template store<FULL>(y_of, block, i, y);
         }
-    }
-    if (a.last && threadIdx.x < 16u && p.ch.live) p.ch.store(a.last + p.state(a.channels, p.b), carry);
+    };
+    for (uint32_t block = job.begin; block < full_end; block += P::kSteps) work(block, std::true_type());
+    for (uint32_t block = full_end; block < job.end; block += P::kSteps) work(block, std::false_type());
+    if (a.last && job.segment + 1u == a.segments && threadIdx.x < 16u) p.ch.store(a.last + p.state(a.channels, p.b), carry);
 }
 
-template <typename T, int WAVES, int L, bool RESETS> __global__ __launch_bounds__(WAVES * 64) void k_recurrence_backward(RecurrenceArgs a)
+template <typename T, int WAVES, int L, bool RESETS, bool GATE> __global__ __launch_bounds__(WAVES * 64, 2) void k_recurrence_backward(RecurrenceArgs a)
 {
     using P = Place<T, WAVES, L>;
-    static_assert(P::kSteps % ADACOMP_RECURRENCE_KEEP == 0, "a block begins with a state that was kept");
-    __shared__ Change room[2][2][WAVES][16];
+    static_assert(ADACOMP_RECURRENCE_KEEP % P::kSteps == 0 || P::kSteps % ADACOMP_RECURRENCE_KEEP == 0, "a block begins with a state that was kept, or is the only one");
+    __shared__ Change room[5][WAVES][16];
     __shared__ f32x4 sums[WAVES * 4][16];
-    const P p(a, blockIdx.x % a.slabs, a.first_sequence + blockIdx.x / a.slabs);
-    f32x4 carry = 0.f, dbias = 0.f;
-    if (a.first && p.ch.live) carry = p.ch.load(a.first + p.state(a.channels, p.b));
+    const Job job(a);
+    const P p(a, job);
+    const Steps x_of = p.steps(a.x), forget_of = p.steps(a.forget), out_of = p.steps(a.out), dy_of = p.steps(a.y), dx_of = p.steps(a.dx), df_of = p.steps(a.dforget),
+                dout_of = p.steps(a.dout);
+    raw4<T> next_x[L], next_forget[L], next_out[L] = {}, next_dy[L];
+    uint8_t next_reset[L] = {};
+    f32x4 next_state;
+    auto fetch = [&](uint32_t block, auto full) __attribute__((always_inline)) {
+        constexpr bool FULL = decltype(full)::value;
+        p.template load<FULL>(next_x, x_of, block);
+        p.template load<FULL>(next_forget, forget_of, block);
+        p.template load<FULL>(next_dy, dy_of, block);
+        if constexpr (GATE) p.template load<FULL>(next_out, out_of, block);
+        if constexpr (RESETS) p.template load_resets<FULL>(next_reset, a, block);
+        next_state = p.ch.load(a.states + p.state(a.channels, uint64_t(p.b) * a.kept + block / ADACOMP_RECURRENCE_KEEP));
+    };
+    const uint32_t full_end = p.full_end(job);
+    f32x4 carry = begin_of_part<WAVES, RESETS, true>(a, p, job, room[4]), dbias = 0.f;
     uint32_t turn = 0;
-    for (uint32_t blocks = a.length / P::kSteps + (a.length % P::kSteps != 0u); blocks-- > 0u;) {
-        const uint32_t block = blocks * P::kSteps, t0 = block + p.run;
-        raw4<T> x[L], forget[L], out[L], dy[L];
-        p.load(x, a.x, t0);
-        p.load(forget, a.forget, t0);
-        p.load(dy, a.y, t0);
-        if (a.out.data) p.load(out, a.out, t0);
-        f32x4 state = 0.f;
-        if (p.ch.live) state = p.ch.load(a.states + p.state(a.channels, uint64_t(p.b) * a.kept + block / ADACOMP_RECURRENCE_KEEP));
-        f32x4 m[L], rest[L], on[L];
+    auto work = [&](uint32_t block, auto full) __attribute__((always_inline)) {
+        constexpr bool FULL = decltype(full)::value;
+        if constexpr (!FULL) fetch(block, full);
+        raw4<T> x[L], out[L], dy[L];
+        f32x4 m[L], rest[L], on[L], state = next_state;
         Change all = {1.f, 0.f}, back = {1.f, 0.f};
 #pragma unroll
         for (int i = 0; i < L; ++i) {
-            p.template gates<RESETS>(a, forget[i], t0 + i, m[i], rest[i], on[i]);
-            all.v = applied<RESETS>({m[i], rest[i] * widen4<T>(x[i])}, all.v);
-            all.m *= m[i];
+            x[i] = next_x[i];
+            out[i] = next_out[i];
+            dy[i] = next_dy[i];
+            p.template gates<FULL, RESETS>(next_forget[i], next_reset[i], block, i, m[i], rest[i], on[i]);
+            all = then<RESETS>(all, {m[i], rest[i] * p.template value<FULL>(x[i], block, i)});
         }
-        f32x4 d[L];
+        if constexpr (FULL) fetch(max(block, job.begin + P::kSteps) - P::kSteps, full);
 #pragma unroll
         for (int i = L - 1; i >= 0; --i) {
-            d[i] = widen4<T>(dy[i]);
-            if (a.out.data) {
-                const f32x4 o = widen4<T>(out[i]);
+            f32x4 d = p.template value<FULL>(dy[i], block, i);
+            if constexpr (GATE) {
+                const f32x4 o = p.template value<FULL>(out[i], block, i);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) d[i][k] *= gate_of<T>(o[k]).on;
+                for (int k = 0; k < 4; ++k) d[k] *= sigmoid_of<T>(o[k]);
             }
 #pragma unroll
-            for (int k = 0; k < 4; ++k) back.v[k] = through<RESETS>(m[i][k], d[i][k] + back.v[k]);
+            for (int k = 0; k < 4; ++k) back.v[k] = through<RESETS>(m[i][k], d[k] + back.v[k]);
         }
         back.m = all.m;
-        const f32x4 h0 = begin_of<WAVES, RESETS, false>(all, state, room[turn][0]);
-        f32x4 c = begin_of<WAVES, RESETS, true>(back, carry, room[turn][1]);
-        turn ^= 1u;
         f32x4 h[L];   // before each place
-        h[0] = h0;
+        h[0] = begin_of<WAVES, RESETS, false>(all, state, room[turn * 2u]);
+        f32x4 c = begin_of<WAVES, RESETS, true>(back, carry, room[turn * 2u + 1u]);
+        turn ^= 1u;
+        renew<T>(x);
+        renew<T>(out);
+        renew<T>(dy);
 #pragma unroll
-        for (int i = 1; i < L; ++i) h[i] = applied<RESETS>({m[i - 1], rest[i - 1] * widen4<T>(x[i - 1])}, h[i - 1]);
-        if (p.ch.live) {
+        for (int i = 1; i < L; ++i) h[i] = applied<RESETS>({m[i - 1], rest[i - 1] * p.template value<FULL>(x[i - 1], block, i - 1)}, h[i - 1]);
 #pragma unroll
-            for (int i = L - 1; i >= 0; --i) {
-                if (t0 + i >= a.length) continue;
-                const f32x4 g = d[i] + c, xi = widen4<T>(x[i]);
-                f32x4 came, df, dout = 0.f;
+        for (int i = L - 1; i >= 0; --i) {
+            const f32x4 xi = p.template value<FULL>(x[i], block, i), up = p.template value<FULL>(dy[i], block, i);
+            f32x4 g = up, came, df, dout;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) came[k] = RESETS && m[i][k] == 0.f ? 0.f : h[i][k];
+            if constexpr (GATE) {
+                const f32x4 o = p.template value<FULL>(out[i], block, i);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    came[k] = RESETS && m[i][k] == 0.f ? 0.f : h[i][k];
-                    c[k] = through<RESETS>(m[i][k], g[k]);
-                    df[k] = g[k] * (on[i][k] * rest[i][k]) * (came[k] - xi[k]);
+                    const Gate gate = gate_of<T>(o[k]);
+                    g[k] *= gate.on;
+                    dout[k] = up[k] * fmaf(m[i][k], came[k], rest[i][k] * xi[k]) * (gate.on * gate.off);
                 }
-                const bool inside = t0 + i < p.end;
-                if (a.out.data) {
-                    const f32x4 o = widen4<T>(out[i]), up = widen4<T>(dy[i]);
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const Gate gate = gate_of<T>(o[k]);
-                        dout[k] = up[k] * fmaf(m[i][k], came[k], rest[i][k] * xi[k]) * (gate.on * gate.off);
-                    }
-                    p.ch.store(p.template row<T>(a.dout, t0 + i), inside ? dout : f32x4(0.f));
-                }
-                if (!inside) df = 0.f;
-                dbias += df;
-                p.ch.store(p.template row<T>(a.dx, t0 + i), inside ? g * rest[i] : f32x4(0.f));
-                p.ch.store(p.template row<T>(a.dforget, t0 + i), df);
+                p.template store<FULL>(dout_of, block, i, dout);
             }
+            g += c;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                c[k] = through<RESETS>(m[i][k], g[k]);
+                df[k] = g[k] * ((RESETS ? on[i][k] : m[i][k]) * rest[i][k]) * (came[k] - xi[k]);   // behind the end `rest` is 0
+            }
+            if (!p.template inside<FULL>(block, i)) df = 0.f;
+            dbias += df;
+            p.template store<FULL>(dx_of, block, i, g * rest[i]);
+            p.template store<FULL>(df_of, block, i, df);
         }
+    };
+    for (uint32_t n = (job.end - full_end + P::kSteps - 1u) / P::kSteps; n-- > 0u;) work(full_end + n * P::kSteps, std::false_type());
+    if (full_end > job.begin) {
+        fetch(full_end - P::kSteps, std::true_type());
+        for (uint32_t n = (full_end - job.begin) / P::kSteps; n-- > 0u;) work(job.begin + n * P::kSteps, std::true_type());
     }
-    if (a.last && threadIdx.x < 16u && p.ch.live) p.ch.store(a.last + p.state(a.channels, p.b), carry);
+    if (a.last && job.segment == 0u && threadIdx.x < 16u) p.ch.store(a.last + p.state(a.channels, p.b), carry);
     if (!a.dbias_parts) return;
     sums[threadIdx.x / 16u][threadIdx.x % 16u] = dbias;
     __syncthreads();
-    if (threadIdx.x >= 16u || !p.ch.live) return;
+    if (threadIdx.x >= 16u) return;
     f32x4 s = 0.f;
     for (uint32_t g = 0; g < WAVES * 4u; ++g) s += sums[g][threadIdx.x];
-    p.ch.store(a.dbias_parts + p.state(a.channels, p.b), s);
+    p.ch.store(a.dbias_parts + p.state(a.channels, uint64_t(p.b) * a.segments + job.segment), s);
+}
+
+// Sequences of few places, single tokens above all, and calls of so many sequences and channels that every one can have a thread: it takes 4
+// channels of a sequence from the first place to the last.
+template <typename T, int L, bool RESETS, bool GATE> __global__ __launch_bounds__(256) void k_recurrence_few(RecurrenceArgs a)
+{
+    const uint32_t groups = (a.channels + 3u) / 4u, i = blockIdx.x * 256u + threadIdx.x;
+    const uint32_t b = a.first_sequence + i / groups;
+    if (b >= a.batch) return;
+    const Channels ch(i % groups * 4u, a.channels);
+    const uint64_t state = uint64_t(b) * a.channels + ch.first;
+    auto address = [&](const StepsArgs &s, uint32_t t) __attribute__((always_inline)) {
+        return static_cast<T *>(const_cast<void *>(s.data)) + int64_t(b) * s.batch + int64_t(t) * s.row + ch.first;
+    };
+    f32x4 bias = 0.f, h = 0.f;
+    if (a.bias) bias = ch.load(a.bias + ch.first);
+    if (a.first) h = ch.load(a.first + state);
+    uint32_t end = a.length;
+    if (a.lengths) end = uint32_t(min(max(a.lengths[b], 0), int32_t(a.length)));
+    for (uint32_t t = 0; t < a.length; t += L) {
+        raw4<T> x[L], forget[L], out[L];
+        uint8_t reset[L] = {};
+#pragma unroll
+        for (int k = 0; k < L; ++k) {
+            const uint32_t at = min(t + k, a.length - 1u);
+            x[k] = ch.load(address(a.x, at));
+            forget[k] = ch.load(address(a.forget, at));
+            if constexpr (GATE) out[k] = ch.load(address(a.out, at));
+            if constexpr (RESETS) reset[k] = a.resets[int64_t(b) * a.resets_stride + at];
+        }
+#pragma unroll
+        for (int k = 0; k < L; ++k) {
+            if (t + k >= a.length) break;
+            if (a.states && (t + k) % ADACOMP_RECURRENCE_KEEP == 0u) ch.store(a.states + (uint64_t(b) * a.kept + (t + k) / ADACOMP_RECURRENCE_KEEP) * a.channels + ch.first, h);
+            const f32x4 f = widen4<T>(forget[k]) + bias, xk = widen4<T>(x[k]);
+            f32x4 y = 0.f;
+            if (t + k < end) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const Gate g = gate_of<T>(f[c]);
+                    h[c] = fmaf(g.off, xk[c], RESETS && reset[k] ? 0.f : g.on * h[c]);
+                    y[c] = h[c];
+                    if constexpr (GATE) y[c] *= sigmoid_of<T>(float(out[k][c]));
+                }
+            }
+            ch.store(address(a.y, t + k), y);
+        }
+    }
+    if (a.last) ch.store(a.last + state, h);
 }
 
 // dbias[c] = sum over the parts, in their order.  32 channels to a workgroup, 32 slices of the parts.
@@ -317,42 +583,80 @@ __global__ __launch_bounds__(1024) void k_bias_sum(BiasSumArgs a)
 
 // ---- launches -----------------------------------------------------------------------------------------------------
 
-constexpr int kWaves = 4, kRun = 4;
+constexpr int kWaves = 4;
+template <typename T> constexpr int kForwardRun = sizeof(T) == 2 ? 8 : 4;
+constexpr int kBackwardRun = 4;
+
+// Whether a call goes place by place: one place after the other takes 0.6 us, a workgroup's block of them 14 ns and a call of few of those 9 us
+// (512 x 16 x 4096 bf16 48 / 453 us, 512 x 64 x 4096 229 / 479, 256 x 64 x 1024 40 / 56, 32 x 32 x 4096 22 / 29, 32 x 48 x 4096 31 / 30, 4 x 8 x 512 9 / 9,
+// 4 x 16 x 512 10.8 / 9.0).
+static bool place_by_place(const RecurrenceArgs &a) { return a.length <= std::max<uint64_t>(12u, uint64_t(a.batch) * a.slabs / 48u); }
 
 // Calls f with the arguments and the grid of every launch: a grid is counted in threads, in 32 bits.
 template <typename F> static int for_sequences(const RecurrenceArgs &args, F &&f)
 {
     RecurrenceArgs a = args;
-    const uint32_t step = (1u << 23) / a.slabs;
+    const uint32_t of_one = a.slabs * a.segments, step = (1u << 23) / of_one;
     for (uint64_t first = 0; first < args.batch; first += step) {
         a.first_sequence = uint32_t(first);
-        if (int rc = f(a, dim3(uint32_t(std::min<uint64_t>(step, args.batch - first)) * a.slabs))) return rc;
+        if (int rc = f(a, dim3(uint32_t(std::min<uint64_t>(step, args.batch - first)) * of_one))) return rc;
     }
     return ADACOMP_OK;
 }
 
+template <typename F> static int with_form(const RecurrenceArgs &a, uint32_t dtype, F &&f)
+{
+    return with_type(dtype, [&](auto of) {
+        const auto gate = [&](auto resets) {
+            if (a.out.data) f(of, resets, std::true_type());
+            else f(of, resets, std::false_type());
+        };
+        if (a.resets) gate(std::true_type());
+        else gate(std::false_type());
+    });
+}
+
 int launch_recurrence_forward(const RecurrenceArgs &args, uint32_t dtype, void *stream)
 {
-    const dim3 wg(kWaves * 64);
     hipStream_t s = static_cast<hipStream_t>(stream);
+    if (place_by_place(args)) {
+        RecurrenceArgs a = args;
+        const uint32_t groups = (a.channels + 3u) / 4u, step = (1u << 30) / groups;   // threads of a launch are counted in 32 bits
+        for (uint64_t first = 0; first < args.batch; first += step) {
+            a.first_sequence = uint32_t(first);
+            a.batch = uint32_t(std::min<uint64_t>(args.batch, first + step));
+            const dim3 grid(((a.batch - a.first_sequence) * groups + 255u) / 256u);
+            const int rc = with_form(a, dtype, [&](auto of, auto resets, auto gate) {
+                using T = decltype(of);
+                constexpr bool RESETS = decltype(resets)::value, GATE = decltype(gate)::value;
+                if (a.length <= 2u) hipLaunchKernelGGL((k_recurrence_few<T, 1, RESETS, GATE>), grid, dim3(256), 0, s, a);
+                else hipLaunchKernelGGL((k_recurrence_few<T, 4, RESETS, GATE>), grid, dim3(256), 0, s, a);
+            });
+            if (rc) return rc;
+        }
+        return ADACOMP_OK;
+    }
     return for_sequences(args, [&](const RecurrenceArgs &a, dim3 grid) {
-        return with_type(dtype, [&](auto of) {
+        return with_form(a, dtype, [&](auto of, auto resets, auto gate) {
             using T = decltype(of);
-            if (a.resets) hipLaunchKernelGGL((k_recurrence_forward<T, kWaves, kRun, true>), grid, wg, 0, s, a);
-            else hipLaunchKernelGGL((k_recurrence_forward<T, kWaves, kRun, false>), grid, wg, 0, s, a);
+            constexpr bool RESETS = decltype(resets)::value, GATE = decltype(gate)::value;
+            if (a.segments > 1u) hipLaunchKernelGGL((k_recurrence_changes<T, 4, 8, RESETS, false, false>), grid, dim3(256), 0, s, a);
+            hipLaunchKernelGGL((k_recurrence_forward<T, kWaves, kForwardRun<T>, RESETS, GATE>), grid, dim3(kWaves * 64), 0, s, a);
         });
     });
 }
 
 int launch_recurrence_backward(const RecurrenceArgs &args, uint32_t dtype, void *stream)
 {
-    const dim3 wg(kWaves * 64);
     hipStream_t s = static_cast<hipStream_t>(stream);
     return for_sequences(args, [&](const RecurrenceArgs &a, dim3 grid) {
-        return with_type(dtype, [&](auto of) {
+        return with_form(a, dtype, [&](auto of, auto resets, auto gate) {
             using T = decltype(of);
-            if (a.resets) hipLaunchKernelGGL((k_recurrence_backward<T, kWaves, kRun, true>), grid, wg, 0, s, a);
-            else hipLaunchKernelGGL((k_recurrence_backward<T, kWaves, kRun, false>), grid, wg, 0, s, a);
+            constexpr bool RESETS = decltype(resets)::value, GATE = decltype(gate)::value;
+            if (a.segments > 1u) hipLaunchKernelGGL((k_recurrence_changes<T, 4, 8, RESETS, true, GATE>), grid, dim3(256), 0, s, a);
+            if (a.length <= 16u) hipLaunchKernelGGL((k_recurrence_backward<T, 1, kBackwardRun, RESETS, GATE>), grid, dim3(64), 0, s, a);
+            else if (a.length <= 32u) hipLaunchKernelGGL((k_recurrence_backward<T, 2, kBackwardRun, RESETS, GATE>), grid, dim3(128), 0, s, a);
+            else hipLaunchKernelGGL((k_recurrence_backward<T, kWaves, kBackwardRun, RESETS, GATE>), grid, dim3(kWaves * 64), 0, s, a);
         });
     });
 }

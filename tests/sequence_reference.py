@@ -64,7 +64,6 @@ class Recurrence:
         inside = torch.ones(b, n, 1, dtype=torch.bool) if lengths is None else torch.arange(n)[None, :, None] < lengths.clamp(0, n)[:, None, None]
         f = forget if bias is None else forget + bias
         f = torch.where(inside, f, zero)
-        f = torch.where(f < -80, zero - 80, f)
         self.inside, self.n = inside, n
         self.x = torch.where(inside, x, zero)
         self.first = torch.zeros(b, c, dtype=x.dtype) if first is None else first
@@ -77,7 +76,7 @@ class Recurrence:
         self.last = self.h[:, -1] if n else self.first
         self.before = torch.where(self.m == 0, zero, shifted(self.h, self.first)) if n else self.h
         self.o = None if out is None else torch.where(inside, out, zero)
-        self.o_on = torch.ones_like(x) if out is None else torch.sigmoid(torch.where(self.o < -80, zero - 80, self.o))
+        self.o_on = torch.ones_like(x) if out is None else torch.sigmoid(self.o)
         self.o_off = None if out is None else torch.sigmoid(-self.o)
         self.y = torch.where(inside, self.o_on * self.h, zero)
         # every place: a relative error of the gates (their argument is a sum and twice part of a product; exponential, sum, reciprocal, product) and a dozen
