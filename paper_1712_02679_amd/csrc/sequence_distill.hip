@@ -23,7 +23,8 @@ __device__ __forceinline__ float value_of(const void *p, uint64_t i, uint32_t dt
     return dtype == ADACOMP_DTYPE_BF16 ? float(static_cast<const bf16 *>(p)[i]) : float(static_cast<const f16 *>(p)[i]);
 }
 
-// What a team has in LDS: its row's top tokens, and behind them the target.
+// What a team has in LDS: its row's top tokens, and behind them the target and entries without a token, in fours.
+__host__ __device__ constexpr uint32_t entry_pitch(uint32_t top) { return (top + 4u) & ~3u; }
 struct Entries {
     uint32_t *token;
     float *t, *z;   // t / temperature, later p;  the student's logit
@@ -51,93 +52,127 @@ template <typename OP, int TPR> __device__ __forceinline__ void leave(float x, f
     }
 }
 
-// Exponentials of one row at a temperature: of z less the row's maximum, or of z / temperature - lse.
-template <typename T> struct Exponent {
+// Exponentials of one row at a temperature: of (z - its maximum) / temperature, or of z / temperature - lse.  In 16 bits the factor and the change
+// of units are one product; nothing but a difference is ever multiplied, so that logits at the ends of the type stay finite.
+template <typename T, bool FROM_LSE> struct Exponent {
     float off, c;
-    bool minus_after;   // off is in units of z / temperature
+    __device__ __forceinline__ Exponent(float o, float per) : off(o), c(!FROM_LSE && sizeof(T) == 2 ? per * kLog2e : per) {}
     __device__ __forceinline__ float of(float z) const
     {
-        if (minus_after) return exp_of<T>(z * c - off);
-        return exp_of<T>((z - off) * c);
+        const float x = FROM_LSE ? fmaf(z, c, -off) : (z - off) * c;
+        if constexpr (sizeof(T) == 4) return exp_of<T>(x);
+        return __builtin_amdgcn_exp2f(FROM_LSE ? x * kLog2e : x);
     }
 };
 
 __device__ __forceinline__ float finite_or_zero(float m) { return m == -kInf ? 0.f : m; }
 
+// Everything that the team's threads have stored, in LDS and in memory, is there for the others.  A wave's own accesses need no barrier, only their end.
+template <int TPR> __device__ __forceinline__ void sync_team()
+{
+    if constexpr (TPR > 64) __syncthreads();
+    else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+}
+// The same for LDS alone.
+template <int TPR> __device__ __forceinline__ void sync_lds()
+{
+    if constexpr (TPR > 64) __syncthreads();
+    else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+}
+
 // HELD: the row fits V groups of 8 to each thread; otherwise the team goes over it in parts, twice where it needs the maximum.
 template <typename T, int TPR, int V, bool HELD, int PASS> __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_distill(DistillArgs a)
 {
     constexpr uint32_t TEAMS = TPR > 256 ? 1 : 256 / TPR, PART = TPR * V * 8;
-    extern __shared__ float entries_room[];
+    extern __shared__ __attribute__((aligned(16))) float entries_room[];
     __shared__ float room[6][16];
-    const uint32_t t = threadIdx.x % TPR, team = team_of<TPR>(), parts = HELD ? 1u : (a.vocab + PART - 1u) / PART;
-    const Entries e(entries_room, team, a.top + 1u);
+    const uint32_t t = threadIdx.x % TPR, team = team_of<TPR>(), whole_parts = HELD ? 0u : a.vocab / PART;
+    const uint32_t pitch = entry_pitch(a.top);
+    const Entries e(entries_room, team, pitch);
     const bool two = a.top != 0u && a.targets && a.per_temperature != 1.f;   // exponentials at both temperatures
     const float c = a.top != 0u ? a.per_temperature : 1.f;
     for (uint64_t first = uint64_t(blockIdx.x) * TEAMS; first < a.rows; first += uint64_t(gridDim.x) * TEAMS) {
         const uint64_t row = first + team;
         const bool live = row < a.rows;
         const T *z = static_cast<const T *>(a.logits) + row * a.logits_stride;
-        auto groups_of = [&](uint32_t part) { return RowGroups<T, TPR, V>{t, a.vocab, part * PART}; };
+        const RowGroups<T, TPR, V> last = {t, a.vocab, whole_parts * PART};   // the part that the row ends in
         raw8<T> raw[V] = {};
-        if (live) groups_of(0).load(raw, z);
-        __syncthreads();   // the row before is done with the entries
+        if (HELD && live) last.load(raw, z);
+        // f(values) of every part: of whole ones, each with the next one on its way, and of the last one, where `behind` stands behind the row's end
+        auto parts = [&](float behind, auto &&f) __attribute__((always_inline)) {
+            if constexpr (!HELD) {
+                if (!live) return;
+                raw8<T> next[V];
+                auto fetch = [&](uint32_t part) __attribute__((always_inline)) {
+#pragma unroll
+                    for (int v = 0; v < V; ++v) next[v] = load8(at(z, part * PART + (t + uint32_t(v) * TPR) * 8u));
+                };
+                if (whole_parts) fetch(0);
+                for (uint32_t part = 0; part < whole_parts; ++part) {
+                    f32x8 x[V];
+#pragma unroll
+                    for (int v = 0; v < V; ++v) x[v] = widen<T>(next[v]);
+                    fetch(min(part + 1u, whole_parts - 1u));
+                    f(x, part * PART, std::true_type());
+                }
+                if (whole_parts * PART == a.vocab) return;
+                last.load(raw, z);
+            }
+            f32x8 x[V];
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                x[v] = last.values(raw[v], v);
+                if (!last.whole(v)) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) x[v][k] = last.col(v) + k < a.vocab ? x[v][k] : behind;
+                }
+            }
+            f(x, whole_parts * PART, std::false_type());
+        };
+        sync_lds<TPR>();   // the row before is done with the entries
         float top_max = -kInf;
         if (live)
-            for (uint32_t k = t; k <= a.top; k += TPR) {
+            for (uint32_t k = t; k < pitch; k += TPR) {
                 uint32_t token = kNoToken;
                 float tk = -kInf, zk = -kInf;
                 if (k < a.top) {
                     token = token_of(a.teacher_tokens, row * a.tokens_stride + k, a.tokens64, a.vocab);
                     if (token != kNoToken) tk = value_of(a.teacher_logits, row * a.teacher_stride + k, a.teacher_dtype) * a.per_temperature;
                     if (tk > top_max || tk != tk) top_max = tk;   // a NaN stays
-                } else if (a.targets) token = token_of(a.targets, row, a.targets64, a.vocab);
+                } else if (k == a.top && a.targets) token = token_of(a.targets, row, a.targets64, a.vocab);
                 if (token != kNoToken) zk = float(z[token]);
                 e.token[k] = token;
                 e.t[k] = tk;
                 e.z[k] = zk;
             }
-        // values of round v, -infinity behind the row's end
-        auto values = [&](const RowGroups<T, TPR, V> &groups, int v) {
-            f32x8 x = groups.values(raw[v], v);
-            if (!groups.whole(v)) {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) x[k] = groups.col(v) + k < a.vocab ? x[k] : -kInf;
-            }
-            return x;
-        };
         float most = -kInf, sum = 0.f, sum1 = 0.f;
         if constexpr (PASS != GRAD) {
-            for (uint32_t part = 0; part < parts; ++part) {
-                const RowGroups<T, TPR, V> groups = groups_of(part);
-                if (part != 0u && live) groups.load(raw, z);
+            parts(-kInf, [&](const f32x8 (&x)[V], uint32_t, auto) __attribute__((always_inline)) {
                 float here = -kInf;
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const f32x8 x = values(groups, v);
+                for (int v = 0; v < V; ++v)
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) here = fmaxf(here, x[k]);
-                }
+                    for (int k = 0; k < 8; ++k) here = fmaxf(here, x[v][k]);
                 if (here > most) {
                     sum *= most == -kInf ? 1.f : exp_of<T>((most - here) * c);
                     if (two) sum1 *= most == -kInf ? 1.f : exp_of<T>(most - here);
                     most = here;
                 }
-                const Exponent<T> ex = {finite_or_zero(most), c, false}, ex1 = {ex.off, 1.f, false};
+                const Exponent<T, false> ex(finite_or_zero(most), c), ex1(ex.off, 1.f);
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const f32x8 x = values(groups, v);
+                for (int v = 0; v < V; ++v)
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) sum += ex.of(x[k]);
-                    if (two)
+                    for (int k = 0; k < 8; ++k) sum += ex.of(x[v][k]);
+                if (two)
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) sum1 += ex1.of(x[k]);
-                }
-            }
+                    for (int v = 0; v < V; ++v)
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) sum1 += ex1.of(x[v][k]);
+            });
             leave<Max, TPR>(most, room[0]);
         }
         leave<Max, TPR>(top_max, room[1]);
-        __syncthreads();
+        sync_lds<TPR>();
         // fmaxf drops a NaN among the threads' maxima, but not in the sums, which then are NaN
         const float tmax = over_team<Max, TPR>(top_max, room[1], team), toff = finite_or_zero(tmax);
         float zmax = 0.f;
@@ -152,15 +187,15 @@ template <typename T, int TPR, int V, bool HELD, int PASS> __global__ __launch_b
         const float zoff = finite_or_zero(zmax);
         float s0 = 0.f, s1 = 0.f;
         if (live)
-            for (uint32_t k = t; k < a.top; k += TPR) {
-                const float tk = e.t[k], p = exp_of<float>(tk - toff);
+            for (uint32_t k = t; k < pitch; k += TPR) {
+                const float tk = e.t[k], p = exp_of<float>(tk - toff);   // 0 of -infinity
                 s0 += p;
                 if (PASS != GRAD && !(p == 0.f)) s1 += p * ((tk - toff) - (e.z[k] - zoff) * c);
                 e.t[k] = p;
             }
         leave<Add, TPR>(s0, room[4]);
         if (PASS != GRAD) leave<Add, TPR>(s1, room[5]);
-        __syncthreads();
+        sync_lds<TPR>();
         s0 = over_team<Add, TPR>(s0, room[4], team);
         const bool taught = !(s0 == 0.f), told = live && e.token[a.top] != kNoToken;
         float lse = 0.f, lse1 = 0.f, inv = 0.f, inv1 = 0.f;
@@ -188,16 +223,15 @@ template <typename T, int TPR, int V, bool HELD, int PASS> __global__ __launch_b
         const float g = !live ? 0.f : a.dloss ? a.scale * a.dloss[row] : a.scale;
         const float soft = taught && g != 0.f ? g * a.soft_grad : 0.f, hard = told && g != 0.f ? g * a.hard : 0.f;
         const bool none = g == 0.f || !(taught || told);
-        Exponent<T> ex, ex1;
+        float off, off1;
         if constexpr (PASS == GRAD) {   // a term that the row does not have: zeros
-            ex = {two ? taught ? finite_or_zero(lse) : kInf : finite_or_zero(taught ? lse : lse1), c, true};
-            ex1 = {told ? finite_or_zero(lse1) : kInf, 1.f, true};
+            off = two ? taught ? finite_or_zero(lse) : kInf : finite_or_zero(taught ? lse : lse1);
+            off1 = told ? finite_or_zero(lse1) : kInf;
             inv = inv1 = 1.f;
         } else {
-            const float off = zmax * c == kInf ? __builtin_nanf("") : finite_or_zero(zmax);
-            ex = {off, c, false};
-            ex1 = {off, 1.f, false};
+            off = off1 = zmax * c == kInf ? __builtin_nanf("") : finite_or_zero(zmax);
         }
+        const Exponent<T, PASS == GRAD> ex(off, c), ex1(off1, 1.f);
         const float by = (two ? soft : soft + hard) * inv, by1 = hard * inv1;
         auto gradient = [&](float x) {
             float q = by * ex.of(x);
@@ -206,25 +240,36 @@ template <typename T, int TPR, int V, bool HELD, int PASS> __global__ __launch_b
         };
         T *dz = static_cast<T *>(a.dlogits) + row * a.dlogits_stride;
         if (live)
-            for (uint32_t part = 0; part < parts; ++part) {
-                const RowGroups<T, TPR, V> groups = groups_of(part);
-                if (!HELD && (PASS != GRAD || part != 0u)) groups.load(raw, z);
-                groups.store(dz, [&](int v) {
-                    f32x8 x = groups.values(raw[v], v);
+            parts(0.f, [&](const f32x8 (&x)[V], uint32_t first_col, auto full) __attribute__((always_inline)) {
+                constexpr bool FULL = decltype(full)::value;
+                f32x8 y[V];
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) x[k] = none ? 0.f : gradient(x[k]);
-                    return x;
-                });
-            }
-        __syncthreads();
+                for (int v = 0; v < V; ++v)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) y[v][k] = none ? 0.f : gradient(x[v][k]);
+                if constexpr (FULL) {
+#pragma unroll
+                    for (int v = 0; v < V; ++v) RowGroups<T, TPR, V>::store_whole(at(dz, first_col + (t + uint32_t(v) * TPR) * 8u), y[v]);
+                } else {
+                    last.store(dz, [&](int v) { return y[v]; });
+                }
+            });
+        sync_team<TPR>();
         if (live && !none)
             for (uint32_t k = t; k <= a.top; k += TPR) {
                 const uint32_t token = e.token[k];
                 if (token == kNoToken) continue;
                 float p = 0.f;
                 if (taught)
-                    for (uint32_t j = 0; j < a.top; ++j)
-                        if (e.token[j] == token) p += e.t[j];
+#pragma unroll 2
+                    for (uint32_t j = 0; j < pitch; j += 4u) {
+                        const uint4 others = *reinterpret_cast<const uint4 *>(e.token + j);
+                        const float4 ps = *reinterpret_cast<const float4 *>(e.t + j);
+                        p += others.x == token ? ps.x : 0.f;
+                        p += others.y == token ? ps.y : 0.f;
+                        p += others.z == token ? ps.z : 0.f;
+                        p += others.w == token ? ps.w : 0.f;
+                    }
                 float x = gradient(e.z[k]);
                 if (taught) x -= soft * (p / s0);
                 if (token == e.token[a.top]) x -= hard;
@@ -235,15 +280,19 @@ template <typename T, int TPR, int V, bool HELD, int PASS> __global__ __launch_b
 
 // ---- launches -----------------------------------------------------------------------------------------------------
 
-// The entries of all teams are within 64 KB of LDS.
-template <typename F> static void with_distill(uint32_t vocab, uint32_t top, F &&f)
+// Threads to a row.  Short rows are held, with the entries of all teams within 64 KB of LDS; others are read in parts, twice for loss and gradient: held
+// in registers they leave so few waves that rows of 16384 take twice as long.  A wave to a row needs no barrier, but many rows; few long rows need all
+// threads that a workgroup can have.  64 / 256 / 1024 threads, loss and gradient of bf16 with 64 top tokens, us: 32768 x 2000 91 / 176 / 840, 16384 x 5000
+// 100 / 128 / 430, 8192 x 16384 166 / 141 / 249, 4096 x 65536 331 / 288 / 298, 1024 x 5000 18.7 / 18.5 / 34, 256 x 50000 65 / 27 / 23.
+template <typename F> static void with_distill(uint64_t rows, uint32_t vocab, uint32_t top, F &&f)
 {
-    if (vocab <= 256u && top < 128u) f(std::integral_constant<int, 8>(), std::integral_constant<int, 4>(), std::true_type());
-    else if (vocab <= 1024u) f(std::integral_constant<int, 32>(), std::integral_constant<int, 4>(), std::true_type());
-    else if (vocab <= 4096u) f(std::integral_constant<int, 128>(), std::integral_constant<int, 4>(), std::true_type());
-    else if (vocab <= 8192u) f(std::integral_constant<int, 256>(), std::integral_constant<int, 4>(), std::true_type());
-    else if (vocab <= 32768u) f(std::integral_constant<int, 1024>(), std::integral_constant<int, 4>(), std::true_type());
-    else f(std::integral_constant<int, 1024>(), std::integral_constant<int, 4>(), std::false_type());
+    using Two = std::integral_constant<int, 2>;
+    using Four = std::integral_constant<int, 4>;
+    if (vocab <= 256u && top < 160u) f(std::integral_constant<int, 8>(), Four(), std::true_type());
+    else if (vocab <= 1024u) f(std::integral_constant<int, 32>(), Four(), std::true_type());
+    else if (rows >= 4096u && vocab <= 8192u) f(std::integral_constant<int, 64>(), Two(), std::false_type());
+    else if (rows >= 512u || vocab <= 16384u) f(std::integral_constant<int, 256>(), Two(), std::false_type());
+    else f(std::integral_constant<int, 1024>(), Two(), std::false_type());
 }
 
 int launch_distill(const DistillArgs &a, uint32_t dtype, DistillPass pass, void *stream)
@@ -253,11 +302,11 @@ int launch_distill(const DistillArgs &a, uint32_t dtype, DistillPass pass, void 
         using T = decltype(of);
         auto go = [&](auto which) {
             constexpr int PASS = decltype(which)::value;
-            with_distill(a.vocab, a.top, [&](auto threads, auto groups, auto held) {
+            with_distill(a.rows, a.vocab, a.top, [&](auto threads, auto groups, auto held) {
                 constexpr uint32_t TPR = decltype(threads)::value, TEAMS = TPR > 256u ? 1u : 256u / TPR;
                 const uint64_t blocks = (a.rows + TEAMS - 1u) / TEAMS;
                 hipLaunchKernelGGL((k_distill<T, int(TPR), decltype(groups)::value, decltype(held)::value, PASS>), dim3(uint32_t(std::min<uint64_t>(blocks, 1u << 20))),
-                                   dim3(std::max(TPR, 256u)), TEAMS * (a.top + 1u) * 12u, s, a);
+                                   dim3(std::max(TPR, 256u)), TEAMS * entry_pitch(a.top) * 12u, s, a);
             });
         };
         if (pass == LOSS) go(std::integral_constant<int, LOSS>());

@@ -209,6 +209,12 @@ template <typename T, int WAVES, int L> struct Place {
         const uint32_t upto = min(job.end, end);
         return whole && upto > job.begin ? job.begin + (upto - job.begin) / kSteps * kSteps : job.begin;
     }
+    // Where the blocks with places inside the sequence end.
+    __device__ __forceinline__ uint32_t live_end(const Job &job) const
+    {
+        const uint32_t upto = min(job.end, end);
+        return upto > job.begin ? job.begin + (upto - job.begin + kSteps - 1u) / kSteps * kSteps : job.begin;
+    }
     // Address of place i of the thread's run in a block.  FULL: an address that the wave shares, and a 32-bit offset.
     template <bool FULL> __device__ __forceinline__ T *at(const Steps &s, uint32_t block, int i) const
     {
@@ -270,8 +276,9 @@ template <typename T, int WAVES, int L, bool RESETS, bool BACK, bool GATE> __glo
     const Job job(a);
     if (job.segment == (BACK ? 0u : a.segments - 1u)) return;   // nobody comes behind
     const Place<T, WAVES, L> p(a, job);
-    const uint32_t each = (job.end - job.begin + WAVES * 4u - 1u) / (WAVES * 4u), group = threadIdx.x / 16u;
-    const uint32_t begin = min(job.begin + group * each, job.end), count = min(each, job.end - begin);
+    const uint32_t last = max(min(job.end, p.end), job.begin);   // places behind the sequence's end change nothing
+    const uint32_t each = (last - job.begin + WAVES * 4u - 1u) / (WAVES * 4u), group = threadIdx.x / 16u;
+    const uint32_t begin = min(job.begin + group * each, last), count = min(each, last - begin);
     const Steps forget_of = p.steps(a.forget), other_of = p.steps(BACK ? a.y : a.x), out_of = p.steps(a.out);
     const uint8_t *resets = RESETS ? a.resets + int64_t(p.b) * a.resets_stride : nullptr;
     Change all = {1.f, 0.f};
@@ -280,7 +287,7 @@ template <typename T, int WAVES, int L, bool RESETS, bool BACK, bool GATE> __glo
         uint8_t reset[L];
         // place i, or the nearest one that is there
         auto place = [&](int i) { const uint32_t k = min(n + i, count - 1u); return BACK ? begin + count - 1u - k : begin + k; };
-        auto inside = [&](int i) { return n + i < count && place(i) < p.end; };
+        auto inside = [&](int i) { return n + i < count; };
         auto load = [&](raw4<T> (&to)[L], const Steps &s) __attribute__((always_inline)) {
 #pragma unroll
             for (int i = 0; i < L; ++i) to[i] = p.ch.load(reinterpret_cast<const T *>(s.base + int64_t(place(i)) * s.row + p.ch.first * sizeof(T)));
@@ -372,10 +379,13 @@ template <typename T, int WAVES, int L, bool RESETS, bool GATE> __global__ __lau
         if constexpr (GATE) p.template load<FULL>(out, out_of, block);
         if constexpr (RESETS) p.template load_resets<FULL>(reset, a, block);
     };
-    const uint32_t full_end = p.full_end(job);   // blocks before it are full
+    const uint32_t full_end = p.full_end(job), live_end = p.live_end(job);   // blocks before them are full, or have places inside the sequence
     if (job.begin < full_end) fetch(job.begin, std::true_type());
     f32x4 carry = begin_of_part<WAVES, RESETS, false>(a, p, job, room[2]);
     uint32_t turn = 0;
+    auto keep = [&](uint32_t t, f32x4 h) __attribute__((always_inline)) {
+        if (a.states && t % ADACOMP_RECURRENCE_KEEP == 0u && t < a.length) p.ch.store(a.states + p.state(a.channels, uint64_t(p.b) * a.kept + t / ADACOMP_RECURRENCE_KEEP), h);
+    };
     auto work = [&](uint32_t block, auto full) __attribute__((always_inline)) {
         constexpr bool FULL = decltype(full)::value;
         raw4<T> out_now[L];
@@ -394,7 +404,7 @@ template <typename T, int WAVES, int L, bool RESETS, bool GATE> __global__ __lau
         turn ^= 1u;
         renew<T>(out_now);
         const uint32_t t0 = block + p.run;
-        if (a.states && t0 % ADACOMP_RECURRENCE_KEEP == 0u && t0 < a.length) p.ch.store(a.states + p.state(a.channels, uint64_t(p.b) * a.kept + t0 / ADACOMP_RECURRENCE_KEEP), h);
+        keep(t0, h);
 #pragma unroll
         for (int i = 0; i < L; ++i) {
             h = applied<RESETS>(step[i], h);
@@ -408,7 +418,11 @@ template <typename T, int WAVES, int L, bool RESETS, bool GATE> __global__ __lau
         }
     };
     for (uint32_t block = job.begin; block < full_end; block += P::kSteps) work(block, std::true_type());
-    for (uint32_t block = full_end; block < job.end; block += P::kSteps) work(block, std::false_type());
+    for (uint32_t block = full_end; block < live_end; block += P::kSteps) work(block, std::false_type());
+    for (uint32_t block = live_end; block < job.end; block += P::kSteps) {
+        keep(block + p.run, carry);
+        for (int i = 0; i < L; ++i) p.template store<false>(y_of, block, i, f32x4(0.f));
+    }
     if (a.last && job.segment + 1u == a.segments && threadIdx.x < 16u) p.ch.store(a.last + p.state(a.channels, p.b), carry);
 }
 
@@ -434,7 +448,7 @@ template <typename T, int WAVES, int L, bool RESETS, bool GATE> __global__ __lau
         if constexpr (RESETS) p.template load_resets<FULL>(next_reset, a, block);
         next_state = p.ch.load(a.states + p.state(a.channels, uint64_t(p.b) * a.kept + block / ADACOMP_RECURRENCE_KEEP));
     };
-    const uint32_t full_end = p.full_end(job);
+    const uint32_t full_end = p.full_end(job), live_end = p.live_end(job);
     f32x4 carry = begin_of_part<WAVES, RESETS, true>(a, p, job, room[4]), dbias = 0.f;
     uint32_t turn = 0;
     auto work = [&](uint32_t block, auto full) __attribute__((always_inline)) {
@@ -501,7 +515,13 @@ template <typename T, int WAVES, int L, bool RESETS, bool GATE> __global__ __lau
             p.template store<FULL>(df_of, block, i, df);
         }
     };
-    for (uint32_t n = (job.end - full_end + P::kSteps - 1u) / P::kSteps; n-- > 0u;) work(full_end + n * P::kSteps, std::false_type());
+    for (uint32_t block = live_end; block < job.end; block += P::kSteps)
+        for (int i = 0; i < L; ++i) {
+            p.template store<false>(dx_of, block, i, f32x4(0.f));
+            p.template store<false>(df_of, block, i, f32x4(0.f));
+            if constexpr (GATE) p.template store<false>(dout_of, block, i, f32x4(0.f));
+        }
+    for (uint32_t n = (live_end - full_end) / P::kSteps; n-- > 0u;) work(full_end + n * P::kSteps, std::false_type());
     if (full_end > job.begin) {
         fetch(full_end - P::kSteps, std::true_type());
         for (uint32_t n = (full_end - job.begin) / P::kSteps; n-- > 0u;) work(job.begin + n * P::kSteps, std::true_type());
@@ -585,7 +605,9 @@ __global__ __launch_bounds__(1024) void k_bias_sum(BiasSumArgs a)
 
 constexpr int kWaves = 4;
 template <typename T> constexpr int kForwardRun = sizeof(T) == 2 ? 8 : 4;
-constexpr int kBackwardRun = 4;
+// The backward pass of 32-bit tensors with a gate has registers for half as many places (8 x 2048 x 2048 308 / 212 us, 47 to 123 registers in memory
+// otherwise; without a gate 152 / 156).
+template <typename T, bool GATE> constexpr int kBackwardRun = sizeof(T) == 4 && GATE ? 2 : 4;
 
 // Whether a call goes place by place: one place after the other takes 0.6 us, a workgroup's block of them 14 ns and a call of few of those 9 us
 // (512 x 16 x 4096 bf16 48 / 453 us, 512 x 64 x 4096 229 / 479, 256 x 64 x 1024 40 / 56, 32 x 32 x 4096 22 / 29, 32 x 48 x 4096 31 / 30, 4 x 8 x 512 9 / 9,
@@ -654,9 +676,10 @@ int launch_recurrence_backward(const RecurrenceArgs &args, uint32_t dtype, void 
             using T = decltype(of);
             constexpr bool RESETS = decltype(resets)::value, GATE = decltype(gate)::value;
             if (a.segments > 1u) hipLaunchKernelGGL((k_recurrence_changes<T, 4, 8, RESETS, true, GATE>), grid, dim3(256), 0, s, a);
-            if (a.length <= 16u) hipLaunchKernelGGL((k_recurrence_backward<T, 1, kBackwardRun, RESETS, GATE>), grid, dim3(64), 0, s, a);
-            else if (a.length <= 32u) hipLaunchKernelGGL((k_recurrence_backward<T, 2, kBackwardRun, RESETS, GATE>), grid, dim3(128), 0, s, a);
-            else hipLaunchKernelGGL((k_recurrence_backward<T, kWaves, kBackwardRun, RESETS, GATE>), grid, dim3(kWaves * 64), 0, s, a);
+            constexpr int L = kBackwardRun<T, GATE>, WAVES = 16 / L;   // blocks of 64 places, or 16 or 32 where the sequence has no more
+            if (a.length <= 16u) hipLaunchKernelGGL((k_recurrence_backward<T, WAVES / 4, L, RESETS, GATE>), grid, dim3(WAVES * 16), 0, s, a);
+            else if (a.length <= 32u) hipLaunchKernelGGL((k_recurrence_backward<T, WAVES / 2, L, RESETS, GATE>), grid, dim3(WAVES * 32), 0, s, a);
+            else hipLaunchKernelGGL((k_recurrence_backward<T, WAVES, L, RESETS, GATE>), grid, dim3(WAVES * 64), 0, s, a);
         });
     });
 }

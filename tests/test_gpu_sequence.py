@@ -203,11 +203,8 @@ def run_forward(A, s, dtype, pad=0, lead=0):
     return g
 
 
-def check_states(got, r, lengths):
+def check_states(got, r):
     want, off = r.states()
-    if lengths is not None:   # states behind a sequence's end are nobody's
-        there = torch.arange(0, r.n, S.KEEP)[None, :] < lengths.clamp(min=1)[:, None]
-        got, want, off = got.cpu()[there], want[there], off[there]
     within(got, want, off + 4 * U * want.abs(), "states")
 
 
@@ -217,7 +214,7 @@ def check_both(A, s, dtype, pad=0, lead=0, accumulate=False):
     g = run_forward(A, s, dtype, pad, lead)
     within(g["y"], r.y, r.y_bound(dtype), "y")
     within(g["last"], r.last, r.last_bound(), "last")
-    check_states(g["states"], r, s["lengths"])
+    check_states(g["states"], r)
     dy, dlast = rand((b, n, c), dtype, 77), rand((b, c), F32, 78)
     want = r.backward(dy.double(), dlast.double())
     fresh = lambda: on_gpu(torch.full((b, n, c), float("nan"), dtype=dtype), pad, lead)
@@ -482,6 +479,30 @@ def test_distill_terms(A, temperature, soft, hard, dtype):
 def test_distill_top_tokens(A, vocab, top):
     """As many top tokens as there can be, more than the vocabulary has, and one."""
     check_distill(A, distill_case(30, vocab, top, F32, 4), F32, 1.5, 0.8, 0.2)
+
+
+@pytest.mark.parametrize("rows,vocab", [(4096, 1025), (4100, 2047), (4097, 8191), (4096, 8193), (513, 9000), (511, 16385), (4099, 1024)])
+def test_distill_many_rows(A, rows, vocab):
+    """Rows enough for a wave each, and the sizes where that ends; the first and the last of them against the formula, all against one another."""
+    g = torch.Generator().manual_seed(12)
+    few = distill_case(24, vocab, 30, BF16, 13)
+    pick = torch.randint(0, 24, (rows,), generator=g)
+    pick[:24], pick[-24:] = torch.arange(24), torch.arange(24)
+    args = dict(temperature=1.5, soft=0.6, hard=0.4)
+    part = lambda i: dict(teacher_tokens=few["tokens"][i].to(DEV), teacher_logits=few["t"][i].to(DEV), targets=few["targets"][i].to(DEV))
+    loss, lse, grad = torch.empty(rows, device=DEV), torch.empty(rows, 2, device=DEV), torch.empty(rows, vocab, dtype=BF16, device=DEV)
+    z = few["z"].to(DEV)[pick.to(DEV)]
+    A.adacomp_distill_forward(z, loss, lse=lse, dlogits=grad, **part(pick), **args)
+    d = S.Distill(few["z"].double(), few["tokens"], few["t"].double(), few["targets"], *(float(np.float32(v)) for v in (1.5, 0.6, 0.4)))
+    want, off = d.gradient(torch.ones(24, dtype=torch.float64))
+    within(loss[:24], d.loss, d.loss_off, "loss")
+    within(grad[:24], want, rounded(want, off, BF16), "dlogits")
+    assert torch.equal(loss, loss[:24][pick.to(DEV)]) and torch.equal(lse, lse[:24][pick.to(DEV)]) and torch.equal(grad, grad[:24][pick.to(DEV)])
+    back = torch.empty_like(grad)
+    A.adacomp_distill_backward(z, lse, back, **part(pick), **args)
+    want, off = d.gradient(torch.ones(24, dtype=torch.float64), from_lse=True)
+    within(back[:24], want, rounded(want, off, BF16), "dlogits from lse")
+    assert torch.equal(back, back[:24][pick.to(DEV)])
 
 
 def test_distill_without_a_teacher_is_cross_entropy(A):
