@@ -626,3 +626,147 @@ def test_distill_refusals(A):
         A.adacomp_distill_forward(z, None, **ok)
     none = torch.zeros(0, 9, device=DEV)
     A.adacomp_distill_forward(none, loss[:0], dlogits=none, targets=targets[:0])
+
+
+# ---- graphs, streams, large calls -----------------------------------------------------------------------------------
+
+def everything(A, seed, rows=(4, 300), vocab=500, c=70, top=9):
+    """One call of each kind on buffers of its own: (a function that makes the calls, the results, the inputs that may change)."""
+    b, n = rows
+    g = lambda shape, k, dtype=BF16: rand(shape, dtype, seed + k).to(DEV)
+    tokens = tokens_of(b * n, vocab, seed).view(b, n).to(DEV)
+    table, x, forget, out, dy, z = g((vocab, c), 1, F32), g((b, n, c), 2), g((b, n, c), 3), g((b, n, c), 4), g((b, n, c), 5), g((b, n, vocab), 6)
+    k, t, targets = torch.randint(0, vocab, (b, n, top), device=DEV), g((b, n, top), 7), torch.randint(0, vocab, (b, n), device=DEV)
+    y, dtable, r, states, last = torch.empty_like(x), torch.empty_like(table), torch.empty_like(x), torch.empty(b, A.adacomp_recurrence_kept(n), c, device=DEV), torch.empty(b, c, device=DEV)
+    dx, df, do, dbias, bias = torch.empty_like(x), torch.empty_like(x), torch.empty_like(x), torch.empty(c, device=DEV), g((c,), 8, F32)
+    loss, lse, dz, dz2 = torch.empty(b, n, device=DEV), torch.empty(b, n, 2, device=DEV), torch.empty_like(z), torch.empty_like(z)
+    ws = room(max(A.adacomp_embed_workspace_bytes(b * n, vocab, c), A.adacomp_recurrence_workspace_bytes(b, n, c)))
+    terms = dict(teacher_tokens=k, teacher_logits=t, targets=targets, temperature=2.0, soft=0.5, hard=0.5)
+
+    def calls():
+        A.adacomp_embed_forward(tokens, table, y, dropout=A.Dropout(0.2, 9, 10))
+        A.adacomp_embed_backward(tokens, dy, dtable, ws, dropout=A.Dropout(0.2, 9, 10))
+        A.adacomp_recurrence_forward(x, forget, r, ws, out=out, bias=bias, states=states, last=last)
+        A.adacomp_recurrence_backward(dy, x, forget, states, dx, df, ws, out=out, dout=do, bias=bias, dbias=dbias)
+        A.adacomp_distill_forward(z, loss, lse=lse, dlogits=dz, **terms)
+        A.adacomp_distill_backward(z, lse, dz2, **terms)
+    return calls, [y, dtable, r, states, last, dx, df, do, dbias, loss, lse, dz, dz2], [x, forget, dy, z, table]
+
+
+def capture(calls):
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            calls()
+    return graph
+
+
+def test_captured_and_replayed(A):
+    """Two graphs with a workspace of their own each, replayed in turn with eager work between, on inputs that change."""
+    pairs = [everything(A, 20), everything(A, 40, rows=(1, 3000), vocab=5000, c=40)]
+    graphs = []
+    for calls, _, _ in pairs:
+        calls()
+        torch.cuda.synchronize()
+        graphs.append(capture(calls))
+    for turn in range(4):
+        for (calls, results, inputs), graph in zip(pairs, graphs):
+            for t in inputs:
+                t.mul_(0.9)
+            calls()
+            eager = [r.clone() for r in results]
+            for r in results:
+                r.fill_(7.0)
+            graph.replay()
+            torch.cuda.synchronize()
+            for i, (got, want) in enumerate(zip(results, eager)):
+                assert torch.equal(got, want), (turn, i)
+
+
+def test_on_other_streams_at_once(A):
+    """Calls of two streams at the same time, each with its workspace, give what they give alone."""
+    pairs = [everything(A, 60, rows=(3, 900)), everything(A, 80, rows=(2, 1500), vocab=3000)]
+    alone = []
+    for calls, results, _ in pairs:
+        calls()
+        alone.append([r.clone() for r in results])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for (calls, results, _), stream in zip(pairs, streams):
+        with torch.cuda.stream(stream):
+            for r in results:
+                r.fill_(7.0)
+            for _ in range(5):
+                calls()
+    torch.cuda.synchronize()
+    for (_, results, _), want in zip(pairs, alone):
+        for i, (got, w) in enumerate(zip(results, want)):
+            assert torch.equal(got, w), i
+
+
+def test_embed_rows_beyond_32_bits(A):
+    """A table and an output of more than 2^32 bytes, and more than 2^31 values: rows at their ends."""
+    vocab, cols = (1 << 19) + 3, 4100
+    table = torch.zeros(vocab, cols, device=DEV)
+    ends = [0, 1, vocab // 2, vocab - 2, vocab - 1]
+    rows = rand((len(ends), cols), F32, 1)
+    table[torch.tensor(ends, device=DEV)] = rows.to(DEV)
+    tokens = torch.tensor(ends, device=DEV).repeat(3)
+    y = torch.empty(len(tokens), cols, dtype=F32, device=DEV)
+    A.adacomp_embed_forward(tokens, table, y)
+    assert torch.equal(y.cpu(), rows.repeat(3, 1))
+    A.adacomp_embed_backward(tokens, y, table.fill_(5.0), embed_room(A, len(tokens), vocab, cols))
+    want = (rows + rows) + rows
+    assert torch.equal(table[torch.tensor(ends, device=DEV)].cpu(), want)
+    table[torch.tensor(ends, device=DEV)] = 0
+    assert not table.any()
+    del table
+    torch.cuda.empty_cache()
+    rows = (1 << 20) + 5
+    y = torch.full((rows, cols), 3.0, dtype=BF16, device=DEV)
+    small = rand((7, cols), F32, 2)
+    tokens = torch.arange(rows, device=DEV) % 8   # the eighth is none
+    A.adacomp_embed_forward(tokens, small.to(DEV), y)
+    for first in (0, (1 << 19) - 2, rows - 9):
+        want = S.embed_forward(tokens[first:first + 9].cpu(), small.double(), 1.0)
+        within(y[first:first + 9], want, rounded(want, 0.0 * want, BF16), first)
+    got = torch.empty(7, cols, device=DEV)
+    A.adacomp_embed_backward(tokens, y.fill_(0.5), got, embed_room(A, rows, 7, cols))
+    assert torch.equal(got.cpu(), (torch.bincount(tokens.cpu(), minlength=8)[:7].float() * 0.5)[:, None].expand(7, cols))
+    del y
+    torch.cuda.empty_cache()
+
+
+def test_recurrence_and_distill_beyond_32_bits(A):
+    """Tensors of more than 2^32 bytes: sequences far apart, rows at both ends."""
+    b, n, c, stride = 3, 70, 66, 1 << 30   # 2^31 bytes between bf16 sequences, which are 70 rows of 2^24 bytes long
+    s = recurrence_case(b, n, c, BF16, True, True, True, False, False, 14)
+    room_ = torch.zeros(2 * stride + n * (1 << 23) + 4096, dtype=BF16, device=DEV)
+    far = room_.as_strided((b, n, c), (stride, 1 << 23, 1))   # rows 2^24 bytes apart
+    far.copy_(s["x"])
+    near = run_forward(A, s, BF16)
+    y = torch.empty(b, n, c, dtype=BF16, device=DEV)
+    A.adacomp_recurrence_forward(far, near["forget"], y, near["ws"], out=near["out"], bias=near["bias"], first=near["first"])
+    assert torch.equal(y, near["y"])
+    A.adacomp_recurrence_forward(far, near["forget"], far, near["ws"], out=near["out"], bias=near["bias"], first=near["first"])
+    assert torch.equal(far, near["y"])
+    del room_, far
+    torch.cuda.empty_cache()
+    rows, vocab = 40000, 70001
+    z = torch.full((rows, vocab), 1.0, dtype=BF16, device=DEV)
+    few = distill_case(8, vocab, 12, BF16, 15)
+    at = torch.tensor([0, 1, 2, 3, rows - 4, rows - 3, rows - 2, rows - 1])
+    z[at.to(DEV)] = few["z"].to(DEV)
+    tokens, t, targets = torch.full((rows, 12), -1), torch.zeros(rows, 12), torch.full((rows,), -1)
+    tokens[at], t[at], targets[at] = few["tokens"], few["t"], few["targets"]
+    d = S.Distill(few["z"].double(), few["tokens"], few["t"].double(), few["targets"], 2.0, 0.5, 0.5)
+    loss = torch.empty(rows, device=DEV)
+    A.adacomp_distill_forward(z, loss, dlogits=z, teacher_tokens=tokens.to(DEV), teacher_logits=t.to(DEV), targets=targets.to(DEV), temperature=2.0, soft=0.5, hard=0.5)
+    want, off = d.gradient(torch.ones(8, dtype=torch.float64))
+    within(loss[at.to(DEV)], d.loss, d.loss_off, "loss")
+    within(z[at.to(DEV)], want, rounded(want, off, BF16), "dlogits")
+    assert not z[4:rows - 4].any() and not loss[4:rows - 4].any()
+    del z
+    torch.cuda.empty_cache()
