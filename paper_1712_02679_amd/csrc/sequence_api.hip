@@ -51,6 +51,21 @@ static int steps_args(const adacomp_steps_t *steps, const adacomp_recurrence_t *
 // Whether 64 rows lie within 32 bits of the first one.
 static bool near_rows(const StepsArgs &s) { return s.row >= 0 && s.row < int64_t(1) << 23; }
 
+// Whether a result shares no memory with what is read, as far as the tensors' first and last bytes say.
+static bool apart(const StepsArgs &out, const StepsArgs &in, const adacomp_recurrence_t *op)
+{
+    const auto ends = [op](const StepsArgs &s, int64_t &low, int64_t &high) {
+        const int64_t e = int64_t(element_bytes(op->dtype)), batch = (int64_t(op->batch) - 1) * s.batch, rows = (int64_t(op->length) - 1) * s.row;
+        low = int64_t(reinterpret_cast<uintptr_t>(s.data)) + (std::min<int64_t>(batch, 0) + std::min<int64_t>(rows, 0)) * e;
+        high = int64_t(reinterpret_cast<uintptr_t>(s.data)) + (std::max<int64_t>(batch, 0) + std::max<int64_t>(rows, 0) + op->channels) * e;
+    };
+    if (!out.data || !in.data) return true;
+    int64_t low, high, in_low, in_high;
+    ends(out, low, high);
+    ends(in, in_low, in_high);
+    return high <= in_low || in_high <= low;
+}
+
 static bool recurrence_sizes(uint64_t batch, uint64_t length, uint64_t channels)
 {
     return batch < kMost && length < kMost && channels <= kMostCols && batch * length < kMost;
@@ -199,6 +214,7 @@ int adacomp_recurrence_forward(const adacomp_recurrence_t *op, const adacomp_ste
     a.last = last;
     a.states = states;
     a.near_rows = near_rows(a.x) && near_rows(a.forget) && near_rows(a.out) && near_rows(a.y);
+    a.apart = apart(a.y, a.x, op) && apart(a.y, a.forget, op) && apart(a.y, a.out, op);
     a.changes = reinterpret_cast<float *>(static_cast<char *>(workspace) + recurrence_sums({a.segments, a.segment}, a.batch, a.channels));
     return launch_recurrence_forward(a, op->dtype, hip_stream);
 }
@@ -226,6 +242,9 @@ int adacomp_recurrence_backward(const adacomp_recurrence_t *op, const adacomp_st
         if (a.length != 0 && !states) return ADACOMP_EINVAL;
         if (int rc = workspace_check(workspace, workspace_bytes, adacomp_recurrence_workspace_bytes(op->batch, op->length, op->channels))) return rc;
         a.near_rows = near_rows(a.x) && near_rows(a.forget) && near_rows(a.out) && near_rows(a.y) && near_rows(a.dx) && near_rows(a.dforget) && near_rows(a.dout);
+        a.apart = true;
+        for (const StepsArgs *out : {&a.dx, &a.dforget, &a.dout})
+            for (const StepsArgs *in : {&a.x, &a.forget, &a.out, &a.y}) a.apart = a.apart && apart(*out, *in, op);
         a.first = dlast;
         a.last = dfirst;
         a.states = const_cast<float *>(states);

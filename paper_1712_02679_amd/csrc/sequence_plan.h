@@ -82,6 +82,7 @@ struct RecurrenceArgs {
     uint32_t segments, segment;                // parts of a sequence, places of a part
     uint32_t first_sequence;                   // of a launch
     uint32_t near_rows;                        // rows of all tensors are so near that a wave's lie within 32 bits
+    uint32_t apart;                            // results share no memory with what is read
 };
 
 constexpr uint32_t kSlab = 64;   // channels of a workgroup: a line of memory in 16 bits
@@ -92,7 +93,7 @@ constexpr uint32_t kSlab = 64;   // channels of a workgroup: a line of memory in
 struct RecurrenceForm { uint32_t segments, segment; };
 inline RecurrenceForm recurrence_form(uint32_t batch, uint32_t length, uint32_t channels)
 {
-    constexpr uint32_t kLeast = 256;   // places of a part, whole blocks of a workgroup
+    constexpr uint32_t kLeast = 128;   // places of a part, whole blocks of a workgroup (128 / 256: 1 x 1024 x 512 13.6 / 17.6 us, backward 20 / 30)
     const uint64_t workgroups = uint64_t(batch) * ((channels + kSlab - 1u) / kSlab);
     if (workgroups == 0 || workgroups >= kComputeUnits || length == 0) return {1u, std::max(length, 1u)};
     const uint64_t wanted = std::min<uint64_t>((2u * kComputeUnits + workgroups - 1u) / workgroups, (length + kLeast - 1u) / kLeast);

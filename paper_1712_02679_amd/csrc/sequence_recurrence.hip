@@ -17,7 +17,8 @@ template <typename T> using raw4 = typename Raw4<T>::vec;
 using f32x4 = raw4<float>;
 
 // The 4 channels that a thread has, of which the last thread of a row may share some with its neighbour: it reads the row's last 4
-// and writes those from `own` on.  Threads behind the row's end read its last 4 as well, and write none.
+// and writes those from `own` on.  Threads behind the row's end read its last 4 as well, and write none.  Where results share no memory with what is
+// read they may write all 4: what they have for their neighbours' channels is what those write.
 struct Channels {
     uint32_t first, own, count;   // count: channels read, 4 but in rows of fewer
     __device__ __forceinline__ Channels(uint32_t c, uint32_t channels)
@@ -187,11 +188,11 @@ template <typename T, int WAVES, int L> struct Place {
     static constexpr uint32_t kSteps = WAVES * 4u * L;   // places of a block
     Channels ch;
     uint32_t b, wave, run, length, end;   // run: first place inside a block; end: of the sequence
-    bool whole;                           // all of the workgroup's channels are there, and its rows near each other
+    bool whole;                           // every thread may read and write 4 channels, and rows are near each other
     f32x4 bias;
     __device__ __forceinline__ Place(const RecurrenceArgs &a, const Job &job)
         : ch(job.slab * kSlab + threadIdx.x % 16u * 4u, a.channels), b(job.sequence), wave(__builtin_amdgcn_readfirstlane(threadIdx.x / 64u)),
-          run(threadIdx.x / 16u * L), length(a.length), end(a.length), whole(a.near_rows && (job.slab + 1u) * kSlab <= a.channels)
+          run(threadIdx.x / 16u * L), length(a.length), end(a.length), whole(a.near_rows && ((job.slab + 1u) * kSlab <= a.channels || (a.apart && a.channels >= 4u)))
     {
         if (a.lengths) end = uint32_t(min(max(a.lengths[b], 0), int32_t(a.length)));
         bias = 0.f;
