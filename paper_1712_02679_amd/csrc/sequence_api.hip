@@ -66,6 +66,13 @@ static bool apart(const StepsArgs &out, const StepsArgs &in, const adacomp_recur
     return high <= in_low || in_high <= low;
 }
 
+// The same of two [batch, channels] states, either of which may be NULL.
+static bool states_apart(const float *one, const float *other, const adacomp_recurrence_t *op)
+{
+    const uint64_t bytes = uint64_t(op->batch) * op->channels * 4u, a = reinterpret_cast<uintptr_t>(one), b = reinterpret_cast<uintptr_t>(other);
+    return !one || !other || a + bytes <= b || b + bytes <= a;
+}
+
 static bool recurrence_sizes(uint64_t batch, uint64_t length, uint64_t channels)
 {
     return batch < kMost && length < kMost && channels <= kMostCols && batch * length < kMost;
@@ -214,7 +221,7 @@ int adacomp_recurrence_forward(const adacomp_recurrence_t *op, const adacomp_ste
     a.last = last;
     a.states = states;
     a.near_rows = near_rows(a.x) && near_rows(a.forget) && near_rows(a.out) && near_rows(a.y);
-    a.apart = apart(a.y, a.x, op) && apart(a.y, a.forget, op) && apart(a.y, a.out, op);
+    a.apart = states_apart(first, last, op) && apart(a.y, a.x, op) && apart(a.y, a.forget, op) && apart(a.y, a.out, op);
     a.changes = reinterpret_cast<float *>(static_cast<char *>(workspace) + recurrence_sums({a.segments, a.segment}, a.batch, a.channels));
     return launch_recurrence_forward(a, op->dtype, hip_stream);
 }
@@ -242,7 +249,7 @@ int adacomp_recurrence_backward(const adacomp_recurrence_t *op, const adacomp_st
         if (a.length != 0 && !states) return ADACOMP_EINVAL;
         if (int rc = workspace_check(workspace, workspace_bytes, adacomp_recurrence_workspace_bytes(op->batch, op->length, op->channels))) return rc;
         a.near_rows = near_rows(a.x) && near_rows(a.forget) && near_rows(a.out) && near_rows(a.y) && near_rows(a.dx) && near_rows(a.dforget) && near_rows(a.dout);
-        a.apart = true;
+        a.apart = states_apart(dlast, dfirst, op);
         for (const StepsArgs *out : {&a.dx, &a.dforget, &a.dout})
             for (const StepsArgs *in : {&a.x, &a.forget, &a.out, &a.y}) a.apart = a.apart && apart(*out, *in, op);
         a.first = dlast;

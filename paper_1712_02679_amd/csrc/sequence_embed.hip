@@ -46,9 +46,8 @@ template <typename T> __global__ __launch_bounds__(256) void k_embed_forward(Emb
 // wave's places of each token go, and the waves look at their run again and put them there in order.  No workgroup waits for
 // another, and the order does not depend on which of them comes first.
 
-constexpr uint32_t kChunks = 16;   // of 64 tokens, that a wave has on their way at once
-
-__global__ __launch_bounds__(kSortThreads) void k_embed_sort(EmbedArgs a)
+// kChunks of 64 tokens are on their way to a wave at once, and stay in its registers if it has no more.
+template <uint32_t kChunks> __global__ __launch_bounds__(kSortThreads) void k_embed_sort(EmbedArgs a)
 {
     extern __shared__ uint32_t counts[];   // [waves][range]
     __shared__ uint32_t room[kSortWaves];
@@ -63,11 +62,14 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_sort(EmbedArgs a)
     // no branch around a load: they are on their way together
     auto fetch = [&](uint32_t from) {
         if (a.index64) {
-            int64_t raw[kChunks];
 #pragma unroll
-            for (uint32_t k = 0; k < kChunks; ++k) raw[k] = static_cast<const int64_t *>(a.tokens)[min(from + k * 64u + lane, a.rows - 1u)];
+            for (uint32_t half = 0; half < kChunks; half += 16u) {
+                int64_t raw[16];
 #pragma unroll
-            for (uint32_t k = 0; k < kChunks; ++k) tokens[k] = uint64_t(raw[k]) < a.vocab ? uint32_t(raw[k]) : a.vocab;
+                for (uint32_t k = 0; k < 16u; ++k) raw[k] = static_cast<const int64_t *>(a.tokens)[min(from + (half + k) * 64u + lane, a.rows - 1u)];
+#pragma unroll
+                for (uint32_t k = 0; k < 16u; ++k) tokens[half + k] = uint64_t(raw[k]) < a.vocab ? uint32_t(raw[k]) : a.vocab;
+            }
         } else {
 #pragma unroll
             for (uint32_t k = 0; k < kChunks; ++k) tokens[k] = static_cast<const uint32_t *>(a.tokens)[min(from + k * 64u + lane, a.rows - 1u)];
@@ -124,7 +126,7 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_sort(EmbedArgs a)
     __syncthreads();
     for (uint32_t from = begin; from < end; from += kChunks * 64u) {
         const uint32_t chunk = (from - begin) / 64u;
-        if (!(hits >> chunk / hits_of_run & (2u << (chunk + kChunks - 1u) / hits_of_run - chunk / hits_of_run) - 1u)) continue;   // none of these is here
+        if (!(hits >> chunk / hits_of_run & uint32_t((uint64_t(2) << (chunk + kChunks - 1u) / hits_of_run - chunk / hits_of_run) - 1u))) continue;   // none of these is here
         if (run > kChunks * 64u) fetch(from);
 #pragma unroll
         for (uint32_t k = 0; k < kChunks; ++k) {
@@ -307,7 +309,10 @@ int launch_embed_backward(const EmbedArgs &args, uint32_t dtype, void *stream)
     a.piece = form.piece;
     a.pieces = form.pieces;
     a.pitch = form.pitch;
-    hipLaunchKernelGGL(k_embed_sort, dim3((a.vocab + a.range - 1u) / a.range), dim3(kSortThreads), a.range * kSortWaves * 4u, s, a);
+    const dim3 ranges((a.vocab + a.range - 1u) / a.range);
+    const uint32_t counts = a.range * kSortWaves * 4u;
+    if (a.rows <= 16u * kSortThreads) hipLaunchKernelGGL(k_embed_sort<16>, ranges, dim3(kSortThreads), counts, s, a);
+    else hipLaunchKernelGGL(k_embed_sort<32>, ranges, dim3(kSortThreads), counts, s, a);
     if (int rc = check_launch()) return rc;
     const uint32_t teams = kSumThreads / a.team;
     a.sum_blocks = uint32_t((uint64_t(a.pieces) * a.slabs + teams - 1u) / teams);

@@ -97,7 +97,7 @@ inline RecurrenceForm recurrence_form(uint32_t batch, uint32_t length, uint32_t 
     const uint64_t workgroups = uint64_t(batch) * ((channels + kSlab - 1u) / kSlab);
     if (workgroups == 0 || workgroups >= kComputeUnits || length == 0) return {1u, std::max(length, 1u)};
     const uint64_t wanted = std::min<uint64_t>((2u * kComputeUnits + workgroups - 1u) / workgroups, (length + kLeast - 1u) / kLeast);
-    const uint32_t segment = uint32_t((length + wanted - 1u) / wanted + kLeast - 1u) / kLeast * kLeast;
+    const uint32_t segment = std::max<uint32_t>(1u, uint32_t(length / wanted + kLeast / 2u) / kLeast) * kLeast;
     return {(length + segment - 1u) / segment, segment};
 }
 

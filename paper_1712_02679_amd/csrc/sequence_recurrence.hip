@@ -270,13 +270,19 @@ template <typename T, int WAVES, int L> struct Place {
 // Few sequences of few channels are cut into parts.  One launch says what each part does to the state (BACK: to the gradient that comes from
 // behind), as one change; the next one's workgroups put the changes before their part together and walk along it.  Here nothing
 // but the end of a part is wanted, so each group of 16 threads goes along a run of its own, without a scan until the last place.
+// The part that nobody comes behind has the place of its change for the state that the sequence begins with: the second launch does not read that where
+// the caller has it, since the last state may be written over it.
 
 template <typename T, int WAVES, int L, bool RESETS, bool BACK, bool GATE> __global__ __launch_bounds__(WAVES * 64) void k_recurrence_changes(RecurrenceArgs a)
 {
     __shared__ Change room[WAVES][16];
     const Job job(a);
-    if (job.segment == (BACK ? 0u : a.segments - 1u)) return;   // nobody comes behind
     const Place<T, WAVES, L> p(a, job);
+    float *to = a.changes + (uint64_t(job.sequence) * a.segments + job.segment) * 2u * a.channels + p.ch.first;
+    if (job.segment == (BACK ? 0u : a.segments - 1u)) {
+        if (threadIdx.x < 16u) p.ch.store(to, a.first ? p.ch.load(a.first + p.state(a.channels, p.b)) : f32x4(0.f));
+        return;
+    }
     const uint32_t last = max(min(job.end, p.end), job.begin);   // places behind the sequence's end change nothing
     const uint32_t each = (last - job.begin + WAVES * 4u - 1u) / (WAVES * 4u), group = threadIdx.x / 16u;
     const uint32_t begin = min(job.begin + group * each, last), count = min(each, last - begin);
@@ -335,7 +341,6 @@ template <typename T, int WAVES, int L, bool RESETS, bool BACK, bool GATE> __glo
     Change total = {1.f, 0.f};
 #pragma unroll
     for (int i = 0; i < WAVES; ++i) total = then<RESETS>(total, room[BACK ? WAVES - 1 - i : i][lane]);
-    float *to = a.changes + (uint64_t(job.sequence) * a.segments + job.segment) * 2u * a.channels + p.ch.first;
     p.ch.store(to, total.m);
     p.ch.store(to + a.channels, total.v);
 }
@@ -346,8 +351,11 @@ template <int WAVES, bool RESETS, bool BACK, typename P>
 __device__ __forceinline__ f32x4 begin_of_part(const RecurrenceArgs &a, const P &p, const Job &job, Change (&room)[WAVES][16])
 {
     f32x4 carry = 0.f;
-    if (a.first) carry = p.ch.load(a.first + p.state(a.channels, p.b));
-    if (a.segments == 1u) return carry;
+    if (a.segments == 1u) {
+        if (a.first) carry = p.ch.load(a.first + p.state(a.channels, p.b));
+        return carry;
+    }
+    carry = p.ch.load(a.changes + (uint64_t(job.sequence) * a.segments + (BACK ? 0u : a.segments - 1u)) * 2u * a.channels + p.ch.first);
     const uint32_t before = BACK ? a.segments - 1u - job.segment : job.segment, each = (before + WAVES * 4u - 1u) / (WAVES * 4u), group = threadIdx.x / 16u;
     const uint32_t order = BACK ? WAVES * 4u - 1u - group : group;
     Change all = {1.f, 0.f};

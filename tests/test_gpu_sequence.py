@@ -293,6 +293,26 @@ def test_recurrence_in_place(A):
             assert torch.equal(got, want[name]), name
 
 
+@pytest.mark.parametrize("batch,length,channels", [(25, 1000, 509), (3, 3000, 67), (200, 300, 131), (300, 20, 66)])
+def test_recurrence_states_over_themselves(A, batch, length, channels):
+    """The last state over the first one, of sequences in parts and in one, with incomplete groups of channels that slabs share: as in separate buffers."""
+    s = recurrence_case(batch, length, channels, BF16, True, True, True, False, False, 16)
+    g = run_forward(A, s, BF16)
+    first, y = g["first"].clone(), torch.empty_like(g["y"])
+    A.adacomp_recurrence_forward(g["x"], g["forget"], y, g["ws"], out=g["out"], bias=g["bias"], first=first, last=first)
+    assert torch.equal(y, g["y"]) and torch.equal(first, g["last"])
+    dy, dlast = rand((batch, length, channels), BF16, 17).to(DEV), rand((batch, channels), F32, 18).to(DEV)
+    results = []
+    for over in (False, True):
+        d, dfirst = [torch.empty_like(dy) for _ in range(3)], torch.empty_like(dlast)
+        start = dlast.clone()
+        dfirst = start if over else dfirst
+        A.adacomp_recurrence_backward(dy, g["x"], g["forget"], g["states"], d[0], d[1], g["ws"], out=g["out"], dout=d[2], bias=g["bias"], dlast=start, dfirst=dfirst)
+        results.append([*d, dfirst])
+    for one, other in zip(*results):
+        assert torch.equal(one, other)
+
+
 def test_recurrence_token_by_token_is_the_whole_sequence(A):
     """Serving: single tokens with the state carried along, against the sequence at once; some sequences get no token now and then."""
     b, n, c = 5, 70, 130
