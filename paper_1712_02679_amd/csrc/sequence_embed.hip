@@ -50,7 +50,7 @@ template <typename T> __global__ __launch_bounds__(256) void k_embed_forward(Emb
 template <uint32_t kChunks> __global__ __launch_bounds__(kSortThreads) void k_embed_sort(EmbedArgs a)
 {
     extern __shared__ uint32_t counts[];   // [waves][range]
-    __shared__ uint32_t room[kSortWaves];
+    __shared__ uint32_t room[2][kSortWaves];   // places below the range and in it, of every wave and of every 64 tokens
     const uint32_t lane = threadIdx.x % 64u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64u);
     const uint32_t low = blockIdx.x * a.range, n = min(a.range, a.vocab - low);
     for (uint32_t i = threadIdx.x; i < n * kSortWaves; i += kSortThreads) counts[i] = 0;
@@ -84,45 +84,45 @@ template <uint32_t kChunks> __global__ __launch_bounds__(kSortThreads) void k_em
         if (from != begin) fetch(from);
 #pragma unroll
         for (uint32_t k = 0; k < kChunks; ++k) {
-            below += tokens[k] < low ? 1u : 0u;
+            below += uint32_t(__builtin_popcountll(__ballot(tokens[k] < low)));   // of the wave
             const bool here = tokens[k] - low < n;
             if (__ballot(here)) hits |= 1u << ((from - begin) / 64u + k) / hits_of_run;
             if (here) atomicAdd(&mine[tokens[k] - low], 1u);
         }
     }
-    for (uint32_t s = 32; s > 0; s /= 2u) below += __shfl_xor(below, s);
-    if (lane == 0u) room[wave] = below;
+    if (lane == 0u) room[0][wave] = below;
     __syncthreads();
-    uint32_t base = 0;
-    for (uint32_t w = 0; w < kSortWaves; ++w) base += room[w];
-    // counts, token by token and in each wave by wave, become where they begin: the first wave adds them up, 64 tokens at a time
-    if (wave == 0u) {
-        for (uint32_t t = 0; t < n; t += 64u) {
-            uint32_t all = 0;
-            if (t + lane < n)
+    // counts, token by token and in each wave by wave, become where they begin: a token to a thread
+    static_assert(kSortRange <= kSortThreads, "a thread for every token");
+    const uint32_t token = threadIdx.x;
+    uint32_t of_wave[kSortWaves], all = 0;
 #pragma unroll
-                for (uint32_t w = 0; w < kSortWaves; ++w) all += counts[w * n + t + lane];
-            uint32_t upto = all;
-            for (uint32_t s = 1; s < 64u; s *= 2u) {
-                const uint32_t other = __shfl_up(upto, s);
-                if (lane >= s) upto += other;
-            }
-            uint32_t at = base + upto - all;
-            base += __shfl(upto, 63);
-            if (t + lane < n) {
-                a.first[low + t + lane] = at;
-                uint32_t of_wave[kSortWaves];
-#pragma unroll
-                for (uint32_t w = 0; w < kSortWaves; ++w) of_wave[w] = counts[w * n + t + lane];
-#pragma unroll
-                for (uint32_t w = 0; w < kSortWaves; ++w) {
-                    counts[w * n + t + lane] = at;
-                    at += of_wave[w];
-                }
-            }
-        }
-        if (lane == 0u && low + n == a.vocab) a.first[a.vocab] = base;
+    for (uint32_t w = 0; w < kSortWaves; ++w) {
+        of_wave[w] = token < n ? counts[w * n + token] : 0u;
+        all += of_wave[w];
     }
+    uint32_t upto = all;
+    for (uint32_t s = 1; s < 64u; s *= 2u) {
+        const uint32_t other = __shfl_up(upto, s);
+        if (lane >= s) upto += other;
+    }
+    if (lane == 63u) room[1][wave] = upto;
+    __syncthreads();
+    uint32_t at = upto - all, total = 0;
+#pragma unroll
+    for (uint32_t w = 0; w < kSortWaves; ++w) {
+        at += room[0][w] + (w < wave ? room[1][w] : 0u);
+        total += room[0][w] + room[1][w];
+    }
+    if (token < n) {
+        a.first[low + token] = at;
+#pragma unroll
+        for (uint32_t w = 0; w < kSortWaves; ++w) {
+            counts[w * n + token] = at;
+            at += of_wave[w];
+        }
+    }
+    if (threadIdx.x == 0u && low + n == a.vocab) a.first[a.vocab] = total;
     __syncthreads();
     for (uint32_t from = begin; from < end; from += kChunks * 64u) {
         const uint32_t chunk = (from - begin) / 64u;
