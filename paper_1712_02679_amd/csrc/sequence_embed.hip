@@ -2,9 +2,10 @@
 //
 // The lookup reads a 32-bit row of the table for every place (those asked for again come from the caches) and writes y: memory bounds it, 16384 x 4096 bf16
 // with dropout, from 32768 rows, 55 us (5.9 TB/s), 65536 x 512 bf16 21 us (6.7 TB/s).  The gradient reads dy once and writes the whole table: three
-// launches, sorting, sums and the joining of what several pieces have of a token.  32768 x 1001 bf16 with dropout over 50000 tokens 99 us (2.7 TB/s of what it needs): sorting 18,
-// sums 59 (4.5 TB/s), joining 7.  12800 x 512 f32 over 65 tokens 26 us, three chains of dependent accesses of 11, 6 and 9.  131072 x 512 bf16 over 50000
-// 119 us, about half of it sorting, whose work is places times ranges.
+// launches, sorting, sums and the joining of what several pieces have of a token.  32768 x 1001 bf16 with dropout over 50000 tokens 72 us on inputs that the
+// caches hold, 90 on others (2.9 TB/s); zeros of tokens that do not occur are stored while places are sorted (without that 80).  12800 x 512 f32 over
+// 65 tokens 26 us, three chains of dependent accesses of 11, 6 and 9.  131072 x 512 bf16 over 50000 117 us, about half of it sorting, whose work is places
+// times ranges.
 #include "layers_device.h"
 #include "sequence_plan.h"
 
@@ -57,6 +58,8 @@ template <uint32_t kChunks> __global__ __launch_bounds__(kSortThreads) void k_em
 {
     extern __shared__ uint32_t counts[];   // [waves][range]
     __shared__ uint32_t room[2][kSortWaves];   // places below the range and in it, of every wave and of every 64 tokens
+    __shared__ uint64_t empty[kSortRange / 64u];
+    typedef float zeros4 __attribute__((ext_vector_type(4), aligned(4)));
     const uint32_t lane = threadIdx.x % 64u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64u);
     const uint32_t low = blockIdx.x * a.range, n = min(a.range, a.vocab - low);
     for (uint32_t i = threadIdx.x; i < n * kSortWaves; i += kSortThreads) counts[i] = 0;
@@ -132,7 +135,22 @@ template <uint32_t kChunks> __global__ __launch_bounds__(kSortThreads) void k_em
         }
     }
     if (threadIdx.x == 0u && low + n == a.vocab) a.first[a.vocab] = total;
+    const uint64_t none = __ballot(token < n && all == 0u);   // of the wave's 64 tokens
+    if (lane == 0u && wave < kSortRange / 64u) empty[wave] = none;
     __syncthreads();
+    // zeros for the tokens that do not occur: stores that are on their way while the places are put in order
+    if (!a.accumulate) {
+        const uint32_t beside = 64u / a.zero_team, c = lane % a.zero_team * 4u;   // rows of a wave side by side, 4 columns to a thread
+        for (uint32_t t = wave * beside + lane / a.zero_team; t < n; t += kSortWaves * beside) {
+            if (!(empty[t / 64u] >> t % 64u & 1u)) continue;
+            float *out = a.dtable + uint64_t(low + t) * a.cols;
+            for (uint32_t col = c; col < a.cols; col += a.zero_team * 4u) {
+                if (col + 4u <= a.cols) *reinterpret_cast<zeros4 *>(out + col) = zeros4(0.f);
+                else
+                    for (uint32_t k = col; k < a.cols; ++k) out[k] = 0.f;
+            }
+        }
+    }
     for (uint32_t from = begin; from < end; from += kChunks * 64u) {
         if (run > kChunks * 64u) fetch(from);
 #pragma unroll
@@ -159,7 +177,6 @@ template <uint32_t kChunks> __global__ __launch_bounds__(kSortThreads) void k_em
 // The order is cut into pieces of as many places, whatever their tokens are, so that a frequent token's are shared out like all others.  A team of
 // threads has a piece and a slab of columns, 8 to a thread, and adds up the rows of a token while it lasts.  A token whose places lie in
 // one piece is done then.  Of one that goes on in another piece every piece leaves its part, and k_embed_join adds them up in order.
-// The other workgroups of the launch write the zeros of tokens that do not occur.
 
 constexpr uint32_t kSumThreads = 256;
 
@@ -168,17 +185,6 @@ template <typename T, bool DROP> __global__ __launch_bounds__(kSumThreads) void 
     extern __shared__ EmbedPlace staged[];   // [teams][piece + 2]: the places of a piece, one before and one behind
     constexpr uint32_t BATCH = 16u / sizeof(T);   // rows on their way at once
     const uint32_t t = threadIdx.x & (a.team - 1u), team = threadIdx.x / a.team, teams = kSumThreads / a.team;
-    if (blockIdx.x >= a.sum_blocks) {
-        for (uint64_t v = (blockIdx.x - a.sum_blocks) * uint64_t(teams) + team; v < a.vocab; v += uint64_t(gridDim.x - a.sum_blocks) * teams) {
-            if (a.first[v] != a.first[v + 1u]) continue;
-            float *out = a.dtable + v * a.cols;
-            for (uint32_t c = t * 8u; c < a.cols; c += a.team * 8u) {
-                if (c + 8u <= a.cols) store8(out + c, f32x8(0.f));
-                else store_some(out + c, a.cols - c, f32x8(0.f));
-            }
-        }
-        return;
-    }
     const Drop d = drop_of(a.drop);
     const uint32_t job = blockIdx.x * teams + team, piece = job / a.slabs, slab = job - piece * a.slabs;
     const uint32_t count_all = a.first[a.vocab], begin = min(piece, a.pieces) * a.piece;
@@ -316,16 +322,17 @@ int launch_embed_backward(const EmbedArgs &args, uint32_t dtype, void *stream)
     a.piece = form.piece;
     a.pieces = form.pieces;
     a.pitch = form.pitch;
+    a.zero_team = 4;
+    while (a.zero_team < 64u && a.zero_team * 4u < a.cols) a.zero_team *= 2u;
     const dim3 ranges((a.vocab + a.range - 1u) / a.range);
     const uint32_t counts = a.range * kSortWaves * 4u;
     if (a.rows <= 16u * kSortThreads) hipLaunchKernelGGL(k_embed_sort<16>, ranges, dim3(kSortThreads), counts, s, a);
     else hipLaunchKernelGGL(k_embed_sort<32>, ranges, dim3(kSortThreads), counts, s, a);
     if (int rc = check_launch()) return rc;
     const uint32_t teams = kSumThreads / a.team;
-    a.sum_blocks = uint32_t((uint64_t(a.pieces) * a.slabs + teams - 1u) / teams);
-    const uint32_t zero_blocks = a.accumulate ? 0u : std::min((a.vocab + teams - 1u) / teams, 8u * kComputeUnits);
-    if (a.sum_blocks + zero_blocks != 0u) {
-        const dim3 grid(a.sum_blocks + zero_blocks), wg(kSumThreads);
+    const uint32_t blocks = uint32_t((uint64_t(a.pieces) * a.slabs + teams - 1u) / teams);
+    if (blocks != 0u) {
+        const dim3 grid(blocks), wg(kSumThreads);
         const uint32_t lds = teams * (a.piece + 2u) * 8u;
         const int rc = with_type(dtype, [&](auto of) {
             using T = decltype(of);

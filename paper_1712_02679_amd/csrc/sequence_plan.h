@@ -23,7 +23,7 @@ struct EmbedArgs {
     uint32_t rows, vocab, cols, groups;   // groups of 8 to a row
     uint32_t index64, accumulate;
     uint32_t range, team, slabs, piece, pieces, pitch;   // see EmbedForm
-    uint32_t sum_blocks;  // workgroups that add up; those behind them write zeros
+    uint32_t zero_team;   // threads that write a row of zeros
     float scale;
     DropArgs drop;
 };
