@@ -210,7 +210,7 @@ template <typename T, int TPR, int V, bool HELD, int PASS> __global__ __launch_b
             sum1 = two ? over_team<Add, TPR>(sum1, room[3], team) : sum;
             inv = sum == 0.f || zmax * c == -kInf ? 0.f : 1.f / sum;
             inv1 = sum1 == 0.f ? 0.f : 1.f / sum1;
-            const float log_sum = logf(sum), log_sum1 = two ? logf(sum1) : log_sum;
+            const float log_sum = zmax * c == kInf ? __builtin_nanf("") : logf(sum), log_sum1 = two ? logf(sum1) : log_sum;
             lse = zmax * c + log_sum;
             lse1 = zmax + log_sum1;
             if (live && t == 0u) {
@@ -234,7 +234,8 @@ template <typename T, int TPR, int V, bool HELD, int PASS> __global__ __launch_b
             off1 = told ? finite_or_zero(lse1) : kInf;
             inv = inv1 = 1.f;
         } else {
-            off = off1 = zmax * c == kInf ? __builtin_nanf("") : finite_or_zero(zmax);
+            off = (taught || !two) && zmax * c == kInf ? __builtin_nanf("") : zoff;
+            off1 = zmax == kInf ? __builtin_nanf("") : zoff;
         }
         const Exponent<T, PASS == GRAD> ex(off, c), ex1(off1, 1.f);
         const float by = (two ? soft : soft + hard) * inv, by1 = hard * inv1;

@@ -247,6 +247,13 @@ def test_recurrence_channels(A, channels, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("batch,length,channels", [(3, 1, 1), (3, 1, 2), (5, 2, 3), (4, 5, 5), (3, 12, 67), (7, 11, 130), (700, 13, 6), (3400, 66, 5)])
+def test_recurrence_place_by_place(A, batch, length, channels, dtype):
+    """Calls whose threads take sequences from their first place to the last: short ones, and very many."""
+    check_both(A, recurrence_case(batch, length, channels, dtype, channels % 2 == 1, True, True, channels != 2, channels in (1, 5, 67), 21), dtype, pad=channels % 3, lead=channels % 2)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("gate,bias,first,ragged,resets", [(False, False, False, False, False), (True, False, True, False, False), (False, True, False, True, False),
                                                            (True, True, True, True, True), (False, True, True, False, True)])
 def test_recurrence_forms(A, gate, bias, first, ragged, resets, dtype):
@@ -628,6 +635,25 @@ def test_distill_nan_stays_in_its_row(A):
         assert torch.isfinite(grad[[0, 3]]).all() and torch.isnan(grad[1]).all() and torch.isnan(grad[2]).all()
 
 
+def test_distill_of_logits_beyond_the_range(A):
+    """z / temperature beyond float32: a row with +infinity there is NaN, loss and gradient, in either way; one with -infinity at all places has q = 0; and the
+    target's term, at a temperature of 1, is what it is in a row without a teacher."""
+    for vocab in (50, 2000, 33000):
+        z = rand((3, vocab), F32, 19)
+        z[0, 7] = 3e38
+        z[1] = torch.finfo(F32).min
+        z[2, 7] = 3e38
+        tokens, t, targets = torch.tensor([[3, 4], [3, 4], [-1, -1]]), rand((3, 2), F32, 20), torch.tensor([1, 1, 7])
+        args = dict(teacher_tokens=tokens.to(DEV), teacher_logits=t.to(DEV), targets=targets.to(DEV), temperature=0.5, soft=0.5, hard=0.5)
+        loss, lse, grad = torch.empty(3, device=DEV), torch.empty(3, 2, device=DEV), torch.empty(3, vocab, device=DEV)
+        A.adacomp_distill_forward(z.to(DEV), loss, lse=lse, dlogits=grad, **args)
+        back = torch.empty_like(grad)
+        A.adacomp_distill_backward(z.to(DEV), lse, back, **args)
+        assert torch.isnan(loss[0]) and loss[1] == float("inf") and loss[2] == 0
+        for g in (grad, back):
+            assert torch.isnan(g[0]).all() and torch.isfinite(g[1:]).all() and torch.all(g[2] == 0)
+
+
 def test_distill_refusals(A):
     z, loss, lse, grad = torch.zeros(4, 9, device=DEV), torch.zeros(4, device=DEV), torch.zeros(4, 2, device=DEV), torch.zeros(4, 9, device=DEV)
     k, t, targets = torch.zeros(4, 3, dtype=torch.int64, device=DEV), torch.zeros(4, 3, device=DEV), torch.zeros(4, dtype=torch.int64, device=DEV)
@@ -703,6 +729,29 @@ def test_captured_and_replayed(A):
             torch.cuda.synchronize()
             for i, (got, want) in enumerate(zip(results, eager)):
                 assert torch.equal(got, want), (turn, i)
+
+
+def test_embed_step_in_memory(A):
+    """A captured lookup and its gradient draw another mask when the number in memory has changed, the same one in both."""
+    tokens, table, dy = tokens_of(200, 30, 22).to(DEV), rand((30, 45), F32, 23).to(DEV), rand((200, 45), F32, 24).to(DEV)
+    y, dtable, ws, step = torch.empty(200, 45, device=DEV), torch.empty(30, 45, device=DEV), embed_room(A, 200, 30, 45), torch.zeros(1, dtype=torch.int64, device=DEV)
+    drop = A.Dropout(0.4, 5, 100, step)
+
+    def calls():
+        A.adacomp_embed_forward(tokens, table, y, dropout=drop)
+        A.adacomp_embed_backward(tokens, dy, dtable, ws, dropout=drop)
+    calls()
+    torch.cuda.synchronize()
+    graph = capture(calls)
+    for number in (0, 3, 3, 9):
+        step.fill_(number)
+        graph.replay()
+        torch.cuda.synchronize()
+        f = (0.4, 5, 100 + number)
+        want = S.embed_forward(tokens.cpu(), table.cpu().double(), 1.0, f)
+        within(y, want, rounded(want, 4 * U * want.abs(), F32), ("y", number))
+        want, size, count = S.embed_backward(tokens.cpu(), dy.cpu().double(), 30, 1.0, f)
+        within(dtable, want, U * ((count + 8).double()[:, None] * size + 2 * want.abs()) + TINY[F32], ("dtable", number))
 
 
 def test_on_other_streams_at_once(A):
