@@ -83,7 +83,7 @@ int adacomp_recurrence_forward(const adacomp_recurrence_t *op, const adacomp_ste
                                const float *first, const adacomp_steps_t *y, float *last, float *states, void *workspace, size_t workspace_bytes,
                                void *hip_stream);
 
-/* out and dout are both given or both NULL.  dlast, dfirst [batch, channels] float32: dlast NULL: zeros, dfirst NULL: not wanted;
+/* out and dout are both given or both NULL.  dlast, dfirst [batch, channels] float32: dlast NULL: zeros, dfirst NULL: not wanted; they may be the same buffer;
  * dbias [channels] NULL: not wanted, accumulate != 0 adds to what is there, 0 overwrites. */
 int adacomp_recurrence_backward(const adacomp_recurrence_t *op, const adacomp_steps_t *dy, const adacomp_steps_t *x, const adacomp_steps_t *forget,
                                 const adacomp_steps_t *out, const float *states, const float *dlast, const adacomp_steps_t *dx,

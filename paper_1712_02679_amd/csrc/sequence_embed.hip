@@ -1,7 +1,7 @@
 // sequence_embed.hip -- kernels of the embedding (adacomp_sequence.h).
 //
 // The lookup reads a 32-bit row of the table for every place (those asked for again come from the caches) and writes y: memory bounds it, 16384 x 4096 bf16
-// with dropout, from 32768 rows, 55 us (5.9 TB/s), 65536 x 512 bf16 21 us (6.7 TB/s).  The gradient reads dy once and writes the whole table: three
+// with dropout, from 32768 rows, 49 us (6.0 TB/s; 55 with results through the caches), 65536 x 512 bf16 20 us (7.1 TB/s).  The gradient reads dy once and writes the whole table: three
 // launches, sorting, sums and the joining of what several pieces have of a token.  32768 x 1001 bf16 with dropout over 50000 tokens 72 us on inputs that the
 // caches hold, 90 on others (2.9 TB/s); zeros of tokens that do not occur are stored while places are sorted (without that 80).  12800 x 512 f32 over
 // 65 tokens 26 us, three chains of dependent accesses of 11, 6 and 9.  131072 x 512 bf16 over 50000 117 us, about half of it sorting, whose work is places
@@ -43,7 +43,8 @@ template <typename T> __global__ __launch_bounds__(256) void k_embed_forward(Emb
         if (a.drop.on) v = drop8(v, d, c / 8u, uint32_t(row));
     }
     T *y = static_cast<T *>(a.rows_of) + row * a.stride + c;
-    if (c + 8u <= a.cols) store8(y, v);
+    if (c + 8u <= a.cols && sizeof(T) == 2) store8_past(y, v);
+    else if (c + 8u <= a.cols) store8(y, v);
     else store_some(y, a.cols - c, v);
 }
 
