@@ -89,6 +89,7 @@ template <int TPR> __device__ __forceinline__ void sync_lds()
 template <typename T, int TPR, int V, bool HELD, int PASS> __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_distill(DistillArgs a)
 {
     constexpr uint32_t TEAMS = TPR > 256 ? 1 : 256 / TPR, PART = TPR * V * 8;
+    using Groups = RowGroups<T, TPR, V, kFlow<T>, DistillForm{TPR, V, HELD}.short_rows()>;
     extern __shared__ __attribute__((aligned(16))) float entries_room[];
     __shared__ float room[6][16];
     const uint32_t t = threadIdx.x % TPR, team = team_of<TPR>(), whole_parts = HELD ? 0u : a.vocab / PART;
@@ -100,7 +101,7 @@ template <typename T, int TPR, int V, bool HELD, int PASS> __global__ __launch_b
         const uint64_t row = first + team;
         const bool live = row < a.rows;
         const T *z = static_cast<const T *>(a.logits) + row * a.logits_stride;
-        const RowGroups<T, TPR, V> last = {t, a.vocab, whole_parts * PART};   // the part that the row ends in
+        const Groups last = {t, a.vocab, whole_parts * PART};   // the part that the row ends in
         raw8<T> raw[V] = {};
         if (HELD && live) last.load(raw, z);
         // f(values) of every part: of whole ones, each with the next one on its way, and of the last one, where `behind` stands behind the row's end
@@ -255,7 +256,7 @@ template <typename T, int TPR, int V, bool HELD, int PASS> __global__ __launch_b
                     for (int k = 0; k < 8; ++k) y[v][k] = none ? 0.f : gradient(x[v][k]);
                 if constexpr (FULL) {
 #pragma unroll
-                    for (int v = 0; v < V; ++v) RowGroups<T, TPR, V>::store_whole(at(dz, first_col + (t + uint32_t(v) * TPR) * 8u), y[v]);
+                    for (int v = 0; v < V; ++v) Groups::store_whole(at(dz, first_col + (t + uint32_t(v) * TPR) * 8u), y[v]);
                 } else {
                     last.store(dz, [&](int v) { return y[v]; });
                 }
@@ -286,18 +287,16 @@ template <typename T, int TPR, int V, bool HELD, int PASS> __global__ __launch_b
 
 // ---- launches -----------------------------------------------------------------------------------------------------
 
-// Threads to a row.  Short rows are held, with the entries of all teams within 64 KB of LDS; others are read in parts, twice for loss and gradient: held
-// in registers they leave so few waves that rows of 16384 take twice as long.  A wave to a row needs no barrier, but many rows; few long rows need all
-// threads that a workgroup can have.  64 / 256 / 1024 threads, loss and gradient of bf16 with 64 top tokens, us: 32768 x 2000 91 / 176 / 840, 16384 x 5000
-// 100 / 128 / 430, 8192 x 16384 166 / 141 / 249, 4096 x 65536 331 / 288 / 298, 1024 x 5000 18.7 / 18.5 / 34, 256 x 50000 65 / 27 / 23.
-template <typename F> static void with_distill(uint64_t rows, uint32_t vocab, uint32_t top, F &&f)
+template <typename F> static void with_distill(const DistillForm &form, F &&f)
 {
+    using One = std::integral_constant<int, 1>;
     using Two = std::integral_constant<int, 2>;
     using Four = std::integral_constant<int, 4>;
-    if (vocab <= 256u && top < 160u) f(std::integral_constant<int, 8>(), Four(), std::true_type());
-    else if (vocab <= 1024u) f(std::integral_constant<int, 32>(), Four(), std::true_type());
-    else if (rows >= 4096u && vocab <= 8192u) f(std::integral_constant<int, 64>(), Two(), std::false_type());
-    else if (rows >= 512u || vocab <= 16384u) f(std::integral_constant<int, 256>(), Two(), std::false_type());
+    if (form.threads == 8u) f(std::integral_constant<int, 8>(), Four(), std::true_type());
+    else if (form.threads == 32u && form.groups == 1u) f(std::integral_constant<int, 32>(), One(), std::true_type());
+    else if (form.threads == 32u) f(std::integral_constant<int, 32>(), Four(), std::true_type());
+    else if (form.threads == 64u) f(std::integral_constant<int, 64>(), Two(), std::false_type());
+    else if (form.threads == 256u) f(std::integral_constant<int, 256>(), Two(), std::false_type());
     else f(std::integral_constant<int, 1024>(), Two(), std::false_type());
 }
 
@@ -308,7 +307,7 @@ int launch_distill(const DistillArgs &a, uint32_t dtype, DistillPass pass, void 
         using T = decltype(of);
         auto go = [&](auto which) {
             constexpr int PASS = decltype(which)::value;
-            with_distill(a.rows, a.vocab, a.top, [&](auto threads, auto groups, auto held) {
+            with_distill(distill_form(a.rows, a.vocab, a.top), [&](auto threads, auto groups, auto held) {
                 constexpr uint32_t TPR = decltype(threads)::value, TEAMS = TPR > 256u ? 1u : 256u / TPR;
                 const uint64_t blocks = (a.rows + TEAMS - 1u) / TEAMS;
                 hipLaunchKernelGGL((k_distill<T, int(TPR), decltype(groups)::value, decltype(held)::value, PASS>), dim3(uint32_t(std::min<uint64_t>(blocks, 1u << 20))),
