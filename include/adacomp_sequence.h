@@ -43,7 +43,8 @@ int adacomp_embed_backward(const adacomp_embed_t *op, const void *dy, float *dta
 /* ---- gated linear recurrence ---------------------------------------------------------------------- */
 
 /* Along each sequence, channel by channel, from the state h[-1] = first:
- *   a[t] = sigmoid(forget[t] + bias),  m[t] = a[t], or 0 where resets[t] != 0 (a document begins there)
+ *   a[t] = sigmoid(forget[t] + bias),  m[t] = a[t], or 0 where resets[t] != 0 (a document begins there: nothing of what was before it
+ *   comes through, and no gradient goes back, NaN and infinities included)
  *   h[t] = m[t] h[t - 1] + (1 - a[t]) x[t],  y[t] = sigmoid(out[t]) h[t], or h[t] without out
  * Places from lengths[b] on are padding: not looked at, the state stays what it is, y and gradients are zeros there.
  * Backward, with G[t] = sigmoid(out[t]) dy[t] + m[t + 1] G[t + 1], at the sequence's last place dlast added:

@@ -83,74 +83,98 @@ template <typename T> __device__ __forceinline__ float sigmoid_of(float f)
     return gate_of<T>(f).on;
 }
 
-// What comes through a place: nothing through one that begins a document, whatever it is.
-template <bool RESETS> __device__ __forceinline__ float through(float m, float h)
+// A change of 4 channels' states.  With resets it says apart from m whether a document begins in it, and then nothing comes through, whatever m is: a product of
+// gates may be NaN in front of the document, or too small for float32 without any.
+template <bool RESETS> struct Change { f32x4 m, v; };
+template <> struct Change<true> { f32x4 m, v; uint32_t cut; };
+
+template <bool RESETS> __device__ __forceinline__ Change<RESETS> change_of(f32x4 m, f32x4 v, uint32_t cut)
 {
-    if constexpr (RESETS) return m == 0.f ? 0.f : m * h;
-    return m * h;
+    if constexpr (RESETS) return {m, v, cut};
+    else return {m, v};
+}
+template <bool RESETS> __device__ __forceinline__ Change<RESETS> no_change() { return change_of<RESETS>(1.f, 0.f, 0u); }
+template <bool RESETS> __device__ __forceinline__ uint32_t cut_of(const Change<RESETS> &c)
+{
+    if constexpr (RESETS) return c.cut;
+    else return 0u;
 }
 
-// A change of 4 channels' states.
-struct Change { f32x4 m, v; };
-
-template <bool RESETS> __device__ __forceinline__ f32x4 applied(const Change &c, f32x4 h)
+template <bool RESETS> __device__ __forceinline__ f32x4 applied(const Change<RESETS> &c, f32x4 h)
 {
     f32x4 r;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) r[k] = RESETS ? through<RESETS>(c.m[k], h[k]) + c.v[k] : fmaf(c.m[k], h[k], c.v[k]);
+    for (int k = 0; k < 4; ++k) {
+        r[k] = fmaf(c.m[k], h[k], c.v[k]);
+        if constexpr (RESETS) r[k] = c.cut ? c.v[k] : r[k];
+    }
     return r;
 }
 // One change and then another.
-template <bool RESETS> __device__ __forceinline__ Change then(const Change &one, const Change &other) { return {one.m * other.m, applied<RESETS>(other, one.v)}; }
+template <bool RESETS> __device__ __forceinline__ Change<RESETS> then(const Change<RESETS> &one, const Change<RESETS> &other)
+{
+    return change_of<RESETS>(one.m * other.m, applied(other, one.v), cut_of(one) | cut_of(other));
+}
+
+// Backwards the gradient behind a place, with what the place adds, goes through it.
+template <bool RESETS> __device__ __forceinline__ f32x4 back_through(const Change<RESETS> &c, f32x4 g) { return cut_of(c) ? f32x4(0.f) : c.m * g; }
 
 // x of the even and the odd one of each two neighbouring groups of 16 lanes; of the lower and the upper half of the wave.
-struct Two { float first, second; };
-__device__ __forceinline__ Two groups_of(float x)
+template <typename V> struct Two { V first, second; };
+template <typename V> __device__ __forceinline__ Two<V> groups_of(V x)
 {
     const uint32_t b = __builtin_bit_cast(uint32_t, x);
     const auto r = __builtin_amdgcn_permlane16_swap(b, b, false, false);
-    return {__builtin_bit_cast(float, uint32_t(r[0])), __builtin_bit_cast(float, uint32_t(r[1]))};
+    return {__builtin_bit_cast(V, uint32_t(r[0])), __builtin_bit_cast(V, uint32_t(r[1]))};
 }
-__device__ __forceinline__ Two halves_of(float x)
+template <typename V> __device__ __forceinline__ Two<V> halves_of(V x)
 {
     const uint32_t b = __builtin_bit_cast(uint32_t, x);
     const auto r = __builtin_amdgcn_permlane32_swap(b, b, false, false);
-    return {__builtin_bit_cast(float, uint32_t(r[0])), __builtin_bit_cast(float, uint32_t(r[1]))};
+    return {__builtin_bit_cast(V, uint32_t(r[0])), __builtin_bit_cast(V, uint32_t(r[1]))};
 }
 
 // Over the 4 groups of 16 lanes of a wave, in their order or (BACK) from the last: what lies before each group, and `all` of them.
-template <bool RESETS, bool BACK> __device__ __forceinline__ Change before_groups(const Change &own, Change &all)
+template <bool RESETS, bool BACK> __device__ __forceinline__ Change<RESETS> before_groups(const Change<RESETS> &own, Change<RESETS> &all)
 {
     const uint32_t group = threadIdx.x % 64u / 16u;
-    Change even, odd, lower, upper;
+    Change<RESETS> even, odd, lower, upper;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        const Two m = groups_of(own.m[k]), v = groups_of(own.v[k]);
+        const Two<float> m = groups_of(float(own.m[k])), v = groups_of(float(own.v[k]));
         even.m[k] = m.first; odd.m[k] = m.second;
         even.v[k] = v.first; odd.v[k] = v.second;
     }
-    const Change pair = BACK ? then<RESETS>(odd, even) : then<RESETS>(even, odd);
+    if constexpr (RESETS) {   // places are the same for the lanes of a group
+        const Two<uint32_t> cut = groups_of(own.cut);
+        even.cut = cut.first; odd.cut = cut.second;
+    }
+    const Change<RESETS> pair = BACK ? then(odd, even) : then(even, odd);
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        const Two m = halves_of(pair.m[k]), v = halves_of(pair.v[k]);
+        const Two<float> m = halves_of(float(pair.m[k])), v = halves_of(float(pair.v[k]));
         lower.m[k] = m.first; upper.m[k] = m.second;
         lower.v[k] = v.first; upper.v[k] = v.second;
     }
-    all = BACK ? then<RESETS>(upper, lower) : then<RESETS>(lower, upper);
-    Change before = {1.f, 0.f};
+    if constexpr (RESETS) {
+        const Two<uint32_t> cut = halves_of(pair.cut);
+        lower.cut = cut.first; upper.cut = cut.second;
+    }
+    all = BACK ? then(upper, lower) : then(lower, upper);
+    Change<RESETS> before = no_change<RESETS>();
     if (BACK ? group < 2u : group >= 2u) before = BACK ? upper : lower;   // the other pair
-    if (BACK ? group % 2u == 0u : group % 2u == 1u) before = then<RESETS>(before, BACK ? odd : even);   // the other one of the pair
+    if (BACK ? group % 2u == 0u : group % 2u == 1u) before = then(before, BACK ? odd : even);   // the other one of the pair
     return before;
 }
 
 // The state that a thread begins with, in a workgroup that begins with `carry`, which becomes the one behind its last thread.
 // room: of this block, and of every other one from then on.
 template <int WAVES, bool RESETS, bool BACK>
-__device__ __forceinline__ f32x4 begin_of(const Change &own, f32x4 &carry, Change (&room)[WAVES][16])
+__device__ __forceinline__ f32x4 begin_of(const Change<RESETS> &own, f32x4 &carry, Change<RESETS> (&room)[WAVES][16])
 {
     const uint32_t lane = threadIdx.x % 64u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64u);
-    Change all;
-    const Change before = before_groups<RESETS, BACK>(own, all);
+    Change<RESETS> all;
+    const Change<RESETS> before = before_groups<RESETS, BACK>(own, all);
     if (lane < 16u) room[wave][lane] = all;
     __syncthreads();
     f32x4 mine = carry;
@@ -158,9 +182,9 @@ __device__ __forceinline__ f32x4 begin_of(const Change &own, f32x4 &carry, Chang
     for (int i = 0; i < WAVES; ++i) {
         const int w = BACK ? WAVES - 1 - i : i;
         if (w == int(wave)) mine = carry;
-        carry = applied<RESETS>(room[w][lane % 16u], carry);
+        carry = applied(room[w][lane % 16u], carry);
     }
-    return applied<RESETS>(before, mine);
+    return applied(before, mine);
 }
 
 // Which part of which sequence a workgroup has: slabs of a part are neighbours.
@@ -248,19 +272,27 @@ template <typename T, int WAVES, int L> struct Place {
 #pragma unroll
         for (int i = 0; i < L; ++i) to[i] = row[FULL ? block + run + i : min(block + run + i, length - 1u)];
     }
+    // Bit i: a document begins at place i of the run.
+    template <bool FULL, bool RESETS> __device__ __forceinline__ uint32_t cuts_of(const uint8_t (&reset)[L], uint32_t block) const
+    {
+        uint32_t cuts = 0;
+        if constexpr (RESETS)
+#pragma unroll
+            for (int i = 0; i < L; ++i) cuts |= reset[i] && inside<FULL>(block, i) ? 1u << i : 0u;
+        return cuts;
+    }
     template <bool FULL> __device__ __forceinline__ bool inside(uint32_t block, int i) const { return FULL || block + run + i < end; }
     // A value that counts only inside the sequence, whatever it is.
     template <bool FULL> __device__ __forceinline__ f32x4 value(raw4<T> raw, uint32_t block, int i) const { return inside<FULL>(block, i) ? widen4<T>(raw) : f32x4(0.f); }
-    // m and 1 - a of a place
-    template <bool FULL, bool RESETS> __device__ __forceinline__ void gates(raw4<T> forget, uint8_t reset, uint32_t block, int i, f32x4 &m, f32x4 &rest, f32x4 &on) const
+    // a, 1 behind the end, and 1 - a of a place
+    template <bool FULL> __device__ __forceinline__ void gates(raw4<T> forget, uint32_t block, int i, f32x4 &a, f32x4 &rest) const
     {
         const f32x4 f = widen4<T>(forget) + bias;
         const bool in = inside<FULL>(block, i);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const Gate g = gate_of<T>(f[k]);
-            on[k] = g.on;
-            m[k] = !in ? 1.f : RESETS && reset ? 0.f : g.on;
+            a[k] = in ? g.on : 1.f;
             rest[k] = in ? g.off : 0.f;
         }
     }
@@ -278,12 +310,13 @@ template <typename T, int WAVES, int L> struct Place {
 // Few sequences of few channels are cut into parts.  One launch says what each part does to the state (BACK: to the gradient that comes from
 // behind), as one change; the next one's workgroups put the changes before their part together and walk along it.  Here nothing
 // but the end of a part is wanted, so each group of 16 threads goes along a run of its own, without a scan until the last place.
+// With resets m is -0 where a document begins in the part: gates and their products are never negative.
 // The part that nobody comes behind has the place of its change for the state that the sequence begins with: the second launch does not read that where
 // the caller has it, since the last state may be written over it.
 
 template <typename T, int WAVES, int L, bool RESETS, bool BACK, bool GATE> __global__ __launch_bounds__(WAVES * 64) void k_recurrence_changes(RecurrenceArgs a)
 {
-    __shared__ Change room[WAVES][16];
+    __shared__ Change<RESETS> room[WAVES][16];
     const Job job(a);
     const Place<T, WAVES, L> p(a, job);
     float *to = a.changes + (uint64_t(job.sequence) * a.segments + job.segment) * 2u * a.channels + p.ch.first;
@@ -296,7 +329,7 @@ template <typename T, int WAVES, int L, bool RESETS, bool BACK, bool GATE> __glo
     const uint32_t begin = min(job.begin + group * each, last), count = min(each, last - begin);
     const Steps forget_of = p.steps(a.forget), other_of = p.steps(BACK ? a.y : a.x), out_of = p.steps(a.out);
     const uint8_t *resets = RESETS ? a.resets + int64_t(p.b) * a.resets_stride : nullptr;
-    Change all = {1.f, 0.f};
+    Change<RESETS> all = no_change<RESETS>();
     for (uint32_t n = 0; n < count; n += L) {
         raw4<T> forget[L], other[L], out[L];
         uint8_t reset[L];
@@ -323,40 +356,40 @@ template <typename T, int WAVES, int L, bool RESETS, bool BACK, bool GATE> __glo
 #pragma unroll
                 for (int k = 0; k < 4; ++k) v[k] *= sigmoid_of<T>(o[k]);
             }
-            Change c;
+            Change<RESETS> c = no_change<RESETS>();
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const Gate g = gate_of<T>(f[k]);
-                c.m[k] = !in ? 1.f : RESETS && reset[i] ? 0.f : g.on;
+                c.m[k] = in ? g.on : 1.f;
                 c.v[k] = !in ? 0.f : BACK ? v[k] : g.off * v[k];
             }
-            if constexpr (BACK) {
-#pragma unroll
-                for (int k = 0; k < 4; ++k) all.v[k] = through<RESETS>(c.m[k], c.v[k] + all.v[k]);
-                all.m *= c.m;
+            if constexpr (RESETS) c.cut = in && reset[i];
+            if constexpr (BACK) {   // what comes from behind and what the place adds go through it together
+                c.v = back_through(c, c.v + all.v);
+                all = change_of<RESETS>(all.m * c.m, c.v, cut_of(all) | cut_of(c));
             } else {
-                all = then<RESETS>(all, c);
+                all = then(all, c);
             }
         }
     }
     // the change of the whole part: what the groups do one after the other
-    Change of_wave;
+    Change<RESETS> of_wave;
     before_groups<RESETS, BACK>(all, of_wave);
     const uint32_t lane = threadIdx.x % 64u;
     if (lane < 16u) room[threadIdx.x / 64u][lane] = of_wave;
     __syncthreads();
     if (threadIdx.x >= 16u) return;
-    Change total = {1.f, 0.f};
+    Change<RESETS> total = no_change<RESETS>();
 #pragma unroll
-    for (int i = 0; i < WAVES; ++i) total = then<RESETS>(total, room[BACK ? WAVES - 1 - i : i][lane]);
-    p.ch.store(to, total.m);
+    for (int i = 0; i < WAVES; ++i) total = then(total, room[BACK ? WAVES - 1 - i : i][lane]);
+    p.ch.store(to, cut_of(total) ? f32x4(-0.f) : total.m);
     p.ch.store(to + a.channels, total.v);
 }
 
 // The state that a part begins with (BACK: the gradient from behind it), from that of the sequence: groups of 16 threads put runs of the
 // changes before it together.
 template <int WAVES, bool RESETS, bool BACK, typename P>
-__device__ __forceinline__ f32x4 begin_of_part(const RecurrenceArgs &a, const P &p, const Job &job, Change (&room)[WAVES][16])
+__device__ __forceinline__ f32x4 begin_of_part(const RecurrenceArgs &a, const P &p, const Job &job, Change<RESETS> (&room)[WAVES][16])
 {
     f32x4 carry = 0.f;
     if (a.segments == 1u) {
@@ -366,11 +399,12 @@ __device__ __forceinline__ f32x4 begin_of_part(const RecurrenceArgs &a, const P 
     carry = p.ch.load(a.changes + (uint64_t(job.sequence) * a.segments + (BACK ? 0u : a.segments - 1u)) * 2u * a.channels + p.ch.first);
     const uint32_t before = BACK ? a.segments - 1u - job.segment : job.segment, each = (before + WAVES * 4u - 1u) / (WAVES * 4u), group = threadIdx.x / 16u;
     const uint32_t order = BACK ? WAVES * 4u - 1u - group : group;
-    Change all = {1.f, 0.f};
+    Change<RESETS> all = no_change<RESETS>();
     for (uint32_t i = order * each; i < min((order + 1u) * each, before); ++i) {
         const uint32_t segment = BACK ? a.segments - 1u - i : i;
         const float *from = a.changes + (uint64_t(job.sequence) * a.segments + segment) * 2u * a.channels + p.ch.first;
-        all = then<RESETS>(all, {p.ch.load(from), p.ch.load(from + a.channels)});
+        const f32x4 m = p.ch.load(from);
+        all = then(all, change_of<RESETS>(m, p.ch.load(from + a.channels), __builtin_bit_cast(uint32_t, float(m[0])) == 0x80000000u));
     }
     begin_of<WAVES, RESETS, BACK>(all, carry, room);
     return carry;
@@ -383,7 +417,7 @@ __device__ __forceinline__ f32x4 begin_of_part(const RecurrenceArgs &a, const P 
 template <typename T, int WAVES, int L, bool RESETS, bool GATE> __global__ __launch_bounds__(WAVES * 64, 2) void k_recurrence_forward(RecurrenceArgs a)
 {
     using P = Place<T, WAVES, L>;
-    __shared__ Change room[3][WAVES][16];
+    __shared__ Change<RESETS> room[3][WAVES][16];
     const Job job(a);
     const P p(a, job);
     const Steps x_of = p.steps(a.x), forget_of = p.steps(a.forget), out_of = p.steps(a.out), y_of = p.steps(a.y);
@@ -406,14 +440,17 @@ template <typename T, int WAVES, int L, bool RESETS, bool GATE> __global__ __lau
     auto work = [&](uint32_t block, auto full) __attribute__((always_inline)) {
         constexpr bool FULL = decltype(full)::value;
         raw4<T> out_now[L];
-        Change step[L], all = {1.f, 0.f};
+        f32x4 m[L], v[L];
+        Change<RESETS> all = no_change<RESETS>();
         if constexpr (!FULL) fetch(block, full);
+        const uint32_t cuts = p.template cuts_of<FULL, RESETS>(reset, block);
+        auto step = [&](int i) __attribute__((always_inline)) { return change_of<RESETS>(m[i], v[i], cuts & 1u << i); };
 #pragma unroll
         for (int i = 0; i < L; ++i) {
-            f32x4 rest, on;
-            p.template gates<FULL, RESETS>(forget[i], reset[i], block, i, step[i].m, rest, on);
-            step[i].v = rest * p.template value<FULL>(x[i], block, i);
-            all = then<RESETS>(all, step[i]);
+            f32x4 rest;
+            p.template gates<FULL>(forget[i], block, i, m[i], rest);
+            v[i] = rest * p.template value<FULL>(x[i], block, i);
+            all = then(all, step(i));
             out_now[i] = out[i];
         }
         if constexpr (FULL) fetch(min(block + P::kSteps, full_end - P::kSteps), full);
@@ -424,7 +461,7 @@ template <typename T, int WAVES, int L, bool RESETS, bool GATE> __global__ __lau
         keep(t0, h);
 #pragma unroll
         for (int i = 0; i < L; ++i) {
-            h = applied<RESETS>(step[i], h);
+            h = applied(step(i), h);
             f32x4 y = h;
             if constexpr (GATE) {
                 const f32x4 o = widen4<T>(out_now[i]);
@@ -447,7 +484,7 @@ template <typename T, int WAVES, int L, bool RESETS, bool GATE> __global__ __lau
 {
     using P = Place<T, WAVES, L>;
     static_assert(ADACOMP_RECURRENCE_KEEP % P::kSteps == 0 || P::kSteps % ADACOMP_RECURRENCE_KEEP == 0, "a block begins with a state that was kept, or is the only one");
-    __shared__ Change room[5][WAVES][16];
+    __shared__ Change<RESETS> room[5][WAVES][16];
     __shared__ f32x4 sums[WAVES * 4][16];
     const Job job(a);
     const P p(a, job);
@@ -472,15 +509,17 @@ template <typename T, int WAVES, int L, bool RESETS, bool GATE> __global__ __lau
         constexpr bool FULL = decltype(full)::value;
         if constexpr (!FULL) fetch(block, full);
         raw4<T> x[L], out[L], dy[L];
-        f32x4 m[L], rest[L], on[L], state = next_state;
-        Change all = {1.f, 0.f}, back = {1.f, 0.f};
+        f32x4 m[L], rest[L], state = next_state;   // m: a
+        Change<RESETS> all = no_change<RESETS>(), back = all;
+        const uint32_t cuts = p.template cuts_of<FULL, RESETS>(next_reset, block);
+        auto step = [&](int i) __attribute__((always_inline)) { return change_of<RESETS>(m[i], rest[i] * p.template value<FULL>(x[i], block, i), cuts & 1u << i); };
 #pragma unroll
         for (int i = 0; i < L; ++i) {
             x[i] = next_x[i];
             out[i] = next_out[i];
             dy[i] = next_dy[i];
-            p.template gates<FULL, RESETS>(next_forget[i], next_reset[i], block, i, m[i], rest[i], on[i]);
-            all = then<RESETS>(all, {m[i], rest[i] * p.template value<FULL>(x[i], block, i)});
+            p.template gates<FULL>(next_forget[i], block, i, m[i], rest[i]);
+            all = then(all, step(i));
         }
         if constexpr (FULL) fetch(max(block, job.begin + P::kSteps) - P::kSteps, full);
 #pragma unroll
@@ -491,10 +530,9 @@ template <typename T, int WAVES, int L, bool RESETS, bool GATE> __global__ __lau
 #pragma unroll
                 for (int k = 0; k < 4; ++k) d[k] *= sigmoid_of<T>(o[k]);
             }
-#pragma unroll
-            for (int k = 0; k < 4; ++k) back.v[k] = through<RESETS>(m[i][k], d[k] + back.v[k]);
+            back.v = back_through(step(i), d + back.v);
         }
-        back.m = all.m;
+        back = change_of<RESETS>(all.m, back.v, cut_of(all));
         f32x4 h[L];   // before each place
         h[0] = begin_of<WAVES, RESETS, false>(all, state, room[turn * 2u]);
         f32x4 c = begin_of<WAVES, RESETS, true>(back, carry, room[turn * 2u + 1u]);
@@ -503,13 +541,12 @@ template <typename T, int WAVES, int L, bool RESETS, bool GATE> __global__ __lau
         renew<T>(out);
         renew<T>(dy);
 #pragma unroll
-        for (int i = 1; i < L; ++i) h[i] = applied<RESETS>({m[i - 1], rest[i - 1] * p.template value<FULL>(x[i - 1], block, i - 1)}, h[i - 1]);
+        for (int i = 1; i < L; ++i) h[i] = applied(step(i - 1), h[i - 1]);
 #pragma unroll
         for (int i = L - 1; i >= 0; --i) {
             const f32x4 xi = p.template value<FULL>(x[i], block, i), up = p.template value<FULL>(dy[i], block, i);
-            f32x4 g = up, came, df, dout;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) came[k] = RESETS && m[i][k] == 0.f ? 0.f : h[i][k];
+            const f32x4 came = cut_of(step(i)) ? f32x4(0.f) : h[i];
+            f32x4 g = up, df, dout;
             if constexpr (GATE) {
                 const f32x4 o = p.template value<FULL>(out[i], block, i);
 #pragma unroll
@@ -523,8 +560,8 @@ template <typename T, int WAVES, int L, bool RESETS, bool GATE> __global__ __lau
             g += c;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                c[k] = through<RESETS>(m[i][k], g[k]);
-                df[k] = g[k] * ((RESETS ? on[i][k] : m[i][k]) * rest[i][k]) * (came[k] - xi[k]);   // behind the end `rest` is 0
+                c[k] = cut_of(step(i)) ? 0.f : m[i][k] * g[k];
+                df[k] = g[k] * (m[i][k] * rest[i][k]) * (came[k] - xi[k]);   // behind the end `rest` is 0
             }
             if (!p.template inside<FULL>(block, i)) df = 0.f;
             dbias += df;
