@@ -101,6 +101,10 @@ inline RecurrenceForm recurrence_form(uint32_t batch, uint32_t length, uint32_t 
     return {(length + segment - 1u) / segment, segment};
 }
 
+// Sequences of a launch of workgroups of up to kRecurrenceThreads, `of_one` of them to a sequence: a grid is counted in threads, in 32 bits.
+constexpr uint32_t kRecurrenceThreads = 512;
+constexpr uint32_t recurrence_sequences(uint32_t of_one) { return (1u << 31) / kRecurrenceThreads / of_one; }
+
 struct BiasSumArgs {
     const float *parts;
     float *dbias;

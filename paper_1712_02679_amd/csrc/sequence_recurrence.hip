@@ -668,11 +668,11 @@ template <typename T, bool GATE> constexpr int kBackwardRun = sizeof(T) == 4 && 
 // 4 x 16 x 512 10.8 / 9.0).
 static bool place_by_place(const RecurrenceArgs &a) { return a.length <= std::max<uint64_t>(12u, uint64_t(a.batch) * a.slabs / 48u); }
 
-// Calls f with the arguments and the grid of every launch: a grid is counted in threads, in 32 bits.
+// Calls f with the arguments and the grid of every launch.
 template <typename F> static int for_sequences(const RecurrenceArgs &args, F &&f)
 {
     RecurrenceArgs a = args;
-    const uint32_t of_one = a.slabs * a.segments, step = (1u << 23) / of_one;
+    const uint32_t of_one = a.slabs * a.segments, step = recurrence_sequences(of_one);
     for (uint64_t first = 0; first < args.batch; first += step) {
         a.first_sequence = uint32_t(first);
         if (int rc = f(a, dim3(uint32_t(std::min<uint64_t>(step, args.batch - first)) * of_one))) return rc;
@@ -716,6 +716,7 @@ int launch_recurrence_forward(const RecurrenceArgs &args, uint32_t dtype, void *
         return with_form(a, dtype, [&](auto of, auto resets, auto gate) {
             using T = decltype(of);
             constexpr bool RESETS = decltype(resets)::value, GATE = decltype(gate)::value;
+            static_assert(kWaves * 64u <= kRecurrenceThreads);
             if (a.segments > 1u) hipLaunchKernelGGL((k_recurrence_changes<T, 4, 8, RESETS, false, false>), grid, dim3(256), 0, s, a);
             hipLaunchKernelGGL((k_recurrence_forward<T, kWaves, kForwardRun<T>, RESETS, GATE>), grid, dim3(kWaves * 64), 0, s, a);
         });
@@ -731,6 +732,7 @@ int launch_recurrence_backward(const RecurrenceArgs &args, uint32_t dtype, void 
             constexpr bool RESETS = decltype(resets)::value, GATE = decltype(gate)::value;
             if (a.segments > 1u) hipLaunchKernelGGL((k_recurrence_changes<T, 4, 8, RESETS, true, GATE>), grid, dim3(256), 0, s, a);
             constexpr int L = kBackwardRun<T, GATE>, WAVES = 16 / L;   // blocks of 64 places, or 16 or 32 where the sequence has no more
+            static_assert(WAVES * 64u <= kRecurrenceThreads);
             if (a.length <= 16u) hipLaunchKernelGGL((k_recurrence_backward<T, WAVES / 4, L, RESETS, GATE>), grid, dim3(WAVES * 16), 0, s, a);
             else if (a.length <= 32u) hipLaunchKernelGGL((k_recurrence_backward<T, WAVES / 2, L, RESETS, GATE>), grid, dim3(WAVES * 32), 0, s, a);
             else hipLaunchKernelGGL((k_recurrence_backward<T, WAVES, L, RESETS, GATE>), grid, dim3(WAVES * 64), 0, s, a);
