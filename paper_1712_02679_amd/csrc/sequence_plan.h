@@ -127,8 +127,9 @@ struct DistillArgs {
     uint64_t rows;
     uint32_t vocab, top;
     uint32_t tokens64, targets64, teacher_dtype;
-    float per_temperature, soft, hard;   // 1 / temperature; soft temperature^2 of a loss, soft temperature of a gradient:
-    float soft_loss, soft_grad, scale;
+    float per_temperature, hard;    // 1 / temperature
+    float soft_loss, soft_grad;     // soft temperature^2 of a loss, soft temperature of a gradient
+    float scale;
 };
 
 // Threads to a row, groups of 8 logits to a thread, whether a row is held in registers.  Short rows are held, with the entries of all teams within 64 KB of
