@@ -36,7 +36,9 @@ int adacomp_embed_forward(const adacomp_embed_t *op, const float *table, void *y
 size_t adacomp_embed_workspace_bytes(uint64_t rows, uint32_t vocab, uint32_t cols);
 
 /* dtable[v] = sum over the rows r with token v of scale D(dy[r]), added up in the order of the rows in pieces that the sizes decide.
- * accumulate != 0 adds to what is there (rows of tokens that do not occur are left alone), 0 overwrites all of dtable. */
+ * accumulate != 0 adds to what is there (rows of tokens that do not occur are left alone), 0 overwrites all of dtable.
+ * Made for mini-batches: for each part of the vocabulary, of up to 512 tokens, the tokens of all rows are looked at, so that the time grows with
+ * rows times vocab where both are large (64 columns bf16: 2^20 rows over 50000 tokens 0.57 ms, over 262144 1.05 ms). */
 int adacomp_embed_backward(const adacomp_embed_t *op, const void *dy, float *dtable, const adacomp_dropout_t *dropout, int accumulate,
                            void *workspace, size_t workspace_bytes, void *hip_stream);
 

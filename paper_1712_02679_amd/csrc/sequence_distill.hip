@@ -9,6 +9,8 @@
 // odd addresses, 210 us (3.9 TB/s; 193 without the 101 places a row that are written again).  Loss and gradient at once read them twice, the second time from the
 // memory-side cache for the most part: 4096 x 65536 291 us, where the two calls take 335; 5003 x 5999 f16 with two temperatures 37 us, bound by 33 vector instructions and 4
 // exponentials a value.  Results of 16 bits go past the caches although some are written again: through them 4096 x 65536 takes 259 us.
+// Cross entropy alone: 4096 x 65536 bf16 losses 100, both 271, the gradient 220 us; 32768 x 65 7.5, 12.3 and 9.9.  A row is never shared out over workgroups: 16 x 131072
+// bf16 with 64 top tokens takes 11, 25 and 19 us.
 #include "layers_device.h"
 #include "sequence_plan.h"
 

@@ -11,8 +11,8 @@
 // Forward reads x, forget and out and writes y, backward reads them and dy and writes their gradients.  8 x 2048 x 4096 bf16 with a gate: 123 us (4.4 TB/s),
 // backward 220 (4.3 TB/s); without its exponentials the same kernel takes 123 and 218, so memory and its order bound it: rows of 128 bytes from 3 to 7 tensors (32 x
 // 512 x 4096 126 us; 8 x 2048 x 2048, half of which the memory-side cache holds, 53 us, 5.0 TB/s).  Runs of 4 / 8 places in the forward pass of 16 bits 128 / 124
-// us, and in the backward pass 227 / 617 (registers in memory).  In parts, 1 x 65536 x 512 f16 without a gate: 31 us for the changes and 38 for the walk (2.9 TB/s of what it
-// needs, 4.9 of what it reads and writes).
+// us, and in the backward pass 227 / 617 (registers in memory).  With resets 132 and 232 us, for 15 % more vector instructions.  In parts, 1 x 65536 x 512
+// f16 without a gate: 29 to 33 us for the changes and 38 to 40 for the walk (2.9 TB/s of what it needs, 4.9 of what it reads and writes).
 #include "layers_device.h"
 #include "sequence_plan.h"
 

@@ -109,7 +109,7 @@ def adacomp_embed_workspace_bytes(rows, vocab, cols) -> int:
 
 def adacomp_embed_backward(tokens, dy, dtable, workspace, scale=1.0, dropout=None, accumulate=False):
     """dtable (a part of the flat gradient): the sum of scale * D(dy) over the places of each token, all of it overwritten, or with accumulate
-    added to."""
+    added to.  Made for mini-batches: beyond some 100000 places the time grows with places times vocabulary (see adacomp_sequence.h)."""
     L = _bound or _lib()
     op, pdy, pt, dev = _embed(tokens, dy, dtable, scale, "dy")
     pw, nw = _room(workspace, dev)
