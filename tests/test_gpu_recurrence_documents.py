@@ -36,8 +36,12 @@ def check(A, s, dtype, dy, dlast):
     agree(g["last"], r.last, r.last_bound(), "last")
     want, off = r.states()
     agree(g["states"], want, off + 4 * S.U * want.abs(), "states")
-    got = backward(A, g, dy, dlast, dtype)
-    for name, (value, off) in r.backward(dy.double(), dlast.double()).items():
+    got, want = backward(A, g, dy, dlast, dtype), r.backward(dy.double(), dlast.double())
+    for name in {"dx", "dforget", "dout"} & set(want):   # zeros behind the end, where the formula has 0 times what is not finite
+        want[name] = tuple(torch.where(r.inside, v, 0.0) for v in want[name])
+    df, off = want["dforget"]
+    want["dbias"] = (df.sum((0, 1)), off.sum((0, 1)) + S.U * (r.n + df.shape[0] + 64) * df.abs().sum((0, 1)))
+    for name, (value, off) in want.items():
         agree(got[name], value, rounded(value, off, dtype if name in ("dx", "dforget", "dout") else F32), name)
 
 
@@ -68,6 +72,23 @@ def test_what_is_not_finite_stays_in_its_document(A, batch, length, channels, wh
     some = at[..., None] & (torch.arange(channels) % 3 != 1)
     t = dy if where == "dy" else s[where.split()[0]]
     t[some] = INF if "infinite" in where else NAN
+    check(A, s, dtype, dy, dlast)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("batch,length,channels", SHAPES)
+def test_documents_of_ragged_sequences(A, batch, length, channels, dtype):
+    """NaN and resets behind the ends too, where they change nothing."""
+    s = recurrence_case(batch, length, channels, dtype, True, True, True, True, False, 39)
+    s["resets"] = documents(batch, length, 40) * 200   # any number but 0
+    dy, dlast = rand((batch, length, channels), dtype, 77), rand((batch, channels), F32, 78)
+    g = torch.Generator().manual_seed(41)
+    for t in (s["x"], s["forget"], s["out"], dy):
+        t[torch.rand(t.shape, generator=g) < 0.001] = NAN
+        for i, end in enumerate(s["lengths"].tolist()):
+            t[i, end:] = NAN
+    for i, end in enumerate(s["lengths"].tolist()):
+        s["resets"][i, end:] = 1
     check(A, s, dtype, dy, dlast)
 
 
